@@ -323,6 +323,113 @@ typedef struct {
 } qadam_profile_work_t;
 int qadam_profile_work(qadam_handle_t h, qadam_profile_work_t* out);
 
+/* ------------------------------------------------------------------------------------------------
+ * Operators beside the step: an ordinary optimizer for lists of tensors, the norm that clips gradients, and the embedding at both
+ * ends of the layer that is the largest of a language model's vector.  They keep the conventions above (device pointers, streams,
+ * return values, allocation only in the init calls), with these differences:
+ *   - buffers need the alignment of their own elements only, since tensors may be slices of a flat vector at any offset;
+ *   - a tensor's elements, and those of a matrix's row, lie one behind the other; rows may lie further apart;
+ *   - calls on one handle share its scratch: order them (one stream, or events).
+ * Sums, moments and norms are taken in fp32 or wider whatever the buffers' types; a result is rounded to its buffer's type once, to
+ * nearest, ties to even. */
+
+/* element types */
+#define QADAM_F32     0
+#define QADAM_BF16    1
+#define QADAM_F16     2
+#define QADAM_CODES8  3     /* weight codes (see above) in int8 and int16, with the k_x they were made with */
+#define QADAM_CODES16 4
+
+/* AdamW with decoupled weight decay over a list of tensors in one call.  For every element of a tensor with a gradient, in fp32 with one
+ * rounding per operation (t = step, c = the gradients' factor):
+ *     g = c grad;   m <- beta1 m + (1-beta1) g;   v <- beta2 v + (1-beta2) g^2;
+ *     x <- x - (lr decay) x;   x <- x - (lr / (1-beta1^t)) m / (sqrt(v) / sqrt(1-beta2^t) + eps)
+ * and copy <- x, in another type, where a tensor has a copy (the weights that a model computes with).
+ *
+ * state_bits = 32: m and v are fp32.  state_bits = 8: m and r = sqrt(v) are kept in blocks of QADAM_STATE_BLOCK consecutive elements
+ * of a tensor (the last one may be shorter), each block with an fp32 scale, the elements as 8-bit floats with 4 exponent and 3 mantissa
+ * bits (the finite-only kind, largest value 448) of the value divided by the scale:
+ *     m_scales[b] = max|m| / 448,    m[i] = nearest(m (448 / max|m|));
+ *     v_scales[b] = max r / 448,     v[i] = nearest(max(r (448 / max r), v > 0 ? 2^-9 : 0)).
+ * The step itself takes the moments before this rounding.  2^-9 is the smallest positive value of the kind: a second moment above zero
+ * never becomes zero, where m / (sqrt(v) + eps) would run away.  A block with max|m| < 2^-116 is kept as zeros.  A moment that is not
+ * finite makes its whole block unusable: pass the factor of qadam_grad_norm, which skips such a step. */
+#define QADAM_STATE_BLOCK 256
+
+typedef struct qadam_adamw_ctx* qadam_adamw_t;
+
+typedef struct {
+    uint32_t struct_size;   /* = sizeof(qadam_adamw_config_t) */
+    int32_t  state_bits;    /* 32 or 8 */
+    double   beta1, beta2;  /* in [0, 1); double, so that 1 - beta is rounded to fp32 once */
+    double   eps;           /* >= 0 */
+} qadam_adamw_config_t;
+
+/* One tensor.  The buffers stay the caller's; their addresses are read at qadam_adamw_init and the handle steps these buffers from then
+ * on, so they live as long as it does. */
+typedef struct {
+    int64_t numel;          /* >= 0 */
+    void*   param;          /* x: QADAM_F32, QADAM_BF16 or QADAM_F16; without fp32 weights an update below half a unit of x's last
+                               place is lost */
+    void*   m;              /* fp32, or one byte per element */
+    void*   v;
+    float*  m_scales;       /* state_bits = 8: ceil(numel / QADAM_STATE_BLOCK); else NULL */
+    float*  v_scales;
+    void*   copy;           /* NULL, or the copy; only beside QADAM_F32 weights */
+    int32_t param_type, grad_type;
+    int32_t copy_type;      /* QADAM_BF16 or QADAM_F16 */
+    float   weight_decay;   /* >= 0 */
+} qadam_adamw_tensor_t;
+
+int qadam_adamw_init(qadam_adamw_t* out, const qadam_adamw_config_t* cfg, const qadam_adamw_tensor_t* tensors, int32_t num_tensors);
+int qadam_adamw_destroy(qadam_adamw_t h);
+
+/* One step.  grads: HOST array of num_tensors device pointers, read during the call; NULL: that tensor has no gradient in this step and
+ * nothing of it changes, its weight decay included.  grad_factor_dev: one fp32 on the device that all gradients are multiplied with
+ * (the second value of qadam_grad_norm's result), or NULL: 1.  A factor that is NaN or infinite skips the whole step: no buffer
+ * changes.  The bias corrections depend on `step` >= 1, so a call is not recorded into a graph (QADAM_EINVAL). */
+int qadam_adamw_step(qadam_adamw_t h, int64_t step, float lr, const void* const* grads, const float* grad_factor_dev, void* stream);
+
+/* Euclidean norm over all tensors of a list, and the factor that clips it:
+ *     out[0] = n = sqrt(sum of all squares),   out[1] = n > max_norm ? max_norm / n : 1;  NaN if n is not finite.
+ * out_dev: two fp32 on the device.  Squares and sums in fp64 and in a fixed order: the same bits on every run, and no overflow (n itself
+ * may be beyond fp32: out[0] is then infinite, out[1] is not).  grads: as in qadam_adamw_step; NULL counts as zeros.  max_norm >= 0;
+ * infinite: the norm alone.  May be recorded into a graph. */
+typedef struct qadam_grad_norm_ctx* qadam_grad_norm_t;
+int qadam_grad_norm_init(qadam_grad_norm_t* out, const int64_t* numels, const int32_t* grad_types, int32_t num_tensors);
+int qadam_grad_norm_destroy(qadam_grad_norm_t h);
+int qadam_grad_norm(qadam_grad_norm_t h, const void* const* grads, float max_norm, float* out_dev, void* stream);
+
+/* Embedding: a matrix of `rows` rows of `dim` elements, looked up by tokens.  max_tokens bounds num_tokens of qadam_embedding_grad,
+ * whose scratch the handle allocates.  Tokens are int32 or int64 (token_bytes 4 or 8).  `padding`: the row of a token that stands for
+ * no text, or a number outside 0..rows-1 for none.  A token outside 0..rows-1 sets QADAM_STATUS_TOKEN_RANGE in the handle's status
+ * word.  Both kinds look up zeros and have no gradient.  Strides: elements from one row to the next. */
+typedef struct qadam_embedding_ctx* qadam_embedding_t;
+#define QADAM_STATUS_TOKEN_RANGE 4u
+
+int qadam_embedding_init(qadam_embedding_t* out, int64_t rows, int32_t dim, int64_t max_tokens);
+int qadam_embedding_destroy(qadam_embedding_t h);
+
+/* out[t] = scale * weight[tokens[t]], t = 0..num_tokens-1 (any number of them).
+ *   weight      matrix in any element type; weight codes with their k_x (0..14, else ignored): x^ = j 2^-(k_x+1), the layer's part of
+ *               what qadam_step_fused emits, without the vector x^ in between; weight_stride >= dim
+ *   out         QADAM_F32, QADAM_BF16 or QADAM_F16; out_stride >= dim */
+int qadam_embedding_lookup(qadam_embedding_t h, const void* weight, int32_t weight_type, int32_t k_x, int64_t weight_stride,
+                           const void* tokens, int32_t token_bytes, int64_t num_tokens, int64_t padding, float scale,
+                           void* out, int32_t out_type, int64_t out_stride, void* stream);
+
+/* Gradient of the lookup: grad[r] = scale * (sum of dout[t] over the t with tokens[t] = r), for every row r; accumulate = 1: added to
+ * what grad[r] holds, and rows without a token are not touched.
+ * The tokens are sorted, and each row's sum is taken in fp32 over its dout[t] in an order that depends on the tokens alone: the same
+ * bits on every run.
+ *   dout        QADAM_F32, QADAM_BF16 or QADAM_F16; dout_stride >= 0 (0: one row for all tokens)
+ *   grad        QADAM_F32, QADAM_BF16 or QADAM_F16, rows x dim; grad_stride >= dim: may be the layer's part of a flat gradient vector */
+int qadam_embedding_grad(qadam_embedding_t h, const void* tokens, int32_t token_bytes, int64_t num_tokens, int64_t padding,
+                         float scale, const void* dout, int32_t dout_type, int64_t dout_stride,
+                         void* grad, int32_t grad_type, int64_t grad_stride, int32_t accumulate, void* stream);
+
+int qadam_embedding_get_status(qadam_embedding_t h, qadam_status_t* out, int32_t clear, void* stream);
+
 /* Text of the last HIP error seen by this thread's calls (static storage). */
 const char* qadam_last_error(void);
 

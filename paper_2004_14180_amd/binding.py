@@ -21,6 +21,9 @@ QADAM_MAX_WORKERS = 32
 QADAM_IDENTITY = -1          # k_g or k_x: that quantizer is the identity
 QADAM_STATUS_NONFINITE_SCALE = 1
 QADAM_STATUS_ERR_BOUND_VIOLATED = 2
+QADAM_STATUS_TOKEN_RANGE = 4
+QADAM_F32, QADAM_BF16, QADAM_F16, QADAM_CODES8, QADAM_CODES16 = range(5)    # element types
+QADAM_STATE_BLOCK = 256
 
 EXPORTS = [
     "qadam_init", "qadam_destroy", "qadam_grad_code_bytes", "qadam_weight_code_bytes",
@@ -29,6 +32,10 @@ EXPORTS = [
     "qadam_weight_dequantize_f16", "qadam_layer_sumsq", "qadam_trust_error_buffers",
     "qadam_get_status", "qadam_last_error", "qadam_profile_enable", "qadam_profile_read", "qadam_profile_work",
     "qadam_quantize_segment_noalloc", "qadam_arena_layout", "qadam_set_scale_polls",
+    "qadam_adamw_init", "qadam_adamw_destroy", "qadam_adamw_step",
+    "qadam_grad_norm_init", "qadam_grad_norm_destroy", "qadam_grad_norm",
+    "qadam_embedding_init", "qadam_embedding_destroy", "qadam_embedding_lookup", "qadam_embedding_grad",
+    "qadam_embedding_get_status",
 ]
 
 
@@ -60,6 +67,16 @@ class _Arena(C.Structure):
 
 class _Status(C.Structure):
     _fields_ = [("flags", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class _AdamWConfig(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("state_bits", C.c_int32), ("beta1", C.c_double), ("beta2", C.c_double),
+                ("eps", C.c_double)]
+
+
+class _AdamWTensor(C.Structure):
+    _fields_ = [("numel", C.c_int64)] + [(n, C.c_void_p) for n in ("param", "m", "v", "m_scales", "v_scales", "copy")] + \
+               [("param_type", C.c_int32), ("grad_type", C.c_int32), ("copy_type", C.c_int32), ("weight_decay", C.c_float)]
 
 
 @dataclass
@@ -149,6 +166,17 @@ def load_library():
     lib.qadam_profile_work.argtypes = [vp, C.POINTER(_ProfileWork)]
     lib.qadam_quantize_segment_noalloc.argtypes = [i32, i64, vp, vp, vp, vp, vp]
     lib.qadam_arena_layout.argtypes = [vp, C.c_size_t, i32, C.POINTER(_Arena)]
+    lib.qadam_adamw_init.argtypes = [C.POINTER(vp), C.POINTER(_AdamWConfig), C.POINTER(_AdamWTensor), i32]
+    lib.qadam_adamw_destroy.argtypes = [vp]
+    lib.qadam_adamw_step.argtypes = [vp, i64, f32, C.POINTER(vp), vp, vp]
+    lib.qadam_grad_norm_init.argtypes = [C.POINTER(vp), C.POINTER(i64), C.POINTER(i32), i32]
+    lib.qadam_grad_norm_destroy.argtypes = [vp]
+    lib.qadam_grad_norm.argtypes = [vp, C.POINTER(vp), f32, vp, vp]
+    lib.qadam_embedding_init.argtypes = [C.POINTER(vp), i64, i32, i64]
+    lib.qadam_embedding_destroy.argtypes = [vp]
+    lib.qadam_embedding_lookup.argtypes = [vp, vp, i32, i32, i64, vp, i32, i64, i64, f32, vp, i32, i64, vp]
+    lib.qadam_embedding_grad.argtypes = [vp, vp, i32, i64, i64, f32, vp, i32, i64, vp, i32, i64, i32, vp]
+    lib.qadam_embedding_get_status.argtypes = [vp, C.POINTER(_Status), i32, vp]
     _native, _segment = _load_native(torch), _address(lib.qadam_quantize_segment_noalloc)
     _lib, _torch = lib, torch
     return lib

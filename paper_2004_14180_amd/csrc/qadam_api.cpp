@@ -56,26 +56,28 @@ struct qadam_ctx {
 };
 
 namespace {
-
 thread_local char g_last_error[256] = "";
+}
 
-int hip_fail(hipError_t e, const char* what)
+int qadam::hip_fail(hipError_t e, const char* what)
 {
     std::snprintf(g_last_error, sizeof g_last_error, "%s: %s", what, hipGetErrorString(e));
     return QADAM_EHIP;
 }
+
+int qadam::fail(int code, const char* msg)
+{
+    std::snprintf(g_last_error, sizeof g_last_error, "%s", msg);
+    return code;
+}
+
+namespace {
 
 #define QADAM_HIP(call)                                      \
     do {                                                     \
         hipError_t e_ = (call);                              \
         if (e_ != hipSuccess) return hip_fail(e_, #call);    \
     } while (0)
-
-int fail(int code, const char* msg)
-{
-    std::snprintf(g_last_error, sizeof g_last_error, "%s", msg);
-    return code;
-}
 
 // qadam_trust_error_buffers(h, 1): smallest number of (tile, worker) pairs of a call for which the filtered
 // scale pass, with its two extra launches, is faster than the full one (measured: slower on a 4-worker,

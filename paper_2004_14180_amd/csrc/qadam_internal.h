@@ -10,6 +10,10 @@
 
 namespace qadam {
 
+// Keep the text for qadam_last_error (defined in qadam_api.cpp): return `code`, QADAM_EHIP.
+int fail(int code, const char* msg);
+int hip_fail(hipError_t e, const char* what);
+
 // One unit of work of every kernel: a run of at most `tile_elems` consecutive elements that lies
 // inside one layer segment.  Tiles start at a multiple of the tile size from the segment start, so
 // the first element of a tile is the first element of a 32-element code group.

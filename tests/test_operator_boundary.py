@@ -1,0 +1,105 @@
+"""CPU-only checks of the operators beside the step: arguments are refused before anything touches a GPU, and what the compiler made of
+their kernels."""
+import ctypes as C
+import re
+
+import pytest
+import torch
+
+SOURCES = ["qadam_tensors.hip", "qadam_embedding.hip"]
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2004_14180_amd import binding
+    from paper_2004_14180_amd.build import build_library
+    import os
+    if not os.path.exists(binding.library_path()):
+        build_library(verbose=False)
+    return binding.load_library()
+
+
+def test_adamw_refuses_on_the_host(lib):
+    from paper_2004_14180_amd.binding import _AdamWConfig, _AdamWTensor
+    h = C.c_void_p()
+    good = dict(struct_size=C.sizeof(_AdamWConfig), state_bits=32, beta1=0.9, beta2=0.999, eps=1e-8)
+    tensor = dict(numel=4, param=256, m=256, v=256, m_scales=256, v_scales=256, copy=None, param_type=0, grad_type=0, copy_type=0,
+                  weight_decay=0.0)
+
+    def init(cfg=None, n=1, **t):
+        c = _AdamWConfig(**{**good, **(cfg or {})})
+        return lib.qadam_adamw_init(C.byref(h), C.byref(c), C.byref(_AdamWTensor(**{**tensor, **t})), n)
+
+    for cfg in [dict(struct_size=4), dict(state_bits=16), dict(beta1=1.0), dict(beta2=-0.5), dict(beta1=float("nan")), dict(eps=-1.0)]:
+        assert init(cfg) == -1, cfg
+        assert lib.qadam_last_error()
+    for t in [dict(numel=-1), dict(param=None), dict(m=None), dict(v=None), dict(param_type=3), dict(grad_type=-1), dict(weight_decay=-1.0),
+              dict(weight_decay=float("nan")), dict(copy=256, copy_type=0), dict(copy=256, copy_type=1, param_type=2), dict(n=-1)]:
+        assert init(**t) == -1, t
+    assert init(dict(state_bits=8), m_scales=None) == -1
+    for t in [dict(param=258), dict(m=257), dict(copy=257, copy_type=1), dict(param=257, param_type=1)]:
+        assert init(**t) == -2, t
+    assert init(dict(state_bits=8), v_scales=258) == -2
+    assert init(numel=(1 << 40) + 1) == -3 and init(numel=1 << 37) == -3
+    assert lib.qadam_adamw_init(None, None, None, 0) == -1 and lib.qadam_adamw_destroy(None) == 0
+    assert lib.qadam_adamw_step(None, 1, 1e-3, None, None, None) == -1
+
+
+def test_norm_and_embedding_refuse_on_the_host(lib):
+    h = C.c_void_p()
+    n64, n32 = (C.c_int64 * 1), (C.c_int32 * 1)
+    for numel, t, n, want in [(-1, 0, 1, -1), (4, 3, 1, -1), (4, 0, -1, -1), (1 << 41, 0, 1, -3), (1 << 37, 0, 1, -3)]:
+        assert lib.qadam_grad_norm_init(C.byref(h), n64(numel), n32(t), n) == want, numel
+    assert lib.qadam_grad_norm_init(C.byref(h), None, None, 1) == -1
+    assert lib.qadam_grad_norm(None, None, 1.0, None, None) == -1 and lib.qadam_grad_norm_destroy(None) == 0
+    for rows, dim, tokens, want in [(0, 1, 1, -1), (1, 0, 1, -1), (1, 1, -1, -1), ((1 << 30) + 1, 1, 1, -3), (1, (1 << 20) + 1, 1, -3),
+                                    (1, 1, (1 << 30) + 1, -3)]:
+        assert lib.qadam_embedding_init(C.byref(h), rows, dim, tokens) == want, (rows, dim, tokens)
+    assert lib.qadam_embedding_lookup(None, None, 0, 0, 1, None, 4, 0, -1, 1.0, None, 0, 1, None) == -1
+    assert lib.qadam_embedding_grad(None, None, 4, 0, -1, 1.0, None, 0, 1, None, 0, 1, 0, None) == -1
+    assert lib.qadam_embedding_get_status(None, None, 0, None) == -1 and lib.qadam_embedding_destroy(None) == 0
+
+
+def test_tensors_that_are_not_on_the_device_are_refused(lib):
+    from paper_2004_14180_amd import AdamW, AdamWConfig, adamw_state
+    p = [torch.zeros(4)]
+    for bits in (32, 8):
+        cfg = AdamWConfig(state_bits=bits)
+        with pytest.raises(ValueError, match="device tensor"):
+            AdamW(cfg, p, **adamw_state(cfg, p))
+
+
+def test_rows_of_a_matrix():
+    """The layouts that stand for rows at one distance, on tensors that pass the check of the device."""
+    from paper_2004_14180_amd import operators
+
+    class OnDevice:
+        def __init__(self, t):
+            self.t = t
+
+        def __getattr__(self, name):
+            return getattr(self.t, name)
+
+    def rows(t, n, dim):
+        return operators._rows(OnDevice(t), "t", n, dim)
+
+    old, operators._on_device = operators._on_device, lambda t, name: None
+    try:
+        z = torch.zeros
+        assert rows(z(6, 4), 6, 4) == 4 and rows(z(2, 3, 4), 6, 4) == 4 and rows(z(6, 9)[:, :4], 6, 4) == 9
+        assert rows(z(2, 3, 9)[..., 2:6], 6, 4) == 9 and rows(z(1, 4).expand(6, 4), 6, 4) == 0
+        assert rows(z(12, 4)[::2], 6, 4) == 8 and rows(z(6, 2)[:, :1], 6, 1) == 2 and rows(z(0, 4), 0, 4) == 4
+        assert rows(z(1, 9)[:, :4], 1, 4) == 4 and rows(z(6, 1, 9)[..., :4], 6, 4) == 9
+        for t in (z(4, 6).t(), z(6, 8)[:, ::2], z(2, 4, 4)[:, :3], z(3, 2, 4).transpose(0, 1), z(24), z(6, 5), z(5, 4), z(1, 1).expand(6, 4)):
+            with pytest.raises(ValueError):
+                rows(t, 6, 4)
+    finally:
+        operators._on_device = old
+
+
+@pytest.mark.parametrize("source", SOURCES)
+def test_the_kernels_keep_out_of_scratch_and_hold_no_packed_fp32(source):
+    from paper_2004_14180_amd.build import device_assembly, device_resource_usage
+    for name, u in device_resource_usage(source).items():
+        assert u["scratch_bytes"] == 0, "%s: %d bytes of scratch per lane" % (name, u["scratch_bytes"])
+    assert not re.findall(r"\bv_pk_(?:add|mul|fma)_f32\b", device_assembly(source))
