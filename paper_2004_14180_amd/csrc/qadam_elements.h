@@ -12,6 +12,11 @@ namespace qadam {
 
 typedef float f4 __attribute__((ext_vector_type(4)));
 
+// Addresses that a kernel reads from a table are global ones: said here, else the compiler takes the instructions that find out.
+#define QADAM_GLOBAL __attribute__((address_space(1)))
+template <typename T>
+__device__ __forceinline__ QADAM_GLOBAL T* global(T* p) { return (QADAM_GLOBAL T*)p; }
+
 template <int TYPE> struct Element;
 template <> struct Element<QADAM_F32> { typedef float T; };
 template <> struct Element<QADAM_BF16> { typedef __bf16 T; };
@@ -31,7 +36,7 @@ struct Run {
 template <int TYPE, int N, bool ONCE = true>
 __device__ __forceinline__ typename Run<TYPE, N>::V load_raw(const void* p)
 {
-    const auto* q = static_cast<const typename Run<TYPE, N>::U*>(p);
+    const auto* q = (const QADAM_GLOBAL typename Run<TYPE, N>::U*)p;
     if constexpr (ONCE) return __builtin_nontemporal_load(q);
     else return *q;
 }
@@ -46,7 +51,7 @@ template <int TYPE, int N, bool ONCE = true>
 __device__ __forceinline__ void store_run(void* p, typename Run<TYPE, N>::F x)
 {
     const auto v = __builtin_convertvector(x, typename Run<TYPE, N>::V);
-    auto* q = static_cast<typename Run<TYPE, N>::U*>(p);
+    auto* q = (QADAM_GLOBAL typename Run<TYPE, N>::U*)p;
     if constexpr (ONCE) __builtin_nontemporal_store(v, q);
     else *q = v;
 }
@@ -59,16 +64,16 @@ inline __host__ __device__ int element_size(int type)
 // one element of a type known at run time
 __device__ __forceinline__ float load_one(const void* p, int type, int64_t i)
 {
-    if (type == QADAM_F32) return static_cast<const float*>(p)[i];
-    if (type == QADAM_BF16) return (float)static_cast<const __bf16*>(p)[i];
-    return (float)static_cast<const _Float16*>(p)[i];
+    if (type == QADAM_F32) return global(static_cast<const float*>(p))[i];
+    if (type == QADAM_BF16) return (float)global(static_cast<const __bf16*>(p))[i];
+    return (float)global(static_cast<const _Float16*>(p))[i];
 }
 
 __device__ __forceinline__ void store_one(void* p, int type, int64_t i, float x)
 {
-    if (type == QADAM_F32) static_cast<float*>(p)[i] = x;
-    else if (type == QADAM_BF16) static_cast<__bf16*>(p)[i] = (__bf16)x;
-    else static_cast<_Float16*>(p)[i] = (_Float16)x;
+    if (type == QADAM_F32) global(static_cast<float*>(p))[i] = x;
+    else if (type == QADAM_BF16) global(static_cast<__bf16*>(p))[i] = (__bf16)x;
+    else global(static_cast<_Float16*>(p))[i] = (_Float16)x;
 }
 
 }  // namespace qadam

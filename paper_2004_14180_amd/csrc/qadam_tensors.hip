@@ -14,14 +14,24 @@ static_assert(kBlock == 4 * kWave, "");
 
 constexpr float kFp8Max = 448.0f, kFp8Least = 0x1p-9f, kTinyBlock = 0x1p-116f;
 
-// the largest of a wavefront's values, none of them negative, in every lane
-__device__ __forceinline__ float wave_max(float x)
+// the largest of a wavefront's values, none of them negative, in every lane: within rows of 16 lanes, then from row to row, by DPP
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t x)
 {
-    for (int d = 1; d < kWave; d <<= 1) {
-        const float y = __shfl_xor(x, d);
-        x = __float_as_uint(y) > __float_as_uint(x) ? y : x;        // a NaN sorts above every number
-    }
-    return x;
+    const uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, false);     // 0 from where there is no lane
+    return y > x ? y : x;
+}
+
+__device__ __forceinline__ float wave_max(float value)
+{
+    uint32_t x = __float_as_uint(value);        // orders like the values; a NaN is above every number
+    x = dpp_max<0x111>(x);      // one lane to the right, two, four, eight
+    x = dpp_max<0x112>(x);
+    x = dpp_max<0x114>(x);
+    x = dpp_max<0x118>(x);
+    x = dpp_max<0x142>(x);      // the row's last lane to the next row
+    x = dpp_max<0x143>(x);      // lane 31 to the upper half
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)x, kWave - 1));
 }
 
 // four values x (quotient of the block's scale) as four 8-bit floats
@@ -37,9 +47,15 @@ __device__ __forceinline__ f4 from_fp8(uint32_t c)
     return f4{lo[0], lo[1], hi[0], hi[1]};
 }
 
-struct Moments {
-    f4 m, v;
-};
+typedef uint32_t word_u __attribute__((aligned(1)));
+__device__ __forceinline__ uint32_t load_word(const uint8_t* p) { return __builtin_nontemporal_load((const QADAM_GLOBAL word_u*)p); }
+__device__ __forceinline__ void store_word(uint8_t* p, uint32_t x) { __builtin_nontemporal_store(x, (QADAM_GLOBAL word_u*)p); }
+
+// lane l's value in all lanes
+__device__ __forceinline__ float lane_value(float x, int l)
+{
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l));
+}
 
 // x, m, v of four elements after the step; `r`: sqrt(v)
 __device__ __forceinline__ void adamw(const AdamwScalars& S, float lr_decay, float factor, f4 grad, f4& x, f4& m, f4& v, f4& r)
@@ -79,16 +95,16 @@ __device__ void ragged_block(const AdamwScalars& S, const ListTensor& T, const v
     const int n = T.numel - first < 0 ? 0 : T.numel - first < 4 ? (int)(T.numel - first) : 4;
     f4 g = 0.0f, x = 0.0f, m = 0.0f, v = 0.0f, r;
     float sm = 0.0f, sv = 0.0f;
-    if (STATE8) { sm = T.m_scales[block]; sv = T.v_scales[block]; }
+    if (STATE8) { sm = global(T.m_scales)[block]; sv = global(T.v_scales)[block]; }
     for (int k = 0; k < n; ++k) {
         g[k] = load_one(grad, gt, first + k);
         x[k] = load_one(T.param, pt, first + k);
         if (STATE8) {
-            m[k] = __builtin_amdgcn_cvt_f32_fp8(static_cast<const uint8_t*>(T.m)[first + k], 0) * sm;
-            v[k] = __builtin_amdgcn_cvt_f32_fp8(static_cast<const uint8_t*>(T.v)[first + k], 0) * sv;
+            m[k] = __builtin_amdgcn_cvt_f32_fp8(global(static_cast<const uint8_t*>(T.m))[first + k], 0) * sm;
+            v[k] = __builtin_amdgcn_cvt_f32_fp8(global(static_cast<const uint8_t*>(T.v))[first + k], 0) * sv;
         } else {
-            m[k] = static_cast<const float*>(T.m)[first + k];
-            v[k] = static_cast<const float*>(T.v)[first + k];
+            m[k] = global(static_cast<const float*>(T.m))[first + k];
+            v[k] = global(static_cast<const float*>(T.v))[first + k];
         }
     }
     if (STATE8) v = v * v;
@@ -103,38 +119,124 @@ __device__ void ragged_block(const AdamwScalars& S, const ListTensor& T, const v
             if (r[k] > 0.0f && iv > 0.0f) qv[k] = fmaxf(qv[k], kFp8Least);
         cm = to_fp8(qm);
         cv = to_fp8(qv);
-        if (lane == 0) { T.m_scales[block] = nm; T.v_scales[block] = nv; }
+        if (lane == 0) { global(T.m_scales)[block] = nm; global(T.v_scales)[block] = nv; }
     }
     for (int k = 0; k < n; ++k) {
         store_one(T.param, pt, first + k, x[k]);
         if (ct != kNoCopy) store_one(T.copy, ct, first + k, x[k]);
         if (STATE8) {
-            static_cast<uint8_t*>(T.m)[first + k] = (uint8_t)(cm >> 8 * k);
-            static_cast<uint8_t*>(T.v)[first + k] = (uint8_t)(cv >> 8 * k);
+            global(static_cast<uint8_t*>(T.m))[first + k] = (uint8_t)(cm >> 8 * k);
+            global(static_cast<uint8_t*>(T.v))[first + k] = (uint8_t)(cv >> 8 * k);
         } else {
-            static_cast<float*>(T.m)[first + k] = m[k];
-            static_cast<float*>(T.v)[first + k] = v[k];
+            global(static_cast<float*>(T.m))[first + k] = m[k];
+            global(static_cast<float*>(T.v))[first + k] = v[k];
         }
     }
 }
 
-// A wavefront takes four blocks of one tensor, a workgroup a tile of four wavefronts.
+// Four whole blocks of a tensor, types known: all loads are under way before the first value is used.
+template <bool STATE8, int PT, int GT, int CT>
+__device__ __forceinline__ void whole_blocks(const AdamwScalars& S, const ListTensor& T, const void* grad, float lr_decay, float factor,
+                                             int64_t block, int lane)
+{
+    typedef typename Element<PT>::T P;
+    typedef typename Element<GT>::T G;
+    const int64_t first = block * kBlock;
+    const int at = lane * 4;
+    const G* gp = static_cast<const G*>(grad) + first;
+    P* xp = static_cast<P*>(T.param) + first;
+    typename Run<GT, 4>::V rg[kBlocks];
+    typename Run<PT, 4>::V rx[kBlocks];
+    f4 m[kBlocks], v[kBlocks];
+    uint32_t cm[kBlocks], cv[kBlocks];
+    float sm = 0.0f, sv = 0.0f;
+    if constexpr (STATE8) {
+        sm = global(T.m_scales)[block + lane % kBlocks];
+        sv = global(T.v_scales)[block + lane % kBlocks];
+    }
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+        rg[b] = load_raw<GT, 4>(gp + (b * kBlock + at));
+        if constexpr (STATE8) {
+            cm[b] = load_word(static_cast<const uint8_t*>(T.m) + first + (b * kBlock + at));
+            cv[b] = load_word(static_cast<const uint8_t*>(T.v) + first + (b * kBlock + at));
+        } else {
+            m[b] = load_raw<QADAM_F32, 4>(static_cast<const float*>(T.m) + first + (b * kBlock + at));
+            v[b] = load_raw<QADAM_F32, 4>(static_cast<const float*>(T.v) + first + (b * kBlock + at));
+        }
+        rx[b] = load_raw<PT, 4>(xp + (b * kBlock + at));
+    }
+    float nm = 0.0f, nv = 0.0f;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+        const f4 g = to_float<GT, 4>(rg[b]);
+        f4 x = to_float<PT, 4>(rx[b]), r;
+        if constexpr (STATE8) {
+            m[b] = from_fp8(cm[b]) * lane_value(sm, b);
+            v[b] = from_fp8(cv[b]) * lane_value(sv, b);
+            v[b] = v[b] * v[b];
+        }
+        adamw(S, lr_decay, factor, g, x, m[b], v[b], r);
+        store_run<PT, 4>(xp + (b * kBlock + at), x);
+        if constexpr (CT != kNoCopy) store_run<CT, 4>(static_cast<typename Element<CT == kNoCopy ? QADAM_F32 : CT>::T*>(T.copy) + first + (b * kBlock + at), x);
+        if constexpr (STATE8) {
+            float im, iv;
+            const float bm = block_scale(wave_max(largest(m[b])), &im), bv = block_scale(wave_max(largest(r)), &iv);
+            if (lane == b) { nm = bm; nv = bv; }
+            f4 q = r * iv;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) q[k] = r[k] > 0.0f && iv > 0.0f ? fmaxf(q[k], kFp8Least) : q[k];
+            store_word(static_cast<uint8_t*>(T.m) + first + (b * kBlock + at), to_fp8(m[b] * im));
+            store_word(static_cast<uint8_t*>(T.v) + first + (b * kBlock + at), to_fp8(q));
+        } else {
+            store_run<QADAM_F32, 4>(static_cast<float*>(T.m) + first + (b * kBlock + at), m[b]);
+            store_run<QADAM_F32, 4>(static_cast<float*>(T.v) + first + (b * kBlock + at), v[b]);
+        }
+    }
+    if (STATE8 && lane < kBlocks) {
+        global(T.m_scales)[block + lane] = nm;
+        global(T.v_scales)[block + lane] = nv;
+    }
+}
+
 template <bool STATE8>
-__global__ void __launch_bounds__(kWave * kWavesPerTile)
+__device__ __forceinline__ void whole_blocks(const AdamwScalars& S, const ListTensor& T, const void* grad, float lr_decay, float factor,
+                                             int64_t block, int lane)
+{
+#define QADAM_CASE(P, G, CP) \
+    case list_types(P, G, CP): whole_blocks<STATE8, P, G, CP>(S, T, grad, lr_decay, factor, block, lane); break;
+#define QADAM_CASES(P, CP) QADAM_CASE(P, QADAM_F32, CP) QADAM_CASE(P, QADAM_BF16, CP) QADAM_CASE(P, QADAM_F16, CP)
+    switch (T.types) {
+        QADAM_CASES(QADAM_F32, kNoCopy)
+        QADAM_CASES(QADAM_F32, QADAM_BF16)
+        QADAM_CASES(QADAM_F32, QADAM_F16)
+        QADAM_CASES(QADAM_BF16, kNoCopy)
+        QADAM_CASES(QADAM_F16, kNoCopy)
+    }
+#undef QADAM_CASES
+#undef QADAM_CASE
+}
+
+// A workgroup is one wavefront and takes four blocks of one tensor.
+template <bool STATE8>
+__global__ void __launch_bounds__(kWave)
 k_adamw(const ListTile* __restrict__ tiles, const ListTensor* __restrict__ tensors, int first_tensor, AdamwScalars S,
         const float* __restrict__ grad_factor, GradTable G)
 {
-    const ListTile tile = tiles[blockIdx.x];
+    const ListTile tile = tiles[blockIdx.x / kWavesPerTile];
     const void* grad = G.grad[tile.tensor - first_tensor];
     if (!grad) return;
     const float factor = grad_factor ? *grad_factor : 1.0f;
     if (!(fabsf(factor) < INFINITY)) return;
     const ListTensor T = tensors[tile.tensor];
-    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int lane = threadIdx.x;
     const float lr_decay = S.lr * T.weight_decay;
-    const int64_t block = (int64_t)tile.tile * (kListTile / kBlock) + wave * kBlocks;
-    for (int b = 0; b < kBlocks; ++b)
-        if ((block + b) * kBlock < T.numel) ragged_block<STATE8>(S, T, grad, lr_decay, factor, block + b, lane);
+    const int64_t block = (int64_t)tile.tile * (kListTile / kBlock) + blockIdx.x % kWavesPerTile * kBlocks;
+    if ((block + kBlocks) * kBlock <= T.numel)
+        whole_blocks<STATE8>(S, T, grad, lr_decay, factor, block, lane);
+    else
+        for (int b = 0; b < kBlocks; ++b)
+            if ((block + b) * kBlock < T.numel) ragged_block<STATE8>(S, T, grad, lr_decay, factor, block + b, lane);
 }
 
 // Sum of the squares of the gradients: a workgroup takes every gridDim.x-th tile; the last one to arrive adds the sums of all.
@@ -151,6 +253,45 @@ __device__ __forceinline__ double group_sum(double x, double* shared)
     return x;
 }
 
+// the squares of what a thread has of a tile: runs of 8 elements, 256 runs apart
+template <int TYPE>
+__device__ __forceinline__ double tile_squares(const void* tile, int n)
+{
+    constexpr int kRun = 8, kRuns = kListTile / (kRun * kNormThreads);
+    const auto* p = static_cast<const typename Element<TYPE>::T*>(tile);
+    double sum = 0.0;
+    if (n == kListTile) {
+        typename Run<TYPE, kRun>::V v[kRuns];
+#pragma unroll
+        for (int j = 0; j < kRuns; ++j) v[j] = load_raw<TYPE, kRun>(p + ((int)threadIdx.x + j * kNormThreads) * kRun);
+#pragma unroll
+        for (int j = 0; j < kRuns; ++j)
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) {
+                const double g = (float)v[j][k];
+                sum = fma(g, g, sum);
+            }
+        return sum;
+    }
+    for (int j = 0; j < kRuns; ++j) {
+        const int at = ((int)threadIdx.x + j * kNormThreads) * kRun;
+        if (at + kRun <= n) {
+            const auto v = load_raw<TYPE, kRun>(p + at);
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) {
+                const double g = (float)v[k];
+                sum = fma(g, g, sum);
+            }
+        } else {
+            for (int k = at; k < n; ++k) {
+                const double g = load_one(p, TYPE, k);
+                sum = fma(g, g, sum);
+            }
+        }
+    }
+    return sum;
+}
+
 __global__ void __launch_bounds__(kNormThreads)
 k_grad_norm(const ListTile* __restrict__ tiles, const ListTensor* __restrict__ tensors, int num_tiles, int first_tensor, NormLaunch N,
             GradTable G)
@@ -165,10 +306,10 @@ k_grad_norm(const ListTile* __restrict__ tiles, const ListTensor* __restrict__ t
         const int64_t first = (int64_t)tile.tile * kListTile, numel = tensors[tile.tensor].numel;
         const int type = tensors[tile.tensor].types >> 2 & 3;
         const int n = numel - first < kListTile ? (int)(numel - first) : kListTile;
-        for (int k = threadIdx.x; k < n; k += kNormThreads) {
-            const double g = load_one(grad, type, first + k);
-            sum += g * g;
-        }
+        const char* p = static_cast<const char*>(grad) + first * element_size(type);
+        if (type == QADAM_F32) sum += tile_squares<QADAM_F32>(p, n);
+        else if (type == QADAM_BF16) sum += tile_squares<QADAM_BF16>(p, n);
+        else sum += tile_squares<QADAM_F16>(p, n);
     }
     sum = group_sum(sum, shared);
     if (threadIdx.x == 0)
@@ -194,7 +335,7 @@ k_grad_norm(const ListTile* __restrict__ tiles, const ListTensor* __restrict__ t
 
 hipError_t launch_adamw(const ListLaunch& L, const AdamwScalars& S, const GradTable& G, const float* grad_factor, bool state8)
 {
-    const dim3 grid(L.num_tiles), block(kWave * kWavesPerTile);
+    const dim3 grid(L.num_tiles * kWavesPerTile), block(kWave);
     if (state8)
         hipLaunchKernelGGL(k_adamw<true>, grid, block, 0, L.stream, L.tiles + L.first_tile, L.tensors, L.first_tensor, S, grad_factor, G);
     else
