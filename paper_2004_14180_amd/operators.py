@@ -10,7 +10,7 @@ from typing import Optional, Sequence
 
 from . import binding
 from .binding import (QADAM_BF16, QADAM_CODES16, QADAM_CODES8, QADAM_F16, QADAM_F32, QADAM_OK, QADAM_STATE_BLOCK, QAdamError, _AdamWConfig,
-                      _AdamWTensor, _Status, _stream)
+                      _AdamWTensor, _Status, _address, _device_and_stream, _stream)
 
 
 def _types():
@@ -68,7 +68,7 @@ class _Handle:
 
     def __init__(self):
         self._lib = binding.load_library()
-        self._h = None
+        self._h = self._plan = None
 
     def _check(self, rc: int):
         if rc != QADAM_OK:
@@ -77,7 +77,7 @@ class _Handle:
     def close(self):
         if self._h is not None:
             getattr(self._lib, self._destroy)(self._h)
-            self._h = None
+            self._h = self._plan = None
 
     def __del__(self):
         try:
@@ -89,9 +89,12 @@ class _Handle:
 class _TensorList(_Handle):
     """What AdamW and GradNorm share: a list of gradients of known types and sizes."""
 
-    def _expect(self, numels, grad_dtypes):
+    def _expect(self, numels, grad_dtypes, entry):
+        types = _types()
         self._numels, self._grad_dtypes = numels, grad_dtypes
         self._table = C.c_void_p * max(1, len(numels))
+        # as in the quantized step's binding: tensors of the common form are checked natively, any other call goes through the checks here
+        self._plan = binding._native.list_plan(self._h.value, _address(entry), list(numels), [types[t] for t in grad_dtypes])
 
     def _grads(self, grads):
         if len(grads) != len(self._numels):
@@ -167,15 +170,18 @@ class AdamW(_TensorList):
                     raise ValueError("copies[%d]: expected bfloat16 or float16" % i)
                 r.copy, r.copy_type = _list_tensor(copies[i], "copies[%d]" % i, copies[i].dtype, r.numel), types[copies[i].dtype]
             r.weight_decay = decays[i]
-        self._expect([p.numel() for p in params], dtypes)
         c = _AdamWConfig(C.sizeof(_AdamWConfig), cfg.state_bits, cfg.beta1, cfg.beta2, cfg.eps)
         h = C.c_void_p()
         self._check(self._lib.qadam_adamw_init(C.byref(h), C.byref(c), table, n))
         self._h = h
+        self._expect([p.numel() for p in params], dtypes, self._lib.qadam_adamw_step)
 
     def step(self, step: int, lr: float, grads: Sequence, grad_scale=None, stream=None):
         """One step with these gradients (None: that tensor rests).  `grad_scale`: one fp32 on the device that all gradients are
         multiplied with, such as GradNorm's out[1:]; where it is NaN or infinite nothing changes."""
+        rc = binding._native.adamw_step(self._plan, *_device_and_stream(stream), step, lr, grads, grad_scale)
+        if rc is not None:
+            return self._check(rc)
         factor = None if grad_scale is None else _list_tensor(grad_scale, "grad_scale", _F32(), 1)
         self._check(self._lib.qadam_adamw_step(self._h, step, lr, self._grads(grads), factor, _stream(stream)))
 
@@ -197,15 +203,18 @@ class GradNorm(_TensorList):
         for t in dtypes:
             if t not in types:
                 raise ValueError("grad_dtype: expected float32, bfloat16 or float16")
-        self._expect(numels, dtypes)
         n = len(numels)
         h = C.c_void_p()
         self._check(self._lib.qadam_grad_norm_init(C.byref(h), (C.c_int64 * max(1, n))(*numels),
                                                    (C.c_int32 * max(1, n))(*[types[t] for t in dtypes]), n))
         self._h = h
+        self._expect(numels, dtypes, self._lib.qadam_grad_norm)
 
     def grad_norm(self, grads: Sequence, max_norm: float, out, stream=None):
         """out[0] = norm, out[1] = max_norm / norm where the norm is beyond max_norm, else 1; NaN where the norm is not finite."""
+        rc = binding._native.grad_norm(self._plan, *_device_and_stream(stream), grads, max_norm, out)
+        if rc is not None:
+            return self._check(rc)
         self._check(self._lib.qadam_grad_norm(self._h, self._grads(grads), max_norm, _list_tensor(out, "out", _F32(), 2), _stream(stream)))
 
 
@@ -220,6 +229,8 @@ class Embedding(_Handle):
         h = C.c_void_p()
         self._check(self._lib.qadam_embedding_init(C.byref(h), self.rows, self.dim, self.max_tokens))
         self._h = h
+        self._plan = binding._native.embedding_plan(h.value, self.rows, self.dim, _address(self._lib.qadam_embedding_lookup),
+                                                    _address(self._lib.qadam_embedding_grad))
 
     def _tokens(self, tokens):
         import torch
@@ -233,6 +244,9 @@ class Embedding(_Handle):
     def lookup(self, weight, tokens, out, scale: float = 1.0, k_x: Optional[int] = None, padding_idx: Optional[int] = None, stream=None):
         """out[t] = scale * weight[tokens[t]]; zeros for the padding and for tokens out of range (status bit QADAM_STATUS_TOKEN_RANGE).
         `weight`: (rows, dim) in float32, bfloat16, float16, or weight codes in int8 or int16 with their `k_x`."""
+        rc = binding._native.embedding_lookup(self._plan, *_device_and_stream(stream), weight, tokens, out, scale, k_x, padding_idx)
+        if rc is not None:
+            return self._check(rc)
         import torch
         types = _types()
         at, size, n = self._tokens(tokens)
@@ -255,6 +269,9 @@ class Embedding(_Handle):
     def grad(self, tokens, dout, grad, scale: float = 1.0, padding_idx: Optional[int] = None, accumulate: bool = False, stream=None):
         """grad[r] = scale * sum of dout[t] over the t with tokens[t] = r, for every row; with `accumulate` added to what grad holds.
         `dout` may be an expanded row."""
+        rc = binding._native.embedding_grad(self._plan, *_device_and_stream(stream), tokens, dout, grad, scale, padding_idx, accumulate)
+        if rc is not None:
+            return self._check(rc)
         types = _types()
         at, size, n = self._tokens(tokens)
         if dout.dtype not in types or grad.dtype not in types:
