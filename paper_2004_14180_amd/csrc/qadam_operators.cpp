@@ -146,7 +146,10 @@ struct qadam_embedding_ctx {
     int device;
     int64_t rows, max_tokens;
     int32_t dim;
-    DeviceArray<uint32_t> status;
+    DeviceArray<uint32_t> status, counts, arrived;
+    DeviceArray<int32_t> sorted;        // keys and order, twice
+    DeviceArray<float> pieces;
+    EmbeddingScratch scratch;
 };
 
 extern "C" {
@@ -287,14 +290,27 @@ int qadam_embedding_init(qadam_embedding_t* out, int64_t rows, int32_t dim, int6
     if (!out) return fail(QADAM_EINVAL, "null argument");
     *out = nullptr;
     if (rows < 1 || dim < 1 || max_tokens < 0) return fail(QADAM_EINVAL, "rows < 1, dim < 1 or max_tokens < 0");
-    if (rows > (int64_t)1 << 30 || max_tokens > (int64_t)1 << 30) return fail(QADAM_ERANGE, "more than 2^30 rows or tokens");
+    if (rows > (int64_t)1 << 30) return fail(QADAM_ERANGE, "more than 2^30 rows");
+    if (max_tokens > (int64_t)1 << 24) return fail(QADAM_ERANGE, "more than 2^24 tokens");
     if (dim > 1 << 20) return fail(QADAM_ERANGE, "more than 2^20 columns");
+    if ((max_tokens + kChunk - 1) / kChunk * column_slices(dim) >= (int64_t)1 << 26)
+        return fail(QADAM_ERANGE, "too many wavefronts for one launch (max_tokens * dim / 4096 must stay below 2^26)");
     return guarded([&]() -> int {
         std::unique_ptr<qadam_embedding_ctx> h(new qadam_embedding_ctx);
         h->rows = rows; h->dim = dim; h->max_tokens = max_tokens;
         QADAM_HIP(hipGetDevice(&h->device));
         QADAM_CHECK(allocate(h->status, 1));
         QADAM_HIP(hipMemset(h->status.get(), 0, sizeof(uint32_t)));
+        const size_t n = (size_t)max_tokens, blocks = (size_t)run_blocks(max_tokens), arrivals = blocks * (size_t)column_slices(dim);
+        if (n > 0) {
+            QADAM_CHECK(allocate(h->sorted, 4 * n));
+            QADAM_CHECK(allocate(h->counts, (size_t)sort_tiles(max_tokens) << kSortBits));
+            QADAM_CHECK(allocate(h->pieces, 2 * blocks * (size_t)dim));
+            QADAM_CHECK(allocate(h->arrived, arrivals));
+            QADAM_HIP(hipMemset(h->arrived.get(), 0, arrivals * sizeof(uint32_t)));
+        }
+        int32_t* s = h->sorted.get();
+        h->scratch = {{s, s + n}, {s + 2 * n, s + 3 * n}, h->counts.get(), h->pieces.get(), h->arrived.get()};
         QADAM_HIP(hipStreamSynchronize(nullptr));
         *out = h.release();
         return QADAM_OK;
@@ -361,6 +377,7 @@ int qadam_embedding_grad(qadam_embedding_t h, const void* tokens, int32_t token_
     QADAM_CHECK(check_matrix(grad, grad_type, h->rows, grad_stride, h->dim, "grad"));
     EmbeddingGradLaunch L;
     L.t = {tokens, token_bytes, num_tokens, padding, h->rows, h->status.get()};
+    L.w = h->scratch;
     L.dout = dout; L.grad = grad; L.dout_type = dout_type; L.grad_type = grad_type; L.dim = h->dim; L.accumulate = accumulate;
     L.dout_stride = dout_stride; L.grad_stride = grad_stride;
     L.scale = scale; L.stream = static_cast<hipStream_t>(stream);

@@ -87,8 +87,23 @@ struct LookupLaunch {
 };
 hipError_t launch_embedding_lookup(const LookupLaunch& L);
 
+// Scratch of the gradient, for lists of up to max_tokens (embedding_scratch): the tokens' sorted order, and what joins long runs.
+constexpr int kSortTile = 4096;         // tokens of a workgroup of the sort in passes
+constexpr int kSortBits = 9;            // of a digit, at most
+constexpr int kRunPiece = 48;           // tokens of one row that a wavefront adds at most; longer runs are joined
+constexpr int kChunk = 16;              // tokens whose pieces a wavefront takes
+
+struct EmbeddingScratch {
+    int32_t*  keys[2];      // [max_tokens] rows in ascending order, `rows` for tokens without one
+    int32_t*  order[2];     // [max_tokens] their positions in the list
+    uint32_t* counts;       // [tiles][1 << kSortBits]
+    float*    pieces;       // [2 (max_tokens / kRunPiece + 1)][dim]
+    uint32_t* arrived;      // [max_tokens / kRunPiece + 1][slices of columns], zero between launches
+};
+
 struct EmbeddingGradLaunch {
     TokenList t;
+    EmbeddingScratch w;
     const void* dout;
     void*   grad;
     int32_t dout_type, grad_type, dim, accumulate;
@@ -97,5 +112,11 @@ struct EmbeddingGradLaunch {
     hipStream_t stream;
 };
 hipError_t launch_embedding_grad(const EmbeddingGradLaunch& L);
+
+inline int64_t sort_tiles(int64_t tokens) { return (tokens + kSortTile - 1) / kSortTile; }
+inline int64_t run_blocks(int64_t tokens) { return tokens / kRunPiece + 1; }
+// a lane's columns: 4, or as few as leave no lane of a narrow matrix idle
+inline int lane_columns(int dim) { return dim > 128 ? 4 : dim > 64 ? 2 : 1; }
+inline int column_slices(int dim) { return (dim + 64 * lane_columns(dim) - 1) / (64 * lane_columns(dim)); }
 
 }  // namespace qadam
