@@ -88,20 +88,187 @@ __device__ void fill_part(const EmbeddingGradLaunch& L, int part, int parts)
         const int64_t begin = part * each, end = begin + each < bytes ? begin + each : bytes;
         char* p = static_cast<char*>(L.grad);
         int64_t at = begin + threadIdx.x * 16;
-        for (; at + 16 <= end; at += kThreads * 16) store_run<QADAM_F32, 4>(p + at, (f4)0.0f);
+        for (; at + 16 <= end; at += (int)blockDim.x * 16) store_run<QADAM_F32, 4>(p + at, (f4)0.0f);
         if (at < end)
             for (; at < end; at += size) store_one(p + at, L.grad_type, 0, 0.0f);
         return;
     }
     for (int64_t r = part; r < L.t.rows; r += parts)
-        for (int k = threadIdx.x; k < L.dim; k += kThreads) store_one(L.grad, L.grad_type, r * L.grad_stride + k, 0.0f);
+        for (int k = threadIdx.x; k < L.dim; k += blockDim.x) store_one(L.grad, L.grad_type, r * L.grad_stride + k, 0.0f);
 }
 
-// A token's place in the sorted list is the number of tokens before it: those of smaller rows, and of its row those in front.  Row and
-// position are one number, `row << bits | position`; a workgroup counts the smaller ones for kTargets tokens.
-constexpr int kTargets = 16;
-constexpr int64_t kRankTokens = 16384;
+// Lists of up to kGroupTokens tokens are sorted in one launch: workgroup b takes the rows with row % kGroups = b, so the order is by
+// row % kGroups, then by row.  Every workgroup reads the whole list, a part per wavefront: it counts the tokens of smaller b, which
+// gives the place of its own, and keeps those in LDS as `row / kGroups << bits | position`.  Few of them are ordered by comparing all
+// pairs, many by counting their digits.  One more workgroup writes `rows` behind the last one, for the tokens without a row.
+constexpr int kGroupBits = 8, kGroups = 1 << kGroupBits;
+constexpr int kGroupThreads = 1024, kGroupWaves = kGroupThreads / 64;
+constexpr int64_t kGroupTokens = 1 << 17;
+constexpr int kKept = 752;              // tokens of a wavefront in LDS; a part with more of the workgroup's is read again.  Two
+                                        // workgroups share a CU
+constexpr int kPairs = 256;             // most tokens whose pairs are compared
 
+template <bool WIDE>
+struct TokenReader {
+    const void* tokens;
+    uint32_t rows, padding;
+
+    __device__ __forceinline__ explicit TokenReader(const TokenList& L)
+        : tokens(L.tokens), rows((uint32_t)L.rows), padding(L.padding >= 0 && L.padding < L.rows ? (uint32_t)L.padding : ~0u) {}
+
+    // the row, or ~0
+    __device__ __forceinline__ uint32_t operator()(int i, bool* outside) const
+    {
+        uint32_t low, high = 0;
+        if constexpr (WIDE) {
+            const uint64_t v = global(static_cast<const uint64_t*>(tokens))[i];
+            low = (uint32_t)v;
+            high = (uint32_t)(v >> 32);
+        } else {
+            low = global(static_cast<const uint32_t*>(tokens))[i];
+        }
+        *outside = high != 0 || low >= rows;
+        return *outside || low == padding ? ~0u : low;
+    }
+};
+
+__device__ __forceinline__ int lanes_below(uint64_t mask)
+{
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
+template <bool WIDE>
+__global__ void __launch_bounds__(kGroupThreads) k_group(EmbeddingGradLaunch L, int bits, int digit_bits)
+{
+    __shared__ uint32_t kept[kGroupWaves][kKept];
+    __shared__ uint32_t place[kGroupWaves][1 << kSortBits];
+    __shared__ uint32_t wave_count[kGroupWaves], wave_smaller[kGroupWaves], wave_ahead[kGroupWaves];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), group = blockIdx.x;
+    if (group > kGroups) {
+        fill_part(L, group - kGroups - 1, gridDim.x - kGroups - 1);
+        return;
+    }
+    const TokenReader<WIDE> read(L.t);
+    const int num = (int)L.t.num, part = ((num + kGroupWaves - 1) / kGroupWaves + 63) / 64 * 64;
+    const int begin = wave * part, end = begin + part < num ? begin + part : num;
+    int count = 0, smaller = 0;
+    bool any_outside = false;
+    constexpr int kLoads = 4;
+    for (int i0 = begin; i0 < end; i0 += 64 * kLoads) {
+        uint32_t row[kLoads];
+        bool outside[kLoads];
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+            const int i = i0 + k * 64 + lane;
+            row[k] = read(i < end ? i : end - 1, &outside[k]);
+            if (i >= end) row[k] = ~0u;
+        }
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+            any_outside |= outside[k];
+            const uint64_t own = __ballot(row[k] != ~0u && (int)(row[k] % kGroups) == group);
+            smaller += __popcll(__ballot(row[k] != ~0u && (int)(row[k] % kGroups) < group));
+            if (!own) continue;
+            const int at = count + lanes_below(own);
+            if (own >> lane & 1 && at < kKept) kept[wave][at] = row[k] / kGroups << bits | (uint32_t)(i0 + k * 64 + lane);
+            count += __popcll(own);
+        }
+    }
+    if (lane == 0) { wave_count[wave] = (uint32_t)count; wave_smaller[wave] = (uint32_t)smaller; }
+    __syncthreads();
+    int base = 0, total = 0, front = 0;
+    bool all_kept = true;
+    for (int w = 0; w < kGroupWaves; ++w) {
+        const int n = (int)wave_count[w];
+        base += (int)wave_smaller[w];
+        front += w < wave ? n : 0;
+        total += n;
+        all_kept &= n <= kKept;
+    }
+    int32_t *keys = L.w.keys[0], *order = L.w.order[0];
+    if (group == kGroups) {
+        // every token with a row is smaller
+        for (int i = base + threadIdx.x; i < num; i += kGroupThreads) global(keys)[i] = (int)L.t.rows;
+        if (any_outside) atomicOr(L.t.status, QADAM_STATUS_TOKEN_RANGE);
+        return;
+    }
+    if (total == 0) return;
+    const uint32_t position = (1u << bits) - 1;
+    if (total <= kPairs && all_kept) {
+        uint32_t* flat = place[0];
+        for (int i = lane; i < count; i += 64) flat[front + i] = kept[wave][i];
+        __syncthreads();
+        const int i = threadIdx.x;
+        if (i >= total) return;
+        const uint32_t mine = flat[i];
+        int rank = 0;
+        for (int j = 0; j < total; ++j) rank += flat[j] < mine;
+        global(keys)[base + rank] = (int)((mine >> bits) * kGroups + (uint32_t)group);
+        global(order)[base + rank] = (int)(mine & position);
+        return;
+    }
+    // the wavefront's tokens, 64 at a time: body(whether the lane has one, row / kGroups << bits | position)
+    auto each = [&](auto&& body) {
+        if (all_kept) {
+            for (int i = 0; i < count; i += 64) body(i + lane < count, kept[wave][i + lane < count ? i + lane : 0]);
+        } else {
+            for (int i = begin; i < end; i += 64) {
+                bool outside;
+                const uint32_t row = read(i + lane < end ? i + lane : end - 1, &outside);
+                body(i + lane < end && row != ~0u && (int)(row % kGroups) == group, row / kGroups << bits | (uint32_t)(i + lane));
+            }
+        }
+    };
+    const int digits = 1 << digit_bits;
+    for (int d = threadIdx.x; d < kGroupWaves << kSortBits; d += kGroupThreads) place[0][d] = 0;
+    __syncthreads();
+    each([&](bool valid, uint32_t c) {
+        if (valid) atomicAdd(&place[wave][c >> bits], 1u);
+    });
+    __syncthreads();
+    // thread d has digit d: its tokens in all wavefronts, then those of the digits in front
+    const int d = threadIdx.x;
+    uint32_t sum = 0;
+    if (d < digits)
+        for (int w = 0; w < kGroupWaves; ++w) sum += place[w][d];
+    uint32_t ahead = sum;
+    for (int s = 1; s < 64; s <<= 1) {
+        const uint32_t n = __shfl_up(ahead, s);
+        if (lane >= s) ahead += n;
+    }
+    if (lane == 63) wave_ahead[wave] = ahead;
+    ahead -= sum;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) ahead += wave_ahead[w];
+    if (d < digits) {
+        uint32_t at = (uint32_t)base + ahead;
+        for (int w = 0; w < kGroupWaves; ++w) {
+            const uint32_t n = place[w][d];
+            place[w][d] = at;
+            at += n;
+        }
+    }
+    __syncthreads();
+    each([&](bool valid, uint32_t c) {
+        const uint32_t digit = c >> bits;
+        uint64_t same = __ballot(valid);
+        for (int b = 0; b < digit_bits; ++b) {
+            const uint64_t set = __ballot(digit >> b & 1);
+            same &= digit >> b & 1 ? set : ~set;
+        }
+        const int rank = lanes_below(same);
+        if (valid) {
+            const uint32_t at = place[wave][digit] + rank;
+            global(keys)[at] = (int)(digit * kGroups + (uint32_t)group);
+            global(order)[at] = (int)(c & position);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (valid && rank == 0) place[wave][digit] += __popcll(same);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    });
+}
+
+// the sum over the wavefront
 __device__ __forceinline__ uint32_t wave_sum(uint32_t x)
 {
 #define QADAM_ADD(CTRL) x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, false)
@@ -109,48 +276,6 @@ __device__ __forceinline__ uint32_t wave_sum(uint32_t x)
 #undef QADAM_ADD
     return (uint32_t)(__builtin_amdgcn_readlane((int)x, 15) + __builtin_amdgcn_readlane((int)x, 31) +
                       __builtin_amdgcn_readlane((int)x, 47) + __builtin_amdgcn_readlane((int)x, 63));
-}
-
-__global__ void __launch_bounds__(kThreads) k_rank(EmbeddingGradLaunch L, int bits, int rank_groups)
-{
-    if ((int)blockIdx.x >= rank_groups) {
-        fill_part(L, blockIdx.x - rank_groups, gridDim.x - rank_groups);
-        return;
-    }
-    __shared__ uint32_t target[kTargets], smaller[kTargets][kThreads / 64];
-    const int num = (int)L.t.num, first = blockIdx.x * kTargets;
-    bool outside = false;
-    if (threadIdx.x < kTargets) {
-        const int t = first + threadIdx.x;
-        target[threadIdx.x] = t < num ? token_key(L.t, t, &outside) << bits | t : 0;
-        if (outside) atomicOr(L.t.status, QADAM_STATUS_TOKEN_RANGE);
-    }
-    __syncthreads();
-    uint32_t mine[kTargets], count[kTargets];
-#pragma unroll
-    for (int j = 0; j < kTargets; ++j) {
-        mine[j] = __builtin_amdgcn_readfirstlane(target[j]);
-        count[j] = 0;
-    }
-#pragma unroll 4
-    for (int u = threadIdx.x; u < num; u += kThreads) {
-        const uint32_t c = token_key(L.t, u, &outside) << bits | u;
-#pragma unroll
-        for (int j = 0; j < kTargets; ++j) count[j] += c < mine[j];
-    }
-#pragma unroll
-    for (int j = 0; j < kTargets; ++j) {
-        const uint32_t sum = wave_sum(count[j]);
-        if (threadIdx.x % 64 == 0) smaller[j][threadIdx.x / 64] = sum;
-    }
-    __syncthreads();
-    const int t = first + threadIdx.x;
-    if (threadIdx.x < kTargets && t < num) {
-        uint32_t rank = 0;
-        for (int w = 0; w < kThreads / 64; ++w) rank += smaller[threadIdx.x][w];
-        global(L.w.keys[0])[rank] = (int)(target[threadIdx.x] >> bits);
-        global(L.w.order[0])[rank] = t;
-    }
 }
 
 // Longer lists: a stable sort by digits of the row, low ones first.  Per pass the tiles' digits are counted, then each tile moves its
@@ -273,41 +398,80 @@ __global__ void __launch_bounds__(kThreads) k_move_digits(EmbeddingGradLaunch L,
 static_assert(kRunPiece % kChunk == 0 && kRunPiece < 64, "a piece ends at most kRunPiece behind the chunk's first position");
 constexpr int kBatch = 8;
 
+// the last `n` of the N columns
 template <int TYPE, int N>
-__device__ __forceinline__ typename Run<QADAM_F32, N>::F load_columns(const void* p, int n)
-{
-    if (n == N) return to_float<TYPE, N>(load_raw<TYPE, N, false>(p));
-    typename Run<QADAM_F32, N>::F x = 0.0f;
-    for (int k = 0; k < N; ++k)
-        if (k < n) x[k] = load_one(p, TYPE, k);
-    return x;
-}
-
-template <int N>
-__device__ __forceinline__ typename Run<QADAM_F32, N>::F load_grad(const void* p, int type, int n)
-{
-    if (type == QADAM_F32) return load_columns<QADAM_F32, N>(p, n);
-    if (type == QADAM_BF16) return load_columns<QADAM_BF16, N>(p, n);
-    return load_columns<QADAM_F16, N>(p, n);
-}
-
-template <int N>
-__device__ __forceinline__ void store_grad(void* p, int type, int n, typename Run<QADAM_F32, N>::F x)
+__device__ __forceinline__ void store_columns(typename Element<TYPE>::T* p, int n, typename Run<QADAM_F32, N>::F x)
 {
     if (n == N) {
-        if (type == QADAM_F32) store_run<QADAM_F32, N, false>(p, x);
-        else if (type == QADAM_BF16) store_run<QADAM_BF16, N, false>(p, x);
-        else store_run<QADAM_F16, N, false>(p, x);
+        store_run<TYPE, N, false>(p, x);
         return;
     }
     for (int k = 0; k < N; ++k)
-        if (k < n) store_one(p, type, k, x[k]);
+        if (k >= N - n) global(p)[k] = (typename Element<TYPE>::T)x[k];
 }
 
-template <int DT, int N>
+// Puts down the sum of a piece of a run that other wavefronts have pieces of too, one per block of kRunPiece positions; the last
+// wavefront to arrive adds them in order.  What crosses from one wavefront to another are agent-scope atomics, which need no cache
+// written back: a piece is in memory before its arrival is counted.
+template <int GT, int N>
+__device__ __forceinline__ void join_piece(const EmbeddingGradLaunch& L, const int* keys, int row, int block, bool is_head,
+                                           typename Run<QADAM_F32, N>::F sum, int lane, int slice, int slices, int n, int col)
+{
+    typedef typename Run<QADAM_F32, N>::F F;
+    typedef typename Element<GT>::T G;
+    const int num = (int)L.t.num;
+    // the run's blocks are [head, tail]: 64 boundaries between blocks are looked at together
+    int head = block, tail = block;
+    while (!is_head) {
+        const int at = (head - lane) * kRunPiece - 1;
+        const uint64_t other = __ballot(at < 0 || global(keys)[at < 0 ? 0 : at] != row);
+        head -= other ? __builtin_ctzll(other) : 64;
+        if (other) break;
+    }
+    for (;;) {
+        const int64_t at = (int64_t)(tail + 1 + lane) * kRunPiece;
+        const uint64_t other = __ballot(at >= num || global(keys)[at < num ? at : 0] != row);
+        tail += other ? __builtin_ctzll(other) : 64;
+        if (other) break;
+    }
+    float* put = L.w.pieces + (int64_t)(2 * block + is_head) * L.dim + col;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        if (k >= N - n) __hip_atomic_store(global(put + k), sum[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    uint32_t* arrived = L.w.arrived + (int64_t)head * slices + slice;
+    int come = 0;
+    if (lane == 0) come = (int)__hip_atomic_fetch_add(global(arrived), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    come = __builtin_amdgcn_readfirstlane(come);
+    if (come != tail - head) return;
+    asm volatile("" ::: "memory");
+    if (lane == 0) __hip_atomic_store(global(arrived), 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    F y = 0.0f;
+    for (int b = head; b <= tail; b += kBatch) {
+        F x[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int at = b + j <= tail ? b + j : tail;
+            const float* get = L.w.pieces + (int64_t)(2 * at + (at == head)) * L.dim + col;
+#pragma unroll
+            for (int k = 0; k < N; ++k) x[j][k] = __hip_atomic_load(global(get + k), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            if (b + j <= tail) y += x[j];
+    }
+    G* out = static_cast<G*>(L.grad) + col + (int64_t)row * L.grad_stride;
+    y = y * L.scale;
+    if (L.accumulate) y = to_float<GT, N>(load_raw<GT, N, false>(out)) + y;
+    store_columns<GT, N>(out, n, y);
+}
+
+template <int DT, int GT, int N>
 __global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int result, int slices)
 {
     typedef typename Run<QADAM_F32, N>::F F;
+    typedef typename Element<DT>::T D;
+    typedef typename Element<GT>::T G;
     const int* keys = L.w.keys[result];
     const int lane = threadIdx.x, slice = blockIdx.x % slices, first = blockIdx.x / slices * kChunk, num = (int)L.t.num;
     const int rows = (int)L.t.rows;
@@ -321,85 +485,54 @@ __global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int resu
     if (!mine) return;
     const int begin = __builtin_ctzll(mine), last = 63 - __builtin_clzll(mine);
     const int end = last + 1 + __builtin_ctzll(cuts >> (last + 1));     // of the last piece: at most kRunPiece behind `first`
-    const int col = (slice * 64 + lane) * N;
-    const int n = L.dim - col < 0 ? 0 : L.dim - col < N ? L.dim - col : N;
-    const int dsize = element_size(DT), gsize = element_size(L.grad_type);
-    F sum = 0.0f;
-    int piece = begin;
+    // a lane at the ragged end takes the last N columns, and writes those of them that no other lane has
+    const int own = (slice * 64 + lane) * N;
+    const int n = L.dim - own < 0 ? 0 : L.dim - own < N ? L.dim - own : N, col = n == N ? own : L.dim - N;
+    const D* from = static_cast<const D*>(L.dout) + col;
+    G* to = static_cast<G*>(L.grad) + col;
+    F sum = 0.0f, earlier = 0.0f, later = 0.0f;
+    int piece = begin, later_piece = -1;
     for (int i = begin; i < end; i += kBatch) {
-        F x[kBatch], old[kBatch];
+        // all loads of a batch are under way together; behind the end they repeat the last one
+        typename Run<DT, N>::V x[kBatch];
+        typename Run<GT, N>::V old[kBatch];
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
-            if (i + j >= end) break;
-            const int64_t t = __builtin_amdgcn_readlane(order, i + j);
-            x[j] = load_columns<DT, N>(static_cast<const char*>(L.dout) + (t * L.dout_stride + col) * dsize, n);
+            const int64_t t = __builtin_amdgcn_readlane(order, i + j < end ? i + j : end - 1);
+            x[j] = load_raw<DT, N, false>(from + t * L.dout_stride);
         }
+        if (L.accumulate)
 #pragma unroll
-        for (int j = 0; j < kBatch; ++j) {
-            old[j] = 0.0f;
-            if (i + j < end && L.accumulate && runs >> (i + j + 1) & 1) {
-                const int64_t row = __builtin_amdgcn_readlane(key, i + j);
-                old[j] = load_grad<N>(static_cast<const char*>(L.grad) + (row * L.grad_stride + col) * gsize, L.grad_type, n);
+            for (int j = 0; j < kBatch; ++j) {
+                const int64_t row = __builtin_amdgcn_readlane(key, i + j < end ? i + j : end - 1);
+                old[j] = load_raw<GT, N, false>(to + row * L.grad_stride);
             }
-        }
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
             if (i + j >= end) break;
-            sum += x[j];
+            sum += to_float<DT, N>(x[j]);
             if (!(cuts >> (i + j + 1) & 1)) continue;
             // the piece ends here
             const int row = __builtin_amdgcn_readlane(key, i + j);
-            char* out = static_cast<char*>(L.grad) + ((int64_t)row * L.grad_stride + col) * gsize;
+            G* out = to + (int64_t)row * L.grad_stride;
             if (runs >> piece & 1 && runs >> (i + j + 1) & 1) {
                 F y = sum * L.scale;
-                if (L.accumulate) y = old[j] + y;
-                store_grad<N>(out, L.grad_type, n, y);
+                if (L.accumulate) y = to_float<GT, N>(old[j]) + y;
+                store_columns<GT, N>(out, n, y);
             } else {
-                // blocks of kRunPiece positions that the run crosses: [head, tail]
-                const int block = (first + piece) / kRunPiece;
-                int head = block, tail = block;
-                if (!(runs >> piece & 1))
-                    for (;;) {
-                        const int at = (head - lane) * kRunPiece - 1;
-                        const uint64_t other = __ballot(at < 0 || global(keys)[at < 0 ? 0 : at] != row);
-                        const int same = other ? __builtin_ctzll(other) : 64;
-                        head -= same;
-                        if (same < 64) break;
-                    }
-                for (;;) {
-                    const int64_t at = (int64_t)(tail + 1 + lane) * kRunPiece;
-                    const uint64_t other = __ballot(at >= num || global(keys)[at < num ? at : 0] != row);
-                    const int same = other ? __builtin_ctzll(other) : 64;
-                    tail += same;
-                    if (same < 64) break;
-                }
-                float* put = L.w.pieces + (int64_t)(2 * block + (block == head)) * L.dim + col;
-                for (int k = 0; k < N; ++k)
-                    if (k < n) __hip_atomic_store(put + k, sum[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
-                uint32_t* arrived = L.w.arrived + (int64_t)head * slices + slice;
-                int come = 0;
-                if (lane == 0) come = (int)__hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                come = __builtin_amdgcn_readfirstlane(come);
-                if (come == tail - head) {
-                    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-                    if (lane == 0) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                    F y = 0.0f;
-#pragma unroll 4
-                    for (int b = head; b <= tail; ++b) {
-                        const float* get = L.w.pieces + (int64_t)(2 * b + (b == head)) * L.dim + col;
-                        for (int k = 0; k < N; ++k)
-                            if (k < n) y[k] += __hip_atomic_load(get + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                    }
-                    y = y * L.scale;
-                    if (L.accumulate) y = load_grad<N>(out, L.grad_type, n) + y;
-                    store_grad<N>(out, L.grad_type, n, y);
-                }
+                // only the first piece can go on from a wavefront's in front, and only the last one into another's
+                if (runs >> piece & 1) { later = sum; later_piece = piece; }
+                else { earlier = sum; }
             }
             sum = 0.0f;
             piece = i + j + 1;
         }
     }
+    if (!(runs >> begin & 1))
+        join_piece<GT, N>(L, keys, __builtin_amdgcn_readlane(key, begin), (first + begin) / kRunPiece, false, earlier, lane, slice, slices, n, col);
+    if (later_piece >= 0)
+        join_piece<GT, N>(L, keys, __builtin_amdgcn_readlane(key, later_piece), (first + later_piece) / kRunPiece, true, later, lane, slice,
+                          slices, n, col);
 }
 
 }  // namespace
@@ -447,17 +580,25 @@ static int bits_of(uint64_t n)
     return b;
 }
 
-template <int DT>
+template <int DT, int GT>
 static hipError_t sum_runs(const EmbeddingGradLaunch& L, int result)
 {
     const int slices = column_slices(L.dim);
     const dim3 grid((unsigned)((L.t.num + kChunk - 1) / kChunk * slices)), block(64);
     switch (lane_columns(L.dim)) {
-    case 4: hipLaunchKernelGGL((k_sum_runs<DT, 4>), grid, block, 0, L.stream, L, result, slices); break;
-    case 2: hipLaunchKernelGGL((k_sum_runs<DT, 2>), grid, block, 0, L.stream, L, result, slices); break;
-    default: hipLaunchKernelGGL((k_sum_runs<DT, 1>), grid, block, 0, L.stream, L, result, slices); break;
+    case 4: hipLaunchKernelGGL((k_sum_runs<DT, GT, 4>), grid, block, 0, L.stream, L, result, slices); break;
+    case 2: hipLaunchKernelGGL((k_sum_runs<DT, GT, 2>), grid, block, 0, L.stream, L, result, slices); break;
+    default: hipLaunchKernelGGL((k_sum_runs<DT, GT, 1>), grid, block, 0, L.stream, L, result, slices); break;
     }
     return hipGetLastError();
+}
+
+template <int DT>
+static hipError_t sum_runs(const EmbeddingGradLaunch& L, int result)
+{
+    if (L.grad_type == QADAM_F32) return sum_runs<DT, QADAM_F32>(L, result);
+    if (L.grad_type == QADAM_BF16) return sum_runs<DT, QADAM_BF16>(L, result);
+    return sum_runs<DT, QADAM_F16>(L, result);
 }
 
 hipError_t launch_embedding_grad(const EmbeddingGradLaunch& L)
@@ -466,11 +607,14 @@ hipError_t launch_embedding_grad(const EmbeddingGradLaunch& L)
     const int64_t bytes = L.t.rows * L.dim * element_size(L.grad_type);
     const int fill = L.accumulate ? 0 : (int)(bytes / 65536 < 1 ? 1 : bytes / 65536 < 4096 ? bytes / 65536 : 4096);
     const int64_t num = L.t.num;
+    if (num == 0 && L.accumulate) return hipSuccess;
     const int row_bits = bits_of((uint64_t)L.t.rows), bits = bits_of((uint64_t)num);
     int result = 0;
-    if (num <= kRankTokens && row_bits + bits <= 32) {
-        const int groups = (int)((num + kTargets - 1) / kTargets);
-        if (groups + fill > 0) hipLaunchKernelGGL(k_rank, dim3(groups + fill), dim3(kThreads), 0, L.stream, L, bits, groups);
+    if (num <= kGroupTokens && row_bits <= kGroupBits + kSortBits) {
+        const int digit = row_bits > kGroupBits ? row_bits - kGroupBits : 0;
+        const dim3 grid(kGroups + 1 + fill), block(kGroupThreads);
+        if (L.t.bytes == 8) hipLaunchKernelGGL(k_group<true>, grid, block, 0, L.stream, L, bits, digit);
+        else hipLaunchKernelGGL(k_group<false>, grid, block, 0, L.stream, L, bits, digit);
         if (const hipError_t e = hipGetLastError()) return e;
     } else {
         const int passes = (row_bits + kSortBits - 1) / kSortBits, digit = (row_bits + passes - 1) / passes;
