@@ -79,23 +79,20 @@ __device__ __forceinline__ uint32_t token_key(const TokenList& L, int64_t t, boo
     return row < 0 ? (uint32_t)L.rows : (uint32_t)row;
 }
 
-// Part `part` of `parts` of the matrix becomes zeros.
-__device__ void fill_part(const EmbeddingGradLaunch& L, int part, int parts)
+// A row of the gradient becomes zeros, by one wavefront.
+template <int GT>
+__device__ __forceinline__ void clear_row(const EmbeddingGradLaunch& L, int64_t row, int lane)
 {
-    const int size = element_size(L.grad_type);
-    if (L.grad_stride == L.dim) {
-        const int64_t bytes = L.t.rows * L.dim * size, each = ((bytes + parts - 1) / parts + 4095) / 4096 * 4096;
-        const int64_t begin = part * each, end = begin + each < bytes ? begin + each : bytes;
-        char* p = static_cast<char*>(L.grad);
-        int64_t at = begin + threadIdx.x * 16;
-        for (; at + 16 <= end; at += (int)blockDim.x * 16) store_run<QADAM_F32, 4>(p + at, (f4)0.0f);
-        if (at < end)
-            for (; at < end; at += size) store_one(p + at, L.grad_type, 0, 0.0f);
-        return;
-    }
-    for (int64_t r = part; r < L.t.rows; r += parts)
-        for (int k = threadIdx.x; k < L.dim; k += blockDim.x) store_one(L.grad, L.grad_type, r * L.grad_stride + k, 0.0f);
+    typedef typename Element<GT>::T G;
+    constexpr int kWide = 16 / sizeof(G);
+    G* p = static_cast<G*>(L.grad) + row * L.grad_stride;
+    int at = lane * kWide;
+    for (; at + kWide <= L.dim; at += 64 * kWide) store_run<QADAM_F32, 4>(p + at, (f4)0.0f);
+    if (at < L.dim)
+        for (; at < L.dim; ++at) global(p)[at] = (G)0.0f;
 }
+
+constexpr int kClearRows = 8;           // rows of a wavefront that clears those without a token
 
 // Lists of up to kGroupTokens tokens are sorted in one launch: workgroup b takes the rows with row % kGroups = b, so the order is by
 // row % kGroups, then by row.  Every workgroup reads the whole list, a part per wavefront: it counts the tokens of smaller b, which
@@ -144,10 +141,6 @@ __global__ void __launch_bounds__(kGroupThreads) k_group(EmbeddingGradLaunch L, 
     __shared__ uint32_t place[kGroupWaves][1 << kSortBits];
     __shared__ uint32_t wave_count[kGroupWaves], wave_smaller[kGroupWaves], wave_ahead[kGroupWaves];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), group = blockIdx.x;
-    if (group > kGroups) {
-        fill_part(L, group - kGroups - 1, gridDim.x - kGroups - 1);
-        return;
-    }
     const TokenReader<WIDE> read(L.t);
     const int num = (int)L.t.num, part = ((num + kGroupWaves - 1) / kGroupWaves + 63) / 64 * 64;
     const int begin = wave * part, end = begin + part < num ? begin + part : num;
@@ -294,10 +287,6 @@ __device__ __forceinline__ uint32_t sort_key(const EmbeddingGradLaunch& L, const
 
 __global__ void __launch_bounds__(kThreads) k_count_digits(EmbeddingGradLaunch L, SortPass P)
 {
-    if ((int)blockIdx.x >= P.tiles) {
-        fill_part(L, blockIdx.x - P.tiles, gridDim.x - P.tiles);
-        return;
-    }
     __shared__ uint32_t counts[1 << kSortBits];
     const int digits = 1 << P.bits, first = blockIdx.x * kSortTile;
     const int end = first + kSortTile < L.t.num ? first + kSortTile : (int)L.t.num;
@@ -413,7 +402,7 @@ __device__ __forceinline__ void store_columns(typename Element<TYPE>::T* p, int 
 // Puts down the sum of a piece of a run that other wavefronts have pieces of too, one per block of kRunPiece positions; the last
 // wavefront to arrive adds them in order.  What crosses from one wavefront to another are agent-scope atomics, which need no cache
 // written back: a piece is in memory before its arrival is counted.
-template <int GT, int N>
+template <int GT, int N, bool ACCUMULATE>
 __device__ __forceinline__ void join_piece(const EmbeddingGradLaunch& L, const int* keys, int row, int block, bool is_head,
                                            typename Run<QADAM_F32, N>::F sum, int lane, int slice, int slices, int n, int col)
 {
@@ -462,18 +451,49 @@ __device__ __forceinline__ void join_piece(const EmbeddingGradLaunch& L, const i
     }
     G* out = static_cast<G*>(L.grad) + col + (int64_t)row * L.grad_stride;
     y = y * L.scale;
-    if (L.accumulate) y = to_float<GT, N>(load_raw<GT, N, false>(out)) + y;
+    if constexpr (ACCUMULATE) y = to_float<GT, N>(load_raw<GT, N, false>(out)) + y;
     store_columns<GT, N>(out, n, y);
 }
 
-template <int DT, int GT, int N>
-__global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int result, int slices)
+// what the sorted list is ordered by
+__device__ __forceinline__ uint32_t sorted_by(uint32_t row, bool grouped)
+{
+    return grouped ? row % kGroups << (32 - kGroupBits) | row / kGroups : row;
+}
+
+// Rows without a token become zeros: lane r looks for the wavefront's row r in the sorted list.
+template <int GT>
+__device__ __forceinline__ void clear_absent(const EmbeddingGradLaunch& L, const int* keys, bool grouped, int64_t first, int lane)
+{
+    const int64_t row = first + lane % kClearRows;
+    const uint32_t want = sorted_by((uint32_t)row, grouped);
+    int low = 0, high = (int)L.t.num;       // the first one that is not smaller
+    while (low < high) {
+        const int mid = (low + high) / 2;
+        const uint32_t k = (uint32_t)global(keys)[mid];
+        const bool less = k < (uint32_t)L.t.rows && sorted_by(k, grouped) < want;
+        low = less ? mid + 1 : low;
+        high = less ? high : mid;
+    }
+    const bool absent = low >= (int)L.t.num || global(keys)[low] != (int)row;
+    const uint64_t clear = __ballot(absent);
+    for (int r = 0; r < kClearRows; ++r)
+        if (clear >> r & 1 && first + r < L.t.rows) clear_row<GT>(L, first + r, lane);
+}
+
+template <int DT, int GT, int N, bool ACCUMULATE>
+__global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int result, int slices, int sum_groups, bool grouped)
 {
     typedef typename Run<QADAM_F32, N>::F F;
     typedef typename Element<DT>::T D;
     typedef typename Element<GT>::T G;
     const int* keys = L.w.keys[result];
-    const int lane = threadIdx.x, slice = blockIdx.x % slices, first = blockIdx.x / slices * kChunk, num = (int)L.t.num;
+    const int lane = threadIdx.x;
+    if (!ACCUMULATE && (int)blockIdx.x >= sum_groups) {
+        clear_absent<GT>(L, keys, grouped, (int64_t)((int)blockIdx.x - sum_groups) * kClearRows, lane);
+        return;
+    }
+    const int slice = blockIdx.x % slices, first = blockIdx.x / slices * kChunk, num = (int)L.t.num;
     const int rows = (int)L.t.rows;
     const int p = first + lane;
     const int key = p < num ? global(keys)[p] : rows, prev = p > 0 && p <= num ? global(keys)[p - 1] : -1;
@@ -501,7 +521,7 @@ __global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int resu
             const int64_t t = __builtin_amdgcn_readlane(order, i + j < end ? i + j : end - 1);
             x[j] = load_raw<DT, N, false>(from + t * L.dout_stride);
         }
-        if (L.accumulate)
+        if constexpr (ACCUMULATE)
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {
                 const int64_t row = __builtin_amdgcn_readlane(key, i + j < end ? i + j : end - 1);
@@ -517,7 +537,7 @@ __global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int resu
             G* out = to + (int64_t)row * L.grad_stride;
             if (runs >> piece & 1 && runs >> (i + j + 1) & 1) {
                 F y = sum * L.scale;
-                if (L.accumulate) y = to_float<GT, N>(old[j]) + y;
+                if constexpr (ACCUMULATE) y = to_float<GT, N>(old[j]) + y;
                 store_columns<GT, N>(out, n, y);
             } else {
                 // only the first piece can go on from a wavefront's in front, and only the last one into another's
@@ -529,10 +549,115 @@ __global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int resu
         }
     }
     if (!(runs >> begin & 1))
-        join_piece<GT, N>(L, keys, __builtin_amdgcn_readlane(key, begin), (first + begin) / kRunPiece, false, earlier, lane, slice, slices, n, col);
+        join_piece<GT, N, ACCUMULATE>(L, keys, __builtin_amdgcn_readlane(key, begin), (first + begin) / kRunPiece, false, earlier, lane, slice, slices, n, col);
     if (later_piece >= 0)
-        join_piece<GT, N>(L, keys, __builtin_amdgcn_readlane(key, later_piece), (first + later_piece) / kRunPiece, true, later, lane, slice,
+        join_piece<GT, N, ACCUMULATE>(L, keys, __builtin_amdgcn_readlane(key, later_piece), (first + later_piece) / kRunPiece, true, later, lane, slice,
                           slices, n, col);
+}
+
+// Short lists, in one launch without a sort: a workgroup per token and slice of columns.  It looks through the list, and where its token
+// is the first of its row adds the dout of all of them: up to kBatch by one wavefront, more of them by four with a quarter each.
+// Further workgroups clear the rows without a token.
+constexpr int kDirectTokens = 1024, kDirectWaves = 4, kDirectPart = kDirectTokens / kDirectWaves;
+
+template <bool WIDE, int GT>
+__device__ __forceinline__ void clear_absent_direct(const EmbeddingGradLaunch& L, int64_t first, int lane)
+{
+    const TokenReader<WIDE> read(L.t);
+    const int num = (int)L.t.num;
+    uint32_t here = 0;
+    for (int i = lane; i < num; i += 64) {
+        bool outside;
+        const uint32_t row = read(i, &outside), r = row - (uint32_t)first;
+        if (row != ~0u && r < kClearRows) here |= 1u << r;
+    }
+    for (int r = 0; r < kClearRows; ++r)
+        if (!__ballot(here >> r & 1) && first + r < L.t.rows) clear_row<GT>(L, first + r, lane);
+}
+
+template <bool WIDE, int DT, int GT, int N>
+__global__ void __launch_bounds__(64 * kDirectWaves) k_sum_direct(EmbeddingGradLaunch L, int slices, int sum_groups)
+{
+    typedef typename Run<QADAM_F32, N>::F F;
+    typedef typename Element<DT>::T D;
+    typedef typename Element<GT>::T G;
+    __shared__ int list[kDirectWaves][kDirectPart], found[kDirectWaves];
+    __shared__ F sums[kDirectWaves][64];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), num = (int)L.t.num;
+    if ((int)blockIdx.x >= sum_groups) {
+        clear_absent_direct<WIDE, GT>(L, ((int64_t)((int)blockIdx.x - sum_groups) * kDirectWaves + wave) * kClearRows, lane);
+        return;
+    }
+    const TokenReader<WIDE> read(L.t);
+    const int slice = blockIdx.x % slices, t = blockIdx.x / slices;
+    bool outside;
+    const uint32_t row = __builtin_amdgcn_readfirstlane(read(t, &outside));
+    if (row == ~0u) {
+        if (outside && slice == 0 && threadIdx.x == 0) atomicOr(L.t.status, QADAM_STATUS_TOKEN_RANGE);
+        return;
+    }
+    // the wavefront's part of the list
+    constexpr int kLoads = kDirectPart / 64;
+    uint32_t other[kLoads];
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+        const int i = wave * kDirectPart + k * 64 + lane;
+        other[k] = ~0u;
+        if (i < num) other[k] = read(i, &outside);
+    }
+    int count = 0;
+    bool earlier = false;
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+        const int i = wave * kDirectPart + k * 64 + lane;
+        const uint64_t same = __ballot(other[k] == row);
+        if (!same) continue;
+        earlier |= __ballot(other[k] == row && i < t) != 0;
+        if (same >> lane & 1) list[wave][count + lanes_below(same)] = i;
+        count += __popcll(same);
+    }
+    if (lane == 0) found[wave] = earlier ? -1 : count;
+    __syncthreads();
+    int total = 0, before[kDirectWaves];
+    for (int w = 0; w < kDirectWaves; ++w) {
+        const int n = found[w];
+        if (n < 0) return;
+        before[w] = total;
+        total += n;
+    }
+    const bool split = total > kBatch;
+    if (!split && wave > 0) return;
+    const int share = split ? (total + kDirectWaves - 1) / kDirectWaves : total;
+    const int begin = wave * share, end = begin + share < total ? begin + share : total;
+    const int own = (slice * 64 + lane) * N;
+    const int n = L.dim - own < 0 ? 0 : L.dim - own < N ? L.dim - own : N, col = n == N ? own : L.dim - N;
+    const D* from = static_cast<const D*>(L.dout) + col;
+    G* out = static_cast<G*>(L.grad) + col + (int64_t)row * L.grad_stride;
+    typename Run<GT, N>::V old;
+    if (L.accumulate && wave == 0) old = load_raw<GT, N, false>(out);
+    F sum = 0.0f;
+    for (int i = begin; i < end; i += kBatch) {
+        // lane j has the position of the batch's token j
+        const int m = i + lane % kBatch < end ? i + lane % kBatch : end - 1;
+        int part = 0;
+        for (int w = 1; w < kDirectWaves; ++w) part = m >= before[w] && found[w] > 0 ? w : part;
+        const int at = list[part][m - before[part]];
+        typename Run<DT, N>::V x[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) x[j] = load_raw<DT, N, false>(from + (int64_t)__builtin_amdgcn_readlane(at, j) * L.dout_stride);
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            if (i + j < end) sum += to_float<DT, N>(x[j]);
+    }
+    if (split) {
+        sums[wave][lane] = sum;
+        __syncthreads();
+        if (wave > 0) return;
+        for (int w = 1; w < kDirectWaves; ++w) sum += sums[w][lane];
+    }
+    F y = sum * L.scale;
+    if (L.accumulate) y = to_float<GT, N>(old) + y;
+    store_columns<GT, N>(out, n, y);
 }
 
 }  // namespace
@@ -580,39 +705,26 @@ static int bits_of(uint64_t n)
     return b;
 }
 
-template <int DT, int GT>
-static hipError_t sum_runs(const EmbeddingGradLaunch& L, int result)
+template <int DT, int GT, int N>
+static hipError_t grad_of(const EmbeddingGradLaunch& L)
 {
-    const int slices = column_slices(L.dim);
-    const dim3 grid((unsigned)((L.t.num + kChunk - 1) / kChunk * slices)), block(64);
-    switch (lane_columns(L.dim)) {
-    case 4: hipLaunchKernelGGL((k_sum_runs<DT, GT, 4>), grid, block, 0, L.stream, L, result, slices); break;
-    case 2: hipLaunchKernelGGL((k_sum_runs<DT, GT, 2>), grid, block, 0, L.stream, L, result, slices); break;
-    default: hipLaunchKernelGGL((k_sum_runs<DT, GT, 1>), grid, block, 0, L.stream, L, result, slices); break;
-    }
-    return hipGetLastError();
-}
-
-template <int DT>
-static hipError_t sum_runs(const EmbeddingGradLaunch& L, int result)
-{
-    if (L.grad_type == QADAM_F32) return sum_runs<DT, QADAM_F32>(L, result);
-    if (L.grad_type == QADAM_BF16) return sum_runs<DT, QADAM_BF16>(L, result);
-    return sum_runs<DT, QADAM_F16>(L, result);
-}
-
-hipError_t launch_embedding_grad(const EmbeddingGradLaunch& L)
-{
-    // workgroups that fill the matrix with zeros, beside those that begin the sort
-    const int64_t bytes = L.t.rows * L.dim * element_size(L.grad_type);
-    const int fill = L.accumulate ? 0 : (int)(bytes / 65536 < 1 ? 1 : bytes / 65536 < 4096 ? bytes / 65536 : 4096);
     const int64_t num = L.t.num;
-    if (num == 0 && L.accumulate) return hipSuccess;
+    const int slices = column_slices(L.dim);
+    const int64_t clear = L.accumulate ? 0 : (L.t.rows + kClearRows - 1) / kClearRows;      // wavefronts
+    if (num <= kDirectTokens) {
+        const int sums = (int)num * slices;
+        const dim3 grid((unsigned)(sums + (clear + kDirectWaves - 1) / kDirectWaves)), block(64 * kDirectWaves);
+        if (grid.x == 0) return hipSuccess;
+        if (L.t.bytes == 8) hipLaunchKernelGGL((k_sum_direct<true, DT, GT, N>), grid, block, 0, L.stream, L, slices, sums);
+        else hipLaunchKernelGGL((k_sum_direct<false, DT, GT, N>), grid, block, 0, L.stream, L, slices, sums);
+        return hipGetLastError();
+    }
     const int row_bits = bits_of((uint64_t)L.t.rows), bits = bits_of((uint64_t)num);
     int result = 0;
-    if (num <= kGroupTokens && row_bits <= kGroupBits + kSortBits) {
+    const bool grouped = num <= kGroupTokens && row_bits <= kGroupBits + kSortBits;
+    if (grouped) {
         const int digit = row_bits > kGroupBits ? row_bits - kGroupBits : 0;
-        const dim3 grid(kGroups + 1 + fill), block(kGroupThreads);
+        const dim3 grid(kGroups + 1), block(kGroupThreads);
         if (L.t.bytes == 8) hipLaunchKernelGGL(k_group<true>, grid, block, 0, L.stream, L, bits, digit);
         else hipLaunchKernelGGL(k_group<false>, grid, block, 0, L.stream, L, bits, digit);
         if (const hipError_t e = hipGetLastError()) return e;
@@ -622,17 +734,43 @@ hipError_t launch_embedding_grad(const EmbeddingGradLaunch& L)
         for (int k = 0; k < passes; ++k) {
             const SortPass P{k ? L.w.keys[(k - 1) & 1] : nullptr, k ? L.w.order[(k - 1) & 1] : nullptr, L.w.keys[k & 1], L.w.order[k & 1],
                              k * digit, digit, tiles};
-            hipLaunchKernelGGL(k_count_digits, dim3(tiles + (k == 0 ? fill : 0)), dim3(kThreads), 0, L.stream, L, P);
+            hipLaunchKernelGGL(k_count_digits, dim3(tiles), dim3(kThreads), 0, L.stream, L, P);
             if (const hipError_t e = hipGetLastError()) return e;
             hipLaunchKernelGGL(k_move_digits, dim3(tiles), dim3(kThreads), 0, L.stream, L, P);
             if (const hipError_t e = hipGetLastError()) return e;
             result = k & 1;
         }
     }
-    if (num == 0) return hipSuccess;
-    if (L.dout_type == QADAM_F32) return sum_runs<QADAM_F32>(L, result);
-    if (L.dout_type == QADAM_BF16) return sum_runs<QADAM_BF16>(L, result);
-    return sum_runs<QADAM_F16>(L, result);
+    const int sums = (int)((num + kChunk - 1) / kChunk) * slices;
+    const dim3 grid((unsigned)(sums + clear)), block(64);
+    if (L.accumulate) hipLaunchKernelGGL((k_sum_runs<DT, GT, N, true>), grid, block, 0, L.stream, L, result, slices, sums, grouped);
+    else hipLaunchKernelGGL((k_sum_runs<DT, GT, N, false>), grid, block, 0, L.stream, L, result, slices, sums, grouped);
+    return hipGetLastError();
+}
+
+template <int DT, int GT>
+static hipError_t grad_of(const EmbeddingGradLaunch& L)
+{
+    switch (lane_columns(L.dim)) {
+    case 4: return grad_of<DT, GT, 4>(L);
+    case 2: return grad_of<DT, GT, 2>(L);
+    default: return grad_of<DT, GT, 1>(L);
+    }
+}
+
+template <int DT>
+static hipError_t grad_of(const EmbeddingGradLaunch& L)
+{
+    if (L.grad_type == QADAM_F32) return grad_of<DT, QADAM_F32>(L);
+    if (L.grad_type == QADAM_BF16) return grad_of<DT, QADAM_BF16>(L);
+    return grad_of<DT, QADAM_F16>(L);
+}
+
+hipError_t launch_embedding_grad(const EmbeddingGradLaunch& L)
+{
+    if (L.dout_type == QADAM_F32) return grad_of<QADAM_F32>(L);
+    if (L.dout_type == QADAM_BF16) return grad_of<QADAM_BF16>(L);
+    return grad_of<QADAM_F16>(L);
 }
 
 }  // namespace qadam

@@ -52,7 +52,7 @@ def test_norm_and_embedding_refuse_on_the_host(lib):
         assert lib.qadam_grad_norm_init(C.byref(h), n64(numel), n32(t), n) == want, numel
     assert lib.qadam_grad_norm_init(C.byref(h), None, None, 1) == -1
     assert lib.qadam_grad_norm(None, None, 1.0, None, None) == -1 and lib.qadam_grad_norm_destroy(None) == 0
-    for rows, dim, tokens, want in [(0, 1, 1, -1), (1, 0, 1, -1), (1, 1, -1, -1), ((1 << 30) + 1, 1, 1, -3), (1, (1 << 20) + 1, 1, -3),
+    for rows, dim, tokens, want in [(0, 1, 1, -1), (1, 0, 1, -1), (1, 1, -1, -1), ((1 << 28) + 1, 1, 1, -3), (1, (1 << 20) + 1, 1, -3),
                                     (1, 1, (1 << 24) + 1, -3)]:
         assert lib.qadam_embedding_init(C.byref(h), rows, dim, tokens) == want, (rows, dim, tokens)
     assert lib.qadam_embedding_lookup(None, None, 0, 0, 1, None, 4, 0, -1, 1.0, None, 0, 1, None) == -1
