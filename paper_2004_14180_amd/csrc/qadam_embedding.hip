@@ -94,16 +94,22 @@ __device__ __forceinline__ void clear_row(const EmbeddingGradLaunch& L, int64_t 
 
 constexpr int kClearRows = 8;           // rows of a wavefront that clears those without a token
 
+// rows of this size that the memory takes while lists are grouped: about 4 us and 0.3 per 1024 tokens, at 5 TB/s
+static int64_t early_rows(int64_t tokens, int64_t rows, int64_t row_bytes)
+{
+    const int64_t n = (20000000 + 1500 * tokens) / row_bytes;
+    return n < rows ? n : rows;
+}
+
 // Lists of up to kGroupTokens tokens are sorted in one launch: workgroup b takes the rows with row % kGroups = b, so the order is by
 // row % kGroups, then by row.  Every workgroup reads the whole list, a part per wavefront: it counts the tokens of smaller b, which
-// gives the place of its own, and keeps those in LDS as `row / kGroups << bits | position`.  Few of them are ordered by comparing all
-// pairs, many by counting their digits.  One more workgroup writes `rows` behind the last one, for the tokens without a row.
+// gives the place of its own, and keeps those in LDS as `row / kGroups << bits | position`.  They are ordered by
+// counting row / kGroups.  One more workgroup writes `rows` behind the last one, for the tokens without a row.
 constexpr int kGroupBits = 8, kGroups = 1 << kGroupBits;
 constexpr int kGroupThreads = 1024, kGroupWaves = kGroupThreads / 64;
 constexpr int64_t kGroupTokens = 1 << 17;
 constexpr int kKept = 752;              // tokens of a wavefront in LDS; a part with more of the workgroup's is read again.  Two
                                         // workgroups share a CU
-constexpr int kPairs = 256;             // most tokens whose pairs are compared
 
 template <bool WIDE>
 struct TokenReader {
@@ -134,13 +140,19 @@ __device__ __forceinline__ int lanes_below(uint64_t mask)
     return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
-template <bool WIDE>
-__global__ void __launch_bounds__(kGroupThreads) k_group(EmbeddingGradLaunch L, int bits, int digit_bits)
+template <bool WIDE, int GT>
+__global__ void __launch_bounds__(kGroupThreads) k_group(EmbeddingGradLaunch L, int bits, int digit_bits, int64_t clear_from)
 {
     __shared__ uint32_t kept[kGroupWaves][kKept];
     __shared__ uint32_t place[kGroupWaves][1 << kSortBits];
     __shared__ uint32_t wave_count[kGroupWaves], wave_smaller[kGroupWaves], wave_ahead[kGroupWaves];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), group = blockIdx.x;
+    if (group > kGroups) {
+        // the GPU's memory has little to do meanwhile: the last rows of the gradient, whether or not they have tokens
+        const int64_t first = clear_from + ((int64_t)(group - kGroups - 1) * kGroupWaves + wave) * kClearRows;
+        for (int64_t r = first; r < first + kClearRows && r < L.t.rows; ++r) clear_row<GT>(L, r, lane);
+        return;
+    }
     const TokenReader<WIDE> read(L.t);
     const int num = (int)L.t.num, part = ((num + kGroupWaves - 1) / kGroupWaves + 63) / 64 * 64;
     const int begin = wave * part, end = begin + part < num ? begin + part : num;
@@ -169,12 +181,11 @@ __global__ void __launch_bounds__(kGroupThreads) k_group(EmbeddingGradLaunch L, 
     }
     if (lane == 0) { wave_count[wave] = (uint32_t)count; wave_smaller[wave] = (uint32_t)smaller; }
     __syncthreads();
-    int base = 0, total = 0, front = 0;
+    int base = 0, total = 0;
     bool all_kept = true;
     for (int w = 0; w < kGroupWaves; ++w) {
         const int n = (int)wave_count[w];
         base += (int)wave_smaller[w];
-        front += w < wave ? n : 0;
         total += n;
         all_kept &= n <= kKept;
     }
@@ -187,19 +198,6 @@ __global__ void __launch_bounds__(kGroupThreads) k_group(EmbeddingGradLaunch L, 
     }
     if (total == 0) return;
     const uint32_t position = (1u << bits) - 1;
-    if (total <= kPairs && all_kept) {
-        uint32_t* flat = place[0];
-        for (int i = lane; i < count; i += 64) flat[front + i] = kept[wave][i];
-        __syncthreads();
-        const int i = threadIdx.x;
-        if (i >= total) return;
-        const uint32_t mine = flat[i];
-        int rank = 0;
-        for (int j = 0; j < total; ++j) rank += flat[j] < mine;
-        global(keys)[base + rank] = (int)((mine >> bits) * kGroups + (uint32_t)group);
-        global(order)[base + rank] = (int)(mine & position);
-        return;
-    }
     // the wavefront's tokens, 64 at a time: body(whether the lane has one, row / kGroups << bits | position)
     auto each = [&](auto&& body) {
         if (all_kept) {
@@ -392,7 +390,7 @@ template <int TYPE, int N>
 __device__ __forceinline__ void store_columns(typename Element<TYPE>::T* p, int n, typename Run<QADAM_F32, N>::F x)
 {
     if (n == N) {
-        store_run<TYPE, N, false>(p, x);
+        store_run<TYPE, N>(p, x);
         return;
     }
     for (int k = 0; k < N; ++k)
@@ -403,30 +401,35 @@ __device__ __forceinline__ void store_columns(typename Element<TYPE>::T* p, int 
 // wavefront to arrive adds them in order.  What crosses from one wavefront to another are agent-scope atomics, which need no cache
 // written back: a piece is in memory before its arrival is counted.
 template <int GT, int N, bool ACCUMULATE>
-__device__ __forceinline__ void join_piece(const EmbeddingGradLaunch& L, const int* keys, int row, int block, bool is_head,
-                                           typename Run<QADAM_F32, N>::F sum, int lane, int slice, int slices, int n, int col)
+__device__ __forceinline__ void join_piece(const EmbeddingGradLaunch& L, const int32_t* keys, int row, int block, int32_t front, int32_t behind,
+                                           bool is_head, typename Run<QADAM_F32, N>::F sum, int lane, int slice, int slices, int n, int col)
 {
     typedef typename Run<QADAM_F32, N>::F F;
     typedef typename Element<GT>::T G;
     const int num = (int)L.t.num;
     // the run's blocks are [head, tail]: 64 boundaries between blocks are looked at together
     int head = block, tail = block;
-    while (!is_head) {
-        const int at = (head - lane) * kRunPiece - 1;
-        const uint64_t other = __ballot(at < 0 || global(keys)[at < 0 ? 0 : at] != row);
+    for (int32_t k = front; !is_head;) {
+        const uint64_t other = __ballot(k != row);
         head -= other ? __builtin_ctzll(other) : 64;
         if (other) break;
+        const int at = (head - lane) * kRunPiece - 1;
+        k = at < 0 ? -1 : global(keys)[at];
     }
-    for (;;) {
-        const int64_t at = (int64_t)(tail + 1 + lane) * kRunPiece;
-        const uint64_t other = __ballot(at >= num || global(keys)[at < num ? at : 0] != row);
+    for (int32_t k = behind;;) {
+        const uint64_t other = __ballot(k != row);
         tail += other ? __builtin_ctzll(other) : 64;
         if (other) break;
+        const int64_t at = (int64_t)(tail + 1 + lane) * kRunPiece;
+        k = at < num ? global(keys)[at] : -1;
     }
     float* put = L.w.pieces + (int64_t)(2 * block + is_head) * L.dim + col;
 #pragma unroll
     for (int k = 0; k < N; ++k)
         if (k >= N - n) __hip_atomic_store(global(put + k), sum[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    G* out = static_cast<G*>(L.grad) + col + (int64_t)row * L.grad_stride;
+    typename Run<GT, N>::V old;
+    if constexpr (ACCUMULATE) old = load_raw<GT, N, false>(out);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     uint32_t* arrived = L.w.arrived + (int64_t)head * slices + slice;
     int come = 0;
@@ -449,9 +452,8 @@ __device__ __forceinline__ void join_piece(const EmbeddingGradLaunch& L, const i
         for (int j = 0; j < kBatch; ++j)
             if (b + j <= tail) y += x[j];
     }
-    G* out = static_cast<G*>(L.grad) + col + (int64_t)row * L.grad_stride;
     y = y * L.scale;
-    if constexpr (ACCUMULATE) y = to_float<GT, N>(load_raw<GT, N, false>(out)) + y;
+    if constexpr (ACCUMULATE) y = to_float<GT, N>(old) + y;
     store_columns<GT, N>(out, n, y);
 }
 
@@ -463,7 +465,7 @@ __device__ __forceinline__ uint32_t sorted_by(uint32_t row, bool grouped)
 
 // Rows without a token become zeros: lane r looks for the wavefront's row r in the sorted list.
 template <int GT>
-__device__ __forceinline__ void clear_absent(const EmbeddingGradLaunch& L, const int* keys, bool grouped, int64_t first, int lane)
+__device__ __forceinline__ void clear_absent(const EmbeddingGradLaunch& L, const int* keys, bool grouped, int64_t first, int64_t end, int lane)
 {
     const int64_t row = first + lane % kClearRows;
     const uint32_t want = sorted_by((uint32_t)row, grouped);
@@ -478,11 +480,11 @@ __device__ __forceinline__ void clear_absent(const EmbeddingGradLaunch& L, const
     const bool absent = low >= (int)L.t.num || global(keys)[low] != (int)row;
     const uint64_t clear = __ballot(absent);
     for (int r = 0; r < kClearRows; ++r)
-        if (clear >> r & 1 && first + r < L.t.rows) clear_row<GT>(L, first + r, lane);
+        if (clear >> r & 1 && first + r < end) clear_row<GT>(L, first + r, lane);
 }
 
 template <int DT, int GT, int N, bool ACCUMULATE>
-__global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int result, int slices, int sum_groups, bool grouped)
+__global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int result, int slices, int sum_groups, bool grouped, int64_t clear_rows)
 {
     typedef typename Run<QADAM_F32, N>::F F;
     typedef typename Element<DT>::T D;
@@ -490,7 +492,7 @@ __global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int resu
     const int* keys = L.w.keys[result];
     const int lane = threadIdx.x;
     if (!ACCUMULATE && (int)blockIdx.x >= sum_groups) {
-        clear_absent<GT>(L, keys, grouped, (int64_t)((int)blockIdx.x - sum_groups) * kClearRows, lane);
+        clear_absent<GT>(L, keys, grouped, (int64_t)((int)blockIdx.x - sum_groups) * kClearRows, clear_rows, lane);
         return;
     }
     const int slice = blockIdx.x % slices, first = blockIdx.x / slices * kChunk, num = (int)L.t.num;
@@ -498,6 +500,10 @@ __global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int resu
     const int p = first + lane;
     const int key = p < num ? global(keys)[p] : rows, prev = p > 0 && p <= num ? global(keys)[p - 1] : -1;
     const int order = p < num ? global(L.w.order[result])[p] : 0;
+    // the rows at the boundaries of this block and those in front, and behind it: for join_piece
+    const int block = first / kRunPiece, at_front = (block - lane) * kRunPiece - 1;
+    const int64_t at_behind = (int64_t)(block + 1 + lane) * kRunPiece;
+    const int32_t front = at_front < 0 ? -1 : global(keys)[at_front], behind = at_behind < num ? global(keys)[at_behind] : -1;
     const uint64_t valid = __ballot(key < rows);
     const uint64_t runs = __ballot(key != prev) | ~valid;               // a run begins, or nothing more comes
     const uint64_t cuts = runs | __ballot(p % kRunPiece == 0);
@@ -549,10 +555,11 @@ __global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int resu
         }
     }
     if (!(runs >> begin & 1))
-        join_piece<GT, N, ACCUMULATE>(L, keys, __builtin_amdgcn_readlane(key, begin), (first + begin) / kRunPiece, false, earlier, lane, slice, slices, n, col);
+        join_piece<GT, N, ACCUMULATE>(L, keys, __builtin_amdgcn_readlane(key, begin), block, front, behind, false, earlier, lane, slice, slices,
+                                      n, col);
     if (later_piece >= 0)
-        join_piece<GT, N, ACCUMULATE>(L, keys, __builtin_amdgcn_readlane(key, later_piece), (first + later_piece) / kRunPiece, true, later, lane, slice,
-                          slices, n, col);
+        join_piece<GT, N, ACCUMULATE>(L, keys, __builtin_amdgcn_readlane(key, later_piece), block, front, behind, true, later, lane, slice,
+                                      slices, n, col);
 }
 
 // Short lists, in one launch without a sort: a workgroup per token and slice of columns.  It looks through the list, and where its token
@@ -710,8 +717,9 @@ static hipError_t grad_of(const EmbeddingGradLaunch& L)
 {
     const int64_t num = L.t.num;
     const int slices = column_slices(L.dim);
-    const int64_t clear = L.accumulate ? 0 : (L.t.rows + kClearRows - 1) / kClearRows;      // wavefronts
+    int64_t clear_rows = L.accumulate ? 0 : L.t.rows;       // of the gradient, the first ones: if they have no token
     if (num <= kDirectTokens) {
+        const int64_t clear = (clear_rows + kClearRows - 1) / kClearRows;       // wavefronts
         const int sums = (int)num * slices;
         const dim3 grid((unsigned)(sums + (clear + kDirectWaves - 1) / kDirectWaves)), block(64 * kDirectWaves);
         if (grid.x == 0) return hipSuccess;
@@ -724,9 +732,12 @@ static hipError_t grad_of(const EmbeddingGradLaunch& L)
     const bool grouped = num <= kGroupTokens && row_bits <= kGroupBits + kSortBits;
     if (grouped) {
         const int digit = row_bits > kGroupBits ? row_bits - kGroupBits : 0;
-        const dim3 grid(kGroups + 1), block(kGroupThreads);
-        if (L.t.bytes == 8) hipLaunchKernelGGL(k_group<true>, grid, block, 0, L.stream, L, bits, digit);
-        else hipLaunchKernelGGL(k_group<false>, grid, block, 0, L.stream, L, bits, digit);
+        if (!L.accumulate) clear_rows -= early_rows(num, L.t.rows, (int64_t)L.dim * element_size(GT));
+        const int64_t early = L.accumulate ? 0 : L.t.rows - clear_rows;
+        constexpr int kEach = kGroupWaves * kClearRows;
+        const dim3 grid((unsigned)(kGroups + 1 + (early + kEach - 1) / kEach)), block(kGroupThreads);
+        if (L.t.bytes == 8) hipLaunchKernelGGL((k_group<true, GT>), grid, block, 0, L.stream, L, bits, digit, clear_rows);
+        else hipLaunchKernelGGL((k_group<false, GT>), grid, block, 0, L.stream, L, bits, digit, clear_rows);
         if (const hipError_t e = hipGetLastError()) return e;
     } else {
         const int passes = (row_bits + kSortBits - 1) / kSortBits, digit = (row_bits + passes - 1) / passes;
@@ -742,9 +753,9 @@ static hipError_t grad_of(const EmbeddingGradLaunch& L)
         }
     }
     const int sums = (int)((num + kChunk - 1) / kChunk) * slices;
-    const dim3 grid((unsigned)(sums + clear)), block(64);
-    if (L.accumulate) hipLaunchKernelGGL((k_sum_runs<DT, GT, N, true>), grid, block, 0, L.stream, L, result, slices, sums, grouped);
-    else hipLaunchKernelGGL((k_sum_runs<DT, GT, N, false>), grid, block, 0, L.stream, L, result, slices, sums, grouped);
+    const dim3 grid((unsigned)(sums + (clear_rows + kClearRows - 1) / kClearRows)), block(64);
+    if (L.accumulate) hipLaunchKernelGGL((k_sum_runs<DT, GT, N, true>), grid, block, 0, L.stream, L, result, slices, sums, grouped, clear_rows);
+    else hipLaunchKernelGGL((k_sum_runs<DT, GT, N, false>), grid, block, 0, L.stream, L, result, slices, sums, grouped, clear_rows);
     return hipGetLastError();
 }
 

@@ -91,7 +91,7 @@ hipError_t launch_embedding_lookup(const LookupLaunch& L);
 constexpr int kSortTile = 4096;         // tokens of a workgroup of the sort in passes
 constexpr int kSortBits = 9;            // of a digit, at most
 constexpr int kRunPiece = 48;           // tokens of one row that a wavefront adds at most; longer runs are joined
-constexpr int kChunk = 16;              // tokens whose pieces a wavefront takes
+constexpr int kChunk = 8;               // tokens whose pieces a wavefront takes
 
 struct EmbeddingScratch {
     int32_t*  keys[2];      // [max_tokens] rows in ascending order, `rows` for tokens without one
