@@ -15,56 +15,39 @@ __device__ __forceinline__ int64_t token_row(const TokenList& L, int64_t t, bool
     return *out_of_range || tok == L.padding ? -1 : tok;
 }
 
-// Lookup: 1 << log_lanes lanes per row take runs of 8 elements, a lane of ROWS rows at a time, whose loads are under way together.
+// Lookup: 1 << log_lanes lanes per row take runs of 8 elements.
 constexpr int kRun = 8;
 
-template <int WT, int OT, int ROWS>
-__device__ __forceinline__ void lookup_rows(const LookupLaunch& L, int log_lanes)
+template <int WT, int OT>
+__device__ __forceinline__ void lookup_row(const LookupLaunch& L, int64_t t, int64_t row, int lane, int lanes)
 {
     typedef typename Element<WT>::T W;
     typedef typename Element<OT>::T O;
-    const int lanes = 1 << log_lanes, lane = threadIdx.x & (lanes - 1), groups = kThreads >> log_lanes;
-    const int64_t t0 = (int64_t)blockIdx.x * (groups * ROWS) + (threadIdx.x >> log_lanes);
-    int64_t row[ROWS];
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        const int64_t t = t0 + r * groups;
-        bool outside = false;
-        row[r] = t < L.t.num ? token_row(L.t, t, &outside) : -1;
-        if (outside && lane == 0) atomicOr(L.t.status, QADAM_STATUS_TOKEN_RANGE);
-    }
+    const W* from = static_cast<const W*>(L.weight) + row * L.weight_stride;
+    O* to = static_cast<O*>(L.out) + t * L.out_stride;
     for (int at = lane * kRun; at < L.dim; at += lanes * kRun) {
-        const bool whole = at + kRun <= L.dim;
-        typename Run<WT, kRun>::V v[ROWS];
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            const W* p = static_cast<const W*>(L.weight) + row[r] * L.weight_stride + at;
-            if (row[r] < 0) v[r] = (W)0;
-            else if (whole) v[r] = load_raw<WT, kRun, false>(p);
-            else
-                for (int k = 0; k < kRun; ++k) v[r][k] = at + k < L.dim ? global(p)[k] : (W)0;
-        }
-#pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            const int64_t t = t0 + r * groups;
-            if (t >= L.t.num) continue;
-            // zero, whatever the scale
-            const auto x = row[r] < 0 ? (typename Run<WT, kRun>::F)0.0f : to_float<WT, kRun>(v[r]) * L.scale;
-            O* p = static_cast<O*>(L.out) + t * L.out_stride + at;
-            if (whole) store_run<OT, kRun, false>(p, x);
-            else
-                for (int k = 0; k < kRun; ++k)
-                    if (at + k < L.dim) global(p)[k] = (O)x[k];
+        if (at + kRun <= L.dim) {
+            typename Run<WT, kRun>::F x = 0.0f;         // zero, whatever the scale
+            if (row >= 0) x = to_float<WT, kRun>(load_raw<WT, kRun, false>(from + at)) * L.scale;
+            store_run<OT, kRun>(to + at, x);
+        } else {
+            for (int k = at; k < L.dim; ++k) global(to)[k] = (O)(row < 0 ? 0.0f : (float)global(from)[k] * L.scale);
         }
     }
 }
 
-template <int WT, int ROWS>
+template <int WT>
 __global__ void __launch_bounds__(kThreads) k_lookup(LookupLaunch L, int log_lanes)
 {
-    if (L.out_type == QADAM_F32) lookup_rows<WT, QADAM_F32, ROWS>(L, log_lanes);
-    else if (L.out_type == QADAM_BF16) lookup_rows<WT, QADAM_BF16, ROWS>(L, log_lanes);
-    else lookup_rows<WT, QADAM_F16, ROWS>(L, log_lanes);
+    const int lanes = 1 << log_lanes, lane = threadIdx.x & (lanes - 1);
+    const int64_t t = (int64_t)blockIdx.x * (kThreads >> log_lanes) + (threadIdx.x >> log_lanes);
+    if (t >= L.t.num) return;
+    bool outside;
+    const int64_t row = token_row(L.t, t, &outside);
+    if (outside && lane == 0) atomicOr(L.t.status, QADAM_STATUS_TOKEN_RANGE);
+    if (L.out_type == QADAM_F32) lookup_row<WT, QADAM_F32>(L, t, row, lane, lanes);
+    else if (L.out_type == QADAM_BF16) lookup_row<WT, QADAM_BF16>(L, t, row, lane, lanes);
+    else lookup_row<WT, QADAM_F16>(L, t, row, lane, lanes);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -92,12 +75,13 @@ __device__ __forceinline__ void clear_row(const EmbeddingGradLaunch& L, int64_t 
         for (; at < L.dim; ++at) global(p)[at] = (G)0.0f;
 }
 
-constexpr int kClearRows = 8;           // rows of a wavefront that clears those without a token
+constexpr int kClearRows = 2;           // rows of a wavefront that clears those without a token
 
-// rows of this size that the memory takes while lists are grouped: about 4 us and 0.3 per 1024 tokens, at 5 TB/s
+// Rows of this size that are cleared while lists are grouped, which leaves the memory idle: about 8 us and 0.6 per 1024 tokens, at 5 TB/s.
+// 16 k tokens, 412 MB: none 99.6 us per call, a quarter of this 99.0, half 96.6, this 93.5
 static int64_t early_rows(int64_t tokens, int64_t rows, int64_t row_bytes)
 {
-    const int64_t n = (20000000 + 1500 * tokens) / row_bytes;
+    const int64_t n = (40000000 + 3000 * tokens) / row_bytes;
     return n < rows ? n : rows;
 }
 
@@ -566,6 +550,7 @@ __global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int resu
 // is the first of its row adds the dout of all of them: up to kBatch by one wavefront, more of them by four with a quarter each.
 // Further workgroups clear the rows without a token.
 constexpr int kDirectTokens = 1024, kDirectWaves = 4, kDirectPart = kDirectTokens / kDirectWaves;
+constexpr int kDirectClear = 8;         // rows of a wavefront that clears, which reads the whole list for them
 
 template <bool WIDE, int GT>
 __device__ __forceinline__ void clear_absent_direct(const EmbeddingGradLaunch& L, int64_t first, int lane)
@@ -576,9 +561,9 @@ __device__ __forceinline__ void clear_absent_direct(const EmbeddingGradLaunch& L
     for (int i = lane; i < num; i += 64) {
         bool outside;
         const uint32_t row = read(i, &outside), r = row - (uint32_t)first;
-        if (row != ~0u && r < kClearRows) here |= 1u << r;
+        if (row != ~0u && r < kDirectClear) here |= 1u << r;
     }
-    for (int r = 0; r < kClearRows; ++r)
+    for (int r = 0; r < kDirectClear; ++r)
         if (!__ballot(here >> r & 1) && first + r < L.t.rows) clear_row<GT>(L, first + r, lane);
 }
 
@@ -592,7 +577,7 @@ __global__ void __launch_bounds__(64 * kDirectWaves) k_sum_direct(EmbeddingGradL
     __shared__ F sums[kDirectWaves][64];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), num = (int)L.t.num;
     if ((int)blockIdx.x >= sum_groups) {
-        clear_absent_direct<WIDE, GT>(L, ((int64_t)((int)blockIdx.x - sum_groups) * kDirectWaves + wave) * kClearRows, lane);
+        clear_absent_direct<WIDE, GT>(L, ((int64_t)((int)blockIdx.x - sum_groups) * kDirectWaves + wave) * kDirectClear, lane);
         return;
     }
     const TokenReader<WIDE> read(L.t);
@@ -674,19 +659,15 @@ static hipError_t lookup_of(const LookupLaunch& L)
 {
     int log_lanes = 0;
     while ((1 << log_lanes) < kThreads && (1 << log_lanes) * kRun < L.dim) ++log_lanes;
-    const int groups = kThreads >> log_lanes;
-    // four rows per lane where that leaves every CU work
-    constexpr int kMany = 4;
-    const int64_t many = (L.t.num + groups * kMany - 1) / (groups * kMany), one = (L.t.num + groups - 1) / groups;
-    if (many >= 1024) hipLaunchKernelGGL((k_lookup<WT, kMany>), dim3((unsigned)many), dim3(kThreads), 0, L.stream, L, log_lanes);
-    else hipLaunchKernelGGL((k_lookup<WT, 1>), dim3((unsigned)one), dim3(kThreads), 0, L.stream, L, log_lanes);
+    const int64_t each = kThreads >> log_lanes;
+    hipLaunchKernelGGL(k_lookup<WT>, dim3((unsigned)((L.t.num + each - 1) / each)), dim3(kThreads), 0, L.stream, L, log_lanes);
     return hipGetLastError();
 }
 
 hipError_t launch_embedding_lookup(const LookupLaunch& all)
 {
-    // workgroups times threads of a launch stay below 2^32: parts of at most 2^24 tokens
-    constexpr int64_t kPart = (int64_t)1 << 24;
+    // workgroups times threads of a launch stay below 2^32: parts of 2^23 tokens
+    constexpr int64_t kPart = (int64_t)1 << 23;
     for (int64_t at = 0; at < all.t.num; at += kPart) {
         LookupLaunch L = all;
         L.t.tokens = static_cast<const char*>(all.t.tokens) + at * all.t.bytes;
@@ -719,7 +700,7 @@ static hipError_t grad_of(const EmbeddingGradLaunch& L)
     const int slices = column_slices(L.dim);
     int64_t clear_rows = L.accumulate ? 0 : L.t.rows;       // of the gradient, the first ones: if they have no token
     if (num <= kDirectTokens) {
-        const int64_t clear = (clear_rows + kClearRows - 1) / kClearRows;       // wavefronts
+        const int64_t clear = (clear_rows + kDirectClear - 1) / kDirectClear;       // wavefronts
         const int sums = (int)num * slices;
         const dim3 grid((unsigned)(sums + (clear + kDirectWaves - 1) / kDirectWaves)), block(64 * kDirectWaves);
         if (grid.x == 0) return hipSuccess;

@@ -91,7 +91,8 @@ struct List {
     {
         int64_t count = 0;
         for (const ListTensor& t : host) count += (t.numel + kListTile - 1) / kListTile;
-        if (count >= ((int64_t)1 << 32) / 256) return fail(QADAM_ERANGE, "too many tiles for one launch (elements / 4096 must stay below 2^24)");
+        // a launch has a wavefront per block of 256 elements, 16 per tile
+        if (count >= ((int64_t)1 << 32) / (64 * 16)) return fail(QADAM_ERANGE, "too many tiles for one launch (elements / 4096 must stay below 2^22)");
         std::vector<ListTile> all;
         all.reserve((size_t)count);
         for (size_t i = 0; i < host.size(); ++i) {

@@ -55,7 +55,7 @@ struct ListLaunch {
 
 hipError_t launch_adamw(const ListLaunch& L, const AdamwScalars& S, const GradTable& G, const float* grad_factor, bool state8);
 
-constexpr int kNormGroups = 2048;       // workgroups of a launch of the norm, at most
+constexpr int kNormGroups = 1024;       // workgroups of a launch of the norm, at most
 inline int norm_groups(int num_tiles) { return num_tiles < 1 ? 1 : num_tiles < kNormGroups ? num_tiles : kNormGroups; }
 
 // partial sums of a launch at sums + first_sum; the last launch (`total` > 0: sums of all launches) finishes

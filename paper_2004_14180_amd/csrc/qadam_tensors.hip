@@ -7,9 +7,7 @@ namespace {
 
 constexpr int kWave = 64;
 constexpr int kBlock = QADAM_STATE_BLOCK;       // a wavefront's 64 lanes of 4 elements
-constexpr int kBlocks = 4;                      // blocks of a wavefront
-constexpr int kWaveElems = kBlock * kBlocks;
-constexpr int kWavesPerTile = kListTile / kWaveElems;
+constexpr int kBlocksPerTile = kListTile / kBlock;
 static_assert(kBlock == 4 * kWave, "");
 
 constexpr float kFp8Max = 448.0f, kFp8Least = 0x1p-9f, kTinyBlock = 0x1p-116f;
@@ -51,12 +49,6 @@ typedef uint32_t word_u __attribute__((aligned(1)));
 __device__ __forceinline__ uint32_t load_word(const uint8_t* p) { return __builtin_nontemporal_load((const QADAM_GLOBAL word_u*)p); }
 __device__ __forceinline__ void store_word(uint8_t* p, uint32_t x) { __builtin_nontemporal_store(x, (QADAM_GLOBAL word_u*)p); }
 
-// lane l's value in all lanes
-__device__ __forceinline__ float lane_value(float x, int l)
-{
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l));
-}
-
 // x, m, v of four elements after the step; `r`: sqrt(v)
 __device__ __forceinline__ void adamw(const AdamwScalars& S, float lr_decay, float factor, f4 grad, f4& x, f4& m, f4& v, f4& r)
 {
@@ -85,126 +77,115 @@ __device__ __forceinline__ float largest(f4 a)
     return fmaxf(b, c);
 }
 
-// One wavefront's block `block` of the tensor: elements that the lane does not have count as zeros.
-template <bool STATE8>
-__device__ void ragged_block(const AdamwScalars& S, const ListTensor& T, const void* grad, float lr_decay, float factor, int64_t block,
-                             int lane)
+// four elements at p + at; of a ragged tensor those from `end` on repeat the last one
+template <int TYPE, bool WHOLE>
+__device__ __forceinline__ typename Run<TYPE, 4>::V load_four(const void* p, int at, int end)
 {
-    const int64_t first = block * kBlock + lane * 4;
-    const int pt = T.types & 3, gt = T.types >> 2 & 3, ct = T.types >> 4;
-    const int n = T.numel - first < 0 ? 0 : T.numel - first < 4 ? (int)(T.numel - first) : 4;
-    f4 g = 0.0f, x = 0.0f, m = 0.0f, v = 0.0f, r;
-    float sm = 0.0f, sv = 0.0f;
-    if (STATE8) { sm = global(T.m_scales)[block]; sv = global(T.v_scales)[block]; }
-    for (int k = 0; k < n; ++k) {
-        g[k] = load_one(grad, gt, first + k);
-        x[k] = load_one(T.param, pt, first + k);
-        if (STATE8) {
-            m[k] = __builtin_amdgcn_cvt_f32_fp8(global(static_cast<const uint8_t*>(T.m))[first + k], 0) * sm;
-            v[k] = __builtin_amdgcn_cvt_f32_fp8(global(static_cast<const uint8_t*>(T.v))[first + k], 0) * sv;
-        } else {
-            m[k] = global(static_cast<const float*>(T.m))[first + k];
-            v[k] = global(static_cast<const float*>(T.v))[first + k];
-        }
+    const auto* q = static_cast<const typename Element<TYPE>::T*>(p);
+    if constexpr (WHOLE) return load_raw<TYPE, 4>(q + at);
+    typename Run<TYPE, 4>::V v;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = global(q)[at + k < end ? at + k : end - 1];
+    return v;
+}
+
+template <int TYPE, bool WHOLE>
+__device__ __forceinline__ void store_four(void* p, int at, int end, f4 x)
+{
+    auto* q = static_cast<typename Element<TYPE>::T*>(p);
+    if constexpr (WHOLE) {
+        store_run<TYPE, 4>(q + at, x);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (at + k < end) global(q)[at + k] = (typename Element<TYPE>::T)x[k];
     }
-    if (STATE8) v = v * v;
-    adamw(S, lr_decay, factor, g, x, m, v, r);
-    uint32_t cm = 0, cv = 0;
-    if (STATE8) {
-        for (int k = n; k < 4; ++k) m[k] = r[k] = 0.0f;     // a factor that is zero times infinity
+}
+
+// the same of bytes
+template <bool WHOLE>
+__device__ __forceinline__ uint32_t load_bytes(const void* p, int at, int end)
+{
+    const uint8_t* q = static_cast<const uint8_t*>(p);
+    if constexpr (WHOLE) return load_word(q + at);
+    uint32_t w = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w |= (uint32_t)global(q)[at + k < end ? at + k : end - 1] << 8 * k;
+    return w;
+}
+
+template <bool WHOLE>
+__device__ __forceinline__ void store_bytes(void* p, int at, int end, uint32_t w)
+{
+    uint8_t* q = static_cast<uint8_t*>(p);
+    if constexpr (WHOLE) {
+        store_word(q + at, w);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (at + k < end) global(q)[at + k] = (uint8_t)(w >> 8 * k);
+    }
+}
+
+// A block of a tensor, types known.  WHOLE: the tensor has all of it.
+template <bool STATE8, int PT, int GT, int CT, bool WHOLE>
+__device__ __forceinline__ void step_block(const AdamwScalars& S, const ListTensor& T, const void* grad, float lr_decay, float factor,
+                                           int64_t block, int lane)
+{
+    const int64_t first = block * kBlock, left = T.numel - first;
+    const int at = lane * 4, end = left < kBlock ? (int)left : kBlock;
+    const void* gp = static_cast<const typename Element<GT>::T*>(grad) + first;
+    void* xp = static_cast<typename Element<PT>::T*>(T.param) + first;
+    const auto grad4 = load_four<GT, WHOLE>(gp, at, end);
+    const auto param4 = load_four<PT, WHOLE>(xp, at, end);
+    f4 m, v, r;
+    void *mp, *vp;
+    if constexpr (STATE8) {
+        mp = static_cast<uint8_t*>(T.m) + first;
+        vp = static_cast<uint8_t*>(T.v) + first;
+        const uint32_t cm = load_bytes<WHOLE>(mp, at, end), cv = load_bytes<WHOLE>(vp, at, end);
+        const float sm = global(T.m_scales)[block], sv = global(T.v_scales)[block];
+        m = from_fp8(cm) * sm;
+        v = from_fp8(cv) * sv;
+        v = v * v;
+    } else {
+        mp = static_cast<float*>(T.m) + first;
+        vp = static_cast<float*>(T.v) + first;
+        m = load_four<QADAM_F32, WHOLE>(mp, at, end);
+        v = load_four<QADAM_F32, WHOLE>(vp, at, end);
+    }
+    f4 x = to_float<PT, 4>(param4);
+    adamw(S, lr_decay, factor, to_float<GT, 4>(grad4), x, m, v, r);
+    store_four<PT, WHOLE>(xp, at, end, x);
+    if constexpr (CT != kNoCopy) store_four<CT, WHOLE>(static_cast<typename Element<CT>::T*>(T.copy) + first, at, end, x);
+    if constexpr (STATE8) {
+        if constexpr (!WHOLE)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (at + k >= end) m[k] = r[k] = 0.0f;
         float im, iv;
         const float nm = block_scale(wave_max(largest(m)), &im), nv = block_scale(wave_max(largest(r)), &iv);
-        f4 qm = m * im, qv = r * iv;
-        for (int k = 0; k < 4; ++k)
-            if (r[k] > 0.0f && iv > 0.0f) qv[k] = fmaxf(qv[k], kFp8Least);
-        cm = to_fp8(qm);
-        cv = to_fp8(qv);
-        if (lane == 0) { global(T.m_scales)[block] = nm; global(T.v_scales)[block] = nv; }
-    }
-    for (int k = 0; k < n; ++k) {
-        store_one(T.param, pt, first + k, x[k]);
-        if (ct != kNoCopy) store_one(T.copy, ct, first + k, x[k]);
-        if (STATE8) {
-            global(static_cast<uint8_t*>(T.m))[first + k] = (uint8_t)(cm >> 8 * k);
-            global(static_cast<uint8_t*>(T.v))[first + k] = (uint8_t)(cv >> 8 * k);
-        } else {
-            global(static_cast<float*>(T.m))[first + k] = m[k];
-            global(static_cast<float*>(T.v))[first + k] = v[k];
+        f4 q = r * iv;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) q[k] = r[k] > 0.0f && iv > 0.0f ? fmaxf(q[k], kFp8Least) : q[k];
+        store_bytes<WHOLE>(mp, at, end, to_fp8(m * im));
+        store_bytes<WHOLE>(vp, at, end, to_fp8(q));
+        if (lane == 0) {
+            global(T.m_scales)[block] = nm;
+            global(T.v_scales)[block] = nv;
         }
+    } else {
+        store_four<QADAM_F32, WHOLE>(mp, at, end, m);
+        store_four<QADAM_F32, WHOLE>(vp, at, end, v);
     }
 }
 
-// Four whole blocks of a tensor, types known: all loads are under way before the first value is used.
-template <bool STATE8, int PT, int GT, int CT>
-__device__ __forceinline__ void whole_blocks(const AdamwScalars& S, const ListTensor& T, const void* grad, float lr_decay, float factor,
-                                             int64_t block, int lane)
-{
-    typedef typename Element<PT>::T P;
-    typedef typename Element<GT>::T G;
-    const int64_t first = block * kBlock;
-    const int at = lane * 4;
-    const G* gp = static_cast<const G*>(grad) + first;
-    P* xp = static_cast<P*>(T.param) + first;
-    typename Run<GT, 4>::V rg[kBlocks];
-    typename Run<PT, 4>::V rx[kBlocks];
-    f4 m[kBlocks], v[kBlocks];
-    uint32_t cm[kBlocks], cv[kBlocks];
-    float sm = 0.0f, sv = 0.0f;
-    if constexpr (STATE8) {
-        sm = global(T.m_scales)[block + lane % kBlocks];
-        sv = global(T.v_scales)[block + lane % kBlocks];
-    }
-#pragma unroll
-    for (int b = 0; b < kBlocks; ++b) {
-        rg[b] = load_raw<GT, 4>(gp + (b * kBlock + at));
-        if constexpr (STATE8) {
-            cm[b] = load_word(static_cast<const uint8_t*>(T.m) + first + (b * kBlock + at));
-            cv[b] = load_word(static_cast<const uint8_t*>(T.v) + first + (b * kBlock + at));
-        } else {
-            m[b] = load_raw<QADAM_F32, 4>(static_cast<const float*>(T.m) + first + (b * kBlock + at));
-            v[b] = load_raw<QADAM_F32, 4>(static_cast<const float*>(T.v) + first + (b * kBlock + at));
-        }
-        rx[b] = load_raw<PT, 4>(xp + (b * kBlock + at));
-    }
-    float nm = 0.0f, nv = 0.0f;
-#pragma unroll
-    for (int b = 0; b < kBlocks; ++b) {
-        const f4 g = to_float<GT, 4>(rg[b]);
-        f4 x = to_float<PT, 4>(rx[b]), r;
-        if constexpr (STATE8) {
-            m[b] = from_fp8(cm[b]) * lane_value(sm, b);
-            v[b] = from_fp8(cv[b]) * lane_value(sv, b);
-            v[b] = v[b] * v[b];
-        }
-        adamw(S, lr_decay, factor, g, x, m[b], v[b], r);
-        store_run<PT, 4>(xp + (b * kBlock + at), x);
-        if constexpr (CT != kNoCopy) store_run<CT, 4>(static_cast<typename Element<CT == kNoCopy ? QADAM_F32 : CT>::T*>(T.copy) + first + (b * kBlock + at), x);
-        if constexpr (STATE8) {
-            float im, iv;
-            const float bm = block_scale(wave_max(largest(m[b])), &im), bv = block_scale(wave_max(largest(r)), &iv);
-            if (lane == b) { nm = bm; nv = bv; }
-            f4 q = r * iv;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) q[k] = r[k] > 0.0f && iv > 0.0f ? fmaxf(q[k], kFp8Least) : q[k];
-            store_word(static_cast<uint8_t*>(T.m) + first + (b * kBlock + at), to_fp8(m[b] * im));
-            store_word(static_cast<uint8_t*>(T.v) + first + (b * kBlock + at), to_fp8(q));
-        } else {
-            store_run<QADAM_F32, 4>(static_cast<float*>(T.m) + first + (b * kBlock + at), m[b]);
-            store_run<QADAM_F32, 4>(static_cast<float*>(T.v) + first + (b * kBlock + at), v[b]);
-        }
-    }
-    if (STATE8 && lane < kBlocks) {
-        global(T.m_scales)[block + lane] = nm;
-        global(T.v_scales)[block + lane] = nv;
-    }
-}
-
-template <bool STATE8>
-__device__ __forceinline__ void whole_blocks(const AdamwScalars& S, const ListTensor& T, const void* grad, float lr_decay, float factor,
-                                             int64_t block, int lane)
+template <bool STATE8, bool WHOLE>
+__device__ __forceinline__ void step_block(const AdamwScalars& S, const ListTensor& T, const void* grad, float lr_decay, float factor,
+                                           int64_t block, int lane)
 {
 #define QADAM_CASE(P, G, CP) \
-    case list_types(P, G, CP): whole_blocks<STATE8, P, G, CP>(S, T, grad, lr_decay, factor, block, lane); break;
+    case list_types(P, G, CP): step_block<STATE8, P, G, CP, WHOLE>(S, T, grad, lr_decay, factor, block, lane); break;
 #define QADAM_CASES(P, CP) QADAM_CASE(P, QADAM_F32, CP) QADAM_CASE(P, QADAM_BF16, CP) QADAM_CASE(P, QADAM_F16, CP)
     switch (T.types) {
         QADAM_CASES(QADAM_F32, kNoCopy)
@@ -217,13 +198,12 @@ __device__ __forceinline__ void whole_blocks(const AdamwScalars& S, const ListTe
 #undef QADAM_CASE
 }
 
-// A workgroup is one wavefront and takes four blocks of one tensor.
 template <bool STATE8>
 __global__ void __launch_bounds__(kWave)
 k_adamw(const ListTile* __restrict__ tiles, const ListTensor* __restrict__ tensors, int first_tensor, AdamwScalars S,
         const float* __restrict__ grad_factor, GradTable G)
 {
-    const ListTile tile = tiles[blockIdx.x / kWavesPerTile];
+    const ListTile tile = tiles[blockIdx.x / kBlocksPerTile];
     const void* grad = G.grad[tile.tensor - first_tensor];
     if (!grad) return;
     const float factor = grad_factor ? *grad_factor : 1.0f;
@@ -231,12 +211,9 @@ k_adamw(const ListTile* __restrict__ tiles, const ListTensor* __restrict__ tenso
     const ListTensor T = tensors[tile.tensor];
     const int lane = threadIdx.x;
     const float lr_decay = S.lr * T.weight_decay;
-    const int64_t block = (int64_t)tile.tile * (kListTile / kBlock) + blockIdx.x % kWavesPerTile * kBlocks;
-    if ((block + kBlocks) * kBlock <= T.numel)
-        whole_blocks<STATE8>(S, T, grad, lr_decay, factor, block, lane);
-    else
-        for (int b = 0; b < kBlocks; ++b)
-            if ((block + b) * kBlock < T.numel) ragged_block<STATE8>(S, T, grad, lr_decay, factor, block + b, lane);
+    const int64_t block = (int64_t)tile.tile * kBlocksPerTile + blockIdx.x % kBlocksPerTile;
+    if ((block + 1) * kBlock <= T.numel) step_block<STATE8, true>(S, T, grad, lr_decay, factor, block, lane);
+    else if (block * kBlock < T.numel) step_block<STATE8, false>(S, T, grad, lr_decay, factor, block, lane);
 }
 
 // Sum of the squares of the gradients: a workgroup takes every gridDim.x-th tile; the last one to arrive adds the sums of all.
@@ -335,7 +312,7 @@ k_grad_norm(const ListTile* __restrict__ tiles, const ListTensor* __restrict__ t
 
 hipError_t launch_adamw(const ListLaunch& L, const AdamwScalars& S, const GradTable& G, const float* grad_factor, bool state8)
 {
-    const dim3 grid(L.num_tiles * kWavesPerTile), block(kWave);
+    const dim3 grid(L.num_tiles * kBlocksPerTile), block(kWave);
     if (state8)
         hipLaunchKernelGGL(k_adamw<true>, grid, block, 0, L.stream, L.tiles + L.first_tile, L.tensors, L.first_tensor, S, grad_factor, G);
     else
