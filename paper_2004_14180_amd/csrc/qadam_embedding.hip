@@ -546,10 +546,11 @@ __global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int resu
                                       slices, n, col);
 }
 
-// Short lists, in one launch without a sort: a workgroup per token and slice of columns.  It looks through the list, and where its token
-// is the first of its row adds the dout of all of them: up to kBatch by one wavefront, more of them by four with a quarter each.
-// Further workgroups clear the rows without a token.
-constexpr int kDirectTokens = 1024, kDirectWaves = 4, kDirectPart = kDirectTokens / kDirectWaves;
+// Short lists, in one launch without a sort: a workgroup per token and up to four slices of columns.  It looks through the list, and
+// where its token is the first of its row adds the dout of all of them, a wavefront per slice; of more than kBatch tokens the
+// wavefronts that a slice has take a part each.  Further workgroups clear the rows without a token.
+constexpr int kDirectTokens = 2048, kDirectWaves = 8, kDirectPart = kDirectTokens / kDirectWaves;
+constexpr int kDirectGroups = 2048;     // most workgroups that look through the list
 constexpr int kDirectClear = 8;         // rows of a wavefront that clears, which reads the whole list for them
 
 template <bool WIDE, int GT>
@@ -568,7 +569,8 @@ __device__ __forceinline__ void clear_absent_direct(const EmbeddingGradLaunch& L
 }
 
 template <bool WIDE, int DT, int GT, int N>
-__global__ void __launch_bounds__(64 * kDirectWaves) k_sum_direct(EmbeddingGradLaunch L, int slices, int sum_groups)
+__global__ void __launch_bounds__(64 * kDirectWaves)
+k_sum_direct(EmbeddingGradLaunch L, int slices, int log_group_slices, int groups_per_token, int sum_groups)
 {
     typedef typename Run<QADAM_F32, N>::F F;
     typedef typename Element<DT>::T D;
@@ -581,21 +583,23 @@ __global__ void __launch_bounds__(64 * kDirectWaves) k_sum_direct(EmbeddingGradL
         return;
     }
     const TokenReader<WIDE> read(L.t);
-    const int slice = blockIdx.x % slices, t = blockIdx.x / slices;
-    bool outside;
-    const uint32_t row = __builtin_amdgcn_readfirstlane(read(t, &outside));
-    if (row == ~0u) {
-        if (outside && slice == 0 && threadIdx.x == 0) atomicOr(L.t.status, QADAM_STATUS_TOKEN_RANGE);
-        return;
-    }
-    // the wavefront's part of the list
+    const int group = blockIdx.x % groups_per_token, t = blockIdx.x / groups_per_token;
+    // the wavefront's part of the list, with the workgroup's token under way beside it
     constexpr int kLoads = kDirectPart / 64;
+    bool outside;
+    const uint32_t own_row = read(t, &outside);
     uint32_t other[kLoads];
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {
         const int i = wave * kDirectPart + k * 64 + lane;
+        bool unused;
         other[k] = ~0u;
-        if (i < num) other[k] = read(i, &outside);
+        if (i < num) other[k] = read(i, &unused);
+    }
+    const uint32_t row = __builtin_amdgcn_readfirstlane(own_row);
+    if (row == ~0u) {
+        if (outside && group == 0 && threadIdx.x == 0) atomicOr(L.t.status, QADAM_STATUS_TOKEN_RANGE);
+        return;
     }
     int count = 0;
     bool earlier = false;
@@ -617,16 +621,17 @@ __global__ void __launch_bounds__(64 * kDirectWaves) k_sum_direct(EmbeddingGradL
         before[w] = total;
         total += n;
     }
-    const bool split = total > kBatch;
-    if (!split && wave > 0) return;
-    const int share = split ? (total + kDirectWaves - 1) / kDirectWaves : total;
-    const int begin = wave * share, end = begin + share < total ? begin + share : total;
+    const int group_slices = 1 << log_group_slices, slice = group * group_slices + wave % group_slices, turn = wave >> log_group_slices;
+    const int turns = total > kBatch ? kDirectWaves >> log_group_slices : 1;
+    if (turns == 1 && (turn > 0 || slice >= slices)) return;
+    const int share = (total + turns - 1) / turns;
+    const int begin = turn * share, end = begin + share < total ? begin + share : total;
     const int own = (slice * 64 + lane) * N;
     const int n = L.dim - own < 0 ? 0 : L.dim - own < N ? L.dim - own : N, col = n == N ? own : L.dim - N;
     const D* from = static_cast<const D*>(L.dout) + col;
     G* out = static_cast<G*>(L.grad) + col + (int64_t)row * L.grad_stride;
     typename Run<GT, N>::V old;
-    if (L.accumulate && wave == 0) old = load_raw<GT, N, false>(out);
+    if (L.accumulate && turn == 0) old = load_raw<GT, N, false>(out);
     F sum = 0.0f;
     for (int i = begin; i < end; i += kBatch) {
         // lane j has the position of the batch's token j
@@ -641,11 +646,11 @@ __global__ void __launch_bounds__(64 * kDirectWaves) k_sum_direct(EmbeddingGradL
         for (int j = 0; j < kBatch; ++j)
             if (i + j < end) sum += to_float<DT, N>(x[j]);
     }
-    if (split) {
+    if (turns > 1) {
         sums[wave][lane] = sum;
         __syncthreads();
-        if (wave > 0) return;
-        for (int w = 1; w < kDirectWaves; ++w) sum += sums[w][lane];
+        if (turn > 0) return;
+        for (int u = 1; u < turns; ++u) sum += sums[wave + u * group_slices][lane];
     }
     F y = sum * L.scale;
     if (L.accumulate) y = to_float<GT, N>(old) + y;
@@ -699,13 +704,16 @@ static hipError_t grad_of(const EmbeddingGradLaunch& L)
     const int64_t num = L.t.num;
     const int slices = column_slices(L.dim);
     int64_t clear_rows = L.accumulate ? 0 : L.t.rows;       // of the gradient, the first ones: if they have no token
-    if (num <= kDirectTokens) {
+    const int log_group_slices = slices > 2 ? 2 : slices - 1, groups_per_token = (slices + (1 << log_group_slices) - 1) >> log_group_slices;
+    if (num <= kDirectTokens && num * groups_per_token <= kDirectGroups) {
         const int64_t clear = (clear_rows + kDirectClear - 1) / kDirectClear;       // wavefronts
-        const int sums = (int)num * slices;
+        const int sums = (int)num * groups_per_token;
         const dim3 grid((unsigned)(sums + (clear + kDirectWaves - 1) / kDirectWaves)), block(64 * kDirectWaves);
         if (grid.x == 0) return hipSuccess;
-        if (L.t.bytes == 8) hipLaunchKernelGGL((k_sum_direct<true, DT, GT, N>), grid, block, 0, L.stream, L, slices, sums);
-        else hipLaunchKernelGGL((k_sum_direct<false, DT, GT, N>), grid, block, 0, L.stream, L, slices, sums);
+        if (L.t.bytes == 8)
+            hipLaunchKernelGGL((k_sum_direct<true, DT, GT, N>), grid, block, 0, L.stream, L, slices, log_group_slices, groups_per_token, sums);
+        else
+            hipLaunchKernelGGL((k_sum_direct<false, DT, GT, N>), grid, block, 0, L.stream, L, slices, log_group_slices, groups_per_token, sums);
         return hipGetLastError();
     }
     const int row_bits = bits_of((uint64_t)L.t.rows), bits = bits_of((uint64_t)num);
