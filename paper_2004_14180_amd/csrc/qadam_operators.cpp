@@ -87,17 +87,22 @@ struct List {
     DeviceArray<ListTile> tiles;
     DeviceArray<ListTensor> tensors;
 
+    static int64_t tiles_of(const ListTensor& t)
+    {
+        return t.numel > 0 ? (t.numel + (t.types >> kTypeBits) + kListTile - 1) / kListTile : 0;
+    }
+
     int build(const std::vector<ListTensor>& host)
     {
         int64_t count = 0;
-        for (const ListTensor& t : host) count += (t.numel + kListTile - 1) / kListTile;
+        for (const ListTensor& t : host) count += tiles_of(t);
         // a launch has a wavefront per block of 256 elements, 16 per tile
         if (count >= ((int64_t)1 << 32) / (64 * 16)) return fail(QADAM_ERANGE, "too many tiles for one launch (elements / 4096 must stay below 2^22)");
         std::vector<ListTile> all;
         all.reserve((size_t)count);
         for (size_t i = 0; i < host.size(); ++i) {
             if (i % kListGrads == 0) parts.push_back({(int32_t)i, 0, (int32_t)all.size(), 0});
-            const int32_t n = (int32_t)((host[i].numel + kListTile - 1) / kListTile);
+            const int32_t n = (int32_t)tiles_of(host[i]);
             for (int32_t k = 0; k < n; ++k) all.push_back({(int32_t)i, k});
             ++parts.back().num_tensors;
             parts.back().num_tiles += n;
@@ -185,8 +190,9 @@ int qadam_adamw_init(qadam_adamw_t* out, const qadam_adamw_config_t* cfg, const 
                 }
                 if (t.copy) QADAM_CHECK(check_address(t.copy, 2, "copy"));
             }
+            const int shift = cfg->state_bits == 8 ? 0 : block_shift(t.param, element_size(t.param_type));
             host.push_back({t.param, t.m, t.v, t.m_scales, t.v_scales, t.copy, t.numel,
-                            list_types(t.param_type, t.grad_type, t.copy ? t.copy_type : kNoCopy), t.weight_decay});
+                            list_types(t.param_type, t.grad_type, t.copy ? t.copy_type : kNoCopy) | shift << kTypeBits, t.weight_decay});
         }
         std::unique_ptr<qadam_adamw_ctx> h(new qadam_adamw_ctx);
         h->cfg = *cfg;

@@ -77,20 +77,23 @@ __device__ __forceinline__ float largest(f4 a)
     return fmaxf(b, c);
 }
 
-// four elements at p + at; of a ragged tensor those from `end` on repeat the last one
+// Of a ragged block a lane has the elements in [low, end); the others repeat the nearest one and are not stored.
+__device__ __forceinline__ int nearest(int i, int low, int end) { return i < low ? low : i < end ? i : end - 1; }
+
+// four elements at p + at
 template <int TYPE, bool WHOLE>
-__device__ __forceinline__ typename Run<TYPE, 4>::V load_four(const void* p, int at, int end)
+__device__ __forceinline__ typename Run<TYPE, 4>::V load_four(const void* p, int at, int low, int end)
 {
     const auto* q = static_cast<const typename Element<TYPE>::T*>(p);
     if constexpr (WHOLE) return load_raw<TYPE, 4>(q + at);
     typename Run<TYPE, 4>::V v;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = global(q)[at + k < end ? at + k : end - 1];
+    for (int k = 0; k < 4; ++k) v[k] = global(q)[nearest(at + k, low, end)];
     return v;
 }
 
 template <int TYPE, bool WHOLE>
-__device__ __forceinline__ void store_four(void* p, int at, int end, f4 x)
+__device__ __forceinline__ void store_four(void* p, int at, int low, int end, f4 x)
 {
     auto* q = static_cast<typename Element<TYPE>::T*>(p);
     if constexpr (WHOLE) {
@@ -98,7 +101,7 @@ __device__ __forceinline__ void store_four(void* p, int at, int end, f4 x)
     } else {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-            if (at + k < end) global(q)[at + k] = (typename Element<TYPE>::T)x[k];
+            if (at + k >= low && at + k < end) global(q)[at + k] = (typename Element<TYPE>::T)x[k];
     }
 }
 
@@ -130,19 +133,21 @@ __device__ __forceinline__ void store_bytes(void* p, int at, int end, uint32_t w
 // A block of a tensor, types known.  WHOLE: the tensor has all of it.
 template <bool STATE8, int PT, int GT, int CT, bool WHOLE>
 __device__ __forceinline__ void step_block(const AdamwScalars& S, const ListTensor& T, const void* grad, float lr_decay, float factor,
-                                           int64_t block, int lane)
+                                           int64_t first, int lane)
 {
-    const int64_t first = block * kBlock, left = T.numel - first;
-    const int at = lane * 4, end = left < kBlock ? (int)left : kBlock;
+    const int64_t left = T.numel - first;
+    const int at = lane * 4, low = first < 0 ? (int)-first : 0, end = left < kBlock ? (int)left : kBlock;
     const void* gp = static_cast<const typename Element<GT>::T*>(grad) + first;
     void* xp = static_cast<typename Element<PT>::T*>(T.param) + first;
-    const auto grad4 = load_four<GT, WHOLE>(gp, at, end);
-    const auto param4 = load_four<PT, WHOLE>(xp, at, end);
+    const auto grad4 = load_four<GT, WHOLE>(gp, at, low, end);
+    const auto param4 = load_four<PT, WHOLE>(xp, at, low, end);
     f4 m, v, r;
     void *mp, *vp;
+    int64_t block = 0;
     if constexpr (STATE8) {
         mp = static_cast<uint8_t*>(T.m) + first;
         vp = static_cast<uint8_t*>(T.v) + first;
+        block = first / kBlock;
         const uint32_t cm = load_bytes<WHOLE>(mp, at, end), cv = load_bytes<WHOLE>(vp, at, end);
         const float sm = global(T.m_scales)[block], sv = global(T.v_scales)[block];
         m = from_fp8(cm) * sm;
@@ -151,13 +156,13 @@ __device__ __forceinline__ void step_block(const AdamwScalars& S, const ListTens
     } else {
         mp = static_cast<float*>(T.m) + first;
         vp = static_cast<float*>(T.v) + first;
-        m = load_four<QADAM_F32, WHOLE>(mp, at, end);
-        v = load_four<QADAM_F32, WHOLE>(vp, at, end);
+        m = load_four<QADAM_F32, WHOLE>(mp, at, low, end);
+        v = load_four<QADAM_F32, WHOLE>(vp, at, low, end);
     }
     f4 x = to_float<PT, 4>(param4);
     adamw(S, lr_decay, factor, to_float<GT, 4>(grad4), x, m, v, r);
-    store_four<PT, WHOLE>(xp, at, end, x);
-    if constexpr (CT != kNoCopy) store_four<CT, WHOLE>(static_cast<typename Element<CT>::T*>(T.copy) + first, at, end, x);
+    store_four<PT, WHOLE>(xp, at, low, end, x);
+    if constexpr (CT != kNoCopy) store_four<CT, WHOLE>(static_cast<typename Element<CT>::T*>(T.copy) + first, at, low, end, x);
     if constexpr (STATE8) {
         if constexpr (!WHOLE)
 #pragma unroll
@@ -175,19 +180,19 @@ __device__ __forceinline__ void step_block(const AdamwScalars& S, const ListTens
             global(T.v_scales)[block] = nv;
         }
     } else {
-        store_four<QADAM_F32, WHOLE>(mp, at, end, m);
-        store_four<QADAM_F32, WHOLE>(vp, at, end, v);
+        store_four<QADAM_F32, WHOLE>(mp, at, low, end, m);
+        store_four<QADAM_F32, WHOLE>(vp, at, low, end, v);
     }
 }
 
 template <bool STATE8, bool WHOLE>
 __device__ __forceinline__ void step_block(const AdamwScalars& S, const ListTensor& T, const void* grad, float lr_decay, float factor,
-                                           int64_t block, int lane)
+                                           int64_t first, int lane)
 {
 #define QADAM_CASE(P, G, CP) \
-    case list_types(P, G, CP): step_block<STATE8, P, G, CP, WHOLE>(S, T, grad, lr_decay, factor, block, lane); break;
+    case list_types(P, G, CP): step_block<STATE8, P, G, CP, WHOLE>(S, T, grad, lr_decay, factor, first, lane); break;
 #define QADAM_CASES(P, CP) QADAM_CASE(P, QADAM_F32, CP) QADAM_CASE(P, QADAM_BF16, CP) QADAM_CASE(P, QADAM_F16, CP)
-    switch (T.types) {
+    switch (T.types & ((1 << kTypeBits) - 1)) {
         QADAM_CASES(QADAM_F32, kNoCopy)
         QADAM_CASES(QADAM_F32, QADAM_BF16)
         QADAM_CASES(QADAM_F32, QADAM_F16)
@@ -212,8 +217,9 @@ k_adamw(const ListTile* __restrict__ tiles, const ListTensor* __restrict__ tenso
     const int lane = threadIdx.x;
     const float lr_decay = S.lr * T.weight_decay;
     const int64_t block = (int64_t)tile.tile * kBlocksPerTile + blockIdx.x % kBlocksPerTile;
-    if ((block + 1) * kBlock <= T.numel) step_block<STATE8, true>(S, T, grad, lr_decay, factor, block, lane);
-    else if (block * kBlock < T.numel) step_block<STATE8, false>(S, T, grad, lr_decay, factor, block, lane);
+    const int64_t first = block * kBlock - (STATE8 ? 0 : T.types >> kTypeBits);
+    if (first >= 0 && first + kBlock <= T.numel) step_block<STATE8, true>(S, T, grad, lr_decay, factor, first, lane);
+    else if (first < T.numel) step_block<STATE8, false>(S, T, grad, lr_decay, factor, first, lane);
 }
 
 // Sum of the squares of the gradients: a workgroup takes every gridDim.x-th tile; the last one to arrive adds the sums of all.
@@ -230,41 +236,54 @@ __device__ __forceinline__ double group_sum(double x, double* shared)
     return x;
 }
 
-// the squares of what a thread has of a tile: runs of 8 elements, 256 runs apart
+template <int TYPE, int N>
+__device__ __forceinline__ double squares(typename Run<TYPE, N>::V v)
+{
+    double sum = 0.0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const double g = (float)v[k];
+        sum = fma(g, g, sum);
+    }
+    return sum;
+}
+
+// The squares of what a thread has of a tile: 16-byte runs from the first aligned address on, 256 runs apart, and of the up to 16 bytes
+// in front of them and behind them an element per thread.
 template <int TYPE>
 __device__ __forceinline__ double tile_squares(const void* tile, int n)
 {
-    constexpr int kRun = 8, kRuns = kListTile / (kRun * kNormThreads);
-    const auto* p = static_cast<const typename Element<TYPE>::T*>(tile);
+    typedef typename Element<TYPE>::T T;
+    constexpr int kRun = 16 / sizeof(T), kRuns = kListTile / (kRun * kNormThreads);
+    const T* p = static_cast<const T*>(tile);
+    const int thread = threadIdx.x, off = (int)(reinterpret_cast<uintptr_t>(p) % 16 / sizeof(T));
+    const int head = off ? (kRun - off < n ? kRun - off : n) : 0;
+    const T* q = p + head;
+    const int runs = (n - head) / kRun, tail = n - head - runs * kRun;
     double sum = 0.0;
-    if (n == kListTile) {
+    if (off == 0 && n == kListTile) {
         typename Run<TYPE, kRun>::V v[kRuns];
 #pragma unroll
-        for (int j = 0; j < kRuns; ++j) v[j] = load_raw<TYPE, kRun>(p + ((int)threadIdx.x + j * kNormThreads) * kRun);
+        for (int j = 0; j < kRuns; ++j) v[j] = load_raw<TYPE, kRun>(q + (thread + j * kNormThreads) * kRun);
 #pragma unroll
-        for (int j = 0; j < kRuns; ++j)
-#pragma unroll
-            for (int k = 0; k < kRun; ++k) {
-                const double g = (float)v[j][k];
-                sum = fma(g, g, sum);
-            }
+        for (int j = 0; j < kRuns; ++j) sum += squares<TYPE, kRun>(v[j]);
         return sum;
     }
-    for (int j = 0; j < kRuns; ++j) {
-        const int at = ((int)threadIdx.x + j * kNormThreads) * kRun;
-        if (at + kRun <= n) {
-            const auto v = load_raw<TYPE, kRun>(p + at);
+    // (a run behind the last one is the last one again, and does not count)
+    if (runs > 0) {
+        typename Run<TYPE, kRun>::V v[kRuns];
 #pragma unroll
-            for (int k = 0; k < kRun; ++k) {
-                const double g = (float)v[k];
-                sum = fma(g, g, sum);
-            }
-        } else {
-            for (int k = at; k < n; ++k) {
-                const double g = load_one(p, TYPE, k);
-                sum = fma(g, g, sum);
-            }
+        for (int j = 0; j < kRuns; ++j) {
+            const int r = thread + j * kNormThreads;
+            v[j] = load_raw<TYPE, kRun>(q + (r < runs ? r : runs - 1) * kRun);
         }
+#pragma unroll
+        for (int j = 0; j < kRuns; ++j)
+            if (thread + j * kNormThreads < runs) sum += squares<TYPE, kRun>(v[j]);
+    }
+    if (thread < head + tail) {
+        const double g = load_one(p, TYPE, thread < head ? thread : n - tail + thread - head);
+        sum = fma(g, g, sum);
     }
     return sum;
 }
@@ -290,18 +309,22 @@ k_grad_norm(const ListTile* __restrict__ tiles, const ListTensor* __restrict__ t
     }
     sum = group_sum(sum, shared);
     if (threadIdx.x == 0)
-        __hip_atomic_store(&N.sums[N.first_sum + blockIdx.x], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(global(&N.sums[N.first_sum + blockIdx.x]), sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (N.total == 0) return;           // a later launch finishes
-    if (threadIdx.x == 0)
-        last = __hip_atomic_fetch_add(N.arrived, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+    // The sums cross workgroups as agent-scope atomics: in memory before the arrival is counted, without a write-back of the caches
+    // (12 M elements in 1024 workgroups: 42 us with one each)
+    if (threadIdx.x == 0) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        last = __hip_atomic_fetch_add(global(N.arrived), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+    }
     __syncthreads();
     if (!last) return;
     sum = 0.0;
     for (int i = threadIdx.x; i < N.total; i += kNormThreads)
-        sum += __hip_atomic_load(&N.sums[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        sum += __hip_atomic_load(global(&N.sums[i]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     sum = group_sum(sum, shared);
     if (threadIdx.x == 0) {
-        __hip_atomic_store(N.arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(global(N.arrived), 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         const double norm = sqrt(sum);
         N.out[0] = (float)norm;
         N.out[1] = !(norm < (double)INFINITY) ? NAN : norm > (double)N.max_norm ? (float)((double)N.max_norm / norm) : 1.0f;
