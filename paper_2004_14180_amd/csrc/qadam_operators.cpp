@@ -103,7 +103,10 @@ struct List {
         for (size_t i = 0; i < host.size(); ++i) {
             if (i % kListGrads == 0) parts.push_back({(int32_t)i, 0, (int32_t)all.size(), 0});
             const int32_t n = (int32_t)tiles_of(host[i]);
-            for (int32_t k = 0; k < n; ++k) all.push_back({(int32_t)i, k});
+            for (int32_t k = 0; k < n; ++k) {
+                const int64_t left = host[i].numel - (int64_t)k * kListTile;
+                all.push_back({(int32_t)i, k, (int32_t)(left < kListTile ? left : kListTile), host[i].types >> 2 & 3});
+            }
             ++parts.back().num_tensors;
             parts.back().num_tiles += n;
             numels.push_back(host[i].numel);
@@ -259,8 +262,8 @@ int qadam_grad_norm_init(qadam_grad_norm_t* out, const int64_t* numels, const in
         h->total = 0;
         for (const List::Part& p : h->list.parts) h->total += norm_groups(p.num_tiles);
         QADAM_CHECK(allocate(h->sums, (size_t)h->total));
-        QADAM_CHECK(allocate(h->arrived, 1));
-        QADAM_HIP(hipMemset(h->arrived.get(), 0, sizeof(uint32_t)));
+        QADAM_CHECK(allocate(h->arrived, kArrivalWords));
+        QADAM_HIP(hipMemset(h->arrived.get(), 0, kArrivalWords * sizeof(uint32_t)));
         QADAM_HIP(hipStreamSynchronize(nullptr));
         *out = h.release();
         return QADAM_OK;

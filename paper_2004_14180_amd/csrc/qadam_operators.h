@@ -16,7 +16,10 @@ constexpr int kListGrads = 448;         // gradients' addresses of one launch: t
 struct ListTile {
     int32_t tensor;         // of the list
     int32_t tile;           // of the tensor
+    int32_t count;          // elements, of tensors that are not shifted
+    int32_t grad_type;
 };
+static_assert(sizeof(ListTile) == 16, "records are read as scalar loads");
 
 // One tensor as the kernels read it.
 struct ListTensor {
@@ -61,7 +64,10 @@ struct ListLaunch {
 
 hipError_t launch_adamw(const ListLaunch& L, const AdamwScalars& S, const GradTable& G, const float* grad_factor, bool state8);
 
-constexpr int kNormGroups = 1024;       // workgroups of a launch of the norm, at most
+constexpr int kNormGroups = 1536;       // workgroups of a launch of the norm, at most
+// arrivals of a launch: workgroups count in one of so many words, the last one of each in the first word, all in lines of their own
+// (one word for all of 1024 workgroups costs 12 us, 12 ns each)
+constexpr int kArrivalCounts = 32, kArrivalStride = 32, kArrivalWords = (kArrivalCounts + 1) * kArrivalStride;
 inline int norm_groups(int num_tiles) { return num_tiles < 1 ? 1 : num_tiles < kNormGroups ? num_tiles : kNormGroups; }
 
 // partial sums of a launch at sums + first_sum; the last launch (`total` > 0: sums of all launches) finishes

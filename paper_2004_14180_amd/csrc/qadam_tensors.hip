@@ -288,34 +288,43 @@ __device__ __forceinline__ double tile_squares(const void* tile, int n)
     return sum;
 }
 
+// whether this is the last of `of` arrivals, which leaves zero
+__device__ __forceinline__ bool arrive(uint32_t* count, uint32_t of)
+{
+    if (__hip_atomic_fetch_add(global(count), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != of - 1) return false;
+    __hip_atomic_store(global(count), 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return true;
+}
+
 __global__ void __launch_bounds__(kNormThreads)
-k_grad_norm(const ListTile* __restrict__ tiles, const ListTensor* __restrict__ tensors, int num_tiles, int first_tensor, NormLaunch N,
-            GradTable G)
+k_grad_norm(const ListTile* __restrict__ tiles, int num_tiles, int first_tensor, NormLaunch N, GradTable G)
 {
     __shared__ double shared[kNormThreads / kWave];
     __shared__ bool last;
     double sum = 0.0;
+    ListTile next{};
+    if ((int)blockIdx.x < num_tiles) next = tiles[blockIdx.x];
     for (int i = blockIdx.x; i < num_tiles; i += gridDim.x) {
-        const ListTile tile = tiles[i];
+        const ListTile tile = next;         // the next one's record is under way beside this one's elements
+        if (i + (int)gridDim.x < num_tiles) next = tiles[i + gridDim.x];
         const void* grad = G.grad[tile.tensor - first_tensor];
         if (!grad) continue;
-        const int64_t first = (int64_t)tile.tile * kListTile, numel = tensors[tile.tensor].numel;
-        const int type = tensors[tile.tensor].types >> 2 & 3;
-        const int n = numel - first < kListTile ? (int)(numel - first) : kListTile;
-        const char* p = static_cast<const char*>(grad) + first * element_size(type);
-        if (type == QADAM_F32) sum += tile_squares<QADAM_F32>(p, n);
-        else if (type == QADAM_BF16) sum += tile_squares<QADAM_BF16>(p, n);
-        else sum += tile_squares<QADAM_F16>(p, n);
+        const char* p = static_cast<const char*>(grad) + (int64_t)tile.tile * kListTile * element_size(tile.grad_type);
+        if (tile.grad_type == QADAM_F32) sum += tile_squares<QADAM_F32>(p, tile.count);
+        else if (tile.grad_type == QADAM_BF16) sum += tile_squares<QADAM_BF16>(p, tile.count);
+        else sum += tile_squares<QADAM_F16>(p, tile.count);
     }
     sum = group_sum(sum, shared);
     if (threadIdx.x == 0)
         __hip_atomic_store(global(&N.sums[N.first_sum + blockIdx.x]), sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (N.total == 0) return;           // a later launch finishes
     // The sums cross workgroups as agent-scope atomics: in memory before the arrival is counted, without a write-back of the caches
-    // (12 M elements in 1024 workgroups: 42 us with one each)
+    // (12 M elements in 1024 workgroups: 42 us with one each, 21 without)
     if (threadIdx.x == 0) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        last = __hip_atomic_fetch_add(global(N.arrived), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+        const uint32_t counts = gridDim.x < kArrivalCounts ? gridDim.x : kArrivalCounts, mine = blockIdx.x % counts;
+        last = arrive(N.arrived + (mine + 1) * kArrivalStride, (gridDim.x - mine + counts - 1) / counts) && arrive(N.arrived, counts);
+        asm volatile("" ::: "memory");
     }
     __syncthreads();
     if (!last) return;
@@ -324,7 +333,6 @@ k_grad_norm(const ListTile* __restrict__ tiles, const ListTensor* __restrict__ t
         sum += __hip_atomic_load(global(&N.sums[i]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     sum = group_sum(sum, shared);
     if (threadIdx.x == 0) {
-        __hip_atomic_store(global(N.arrived), 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         const double norm = sqrt(sum);
         N.out[0] = (float)norm;
         N.out[1] = !(norm < (double)INFINITY) ? NAN : norm > (double)N.max_norm ? (float)((double)N.max_norm / norm) : 1.0f;
@@ -345,7 +353,7 @@ hipError_t launch_adamw(const ListLaunch& L, const AdamwScalars& S, const GradTa
 
 hipError_t launch_grad_norm(const ListLaunch& L, const NormLaunch& N, const GradTable& G)
 {
-    hipLaunchKernelGGL(k_grad_norm, dim3(norm_groups(L.num_tiles)), dim3(kNormThreads), 0, L.stream, L.tiles + L.first_tile, L.tensors,
+    hipLaunchKernelGGL(k_grad_norm, dim3(norm_groups(L.num_tiles)), dim3(kNormThreads), 0, L.stream, L.tiles + L.first_tile,
                        L.num_tiles, L.first_tensor, N, G);
     return hipGetLastError();
 }
