@@ -70,7 +70,7 @@ __device__ __forceinline__ void clear_row(const EmbeddingGradLaunch& L, int64_t 
     constexpr int kWide = 16 / sizeof(G);
     G* p = static_cast<G*>(L.grad) + row * L.grad_stride;
     int at = lane * kWide;
-    for (; at + kWide <= L.dim; at += 64 * kWide) store_run<QADAM_F32, 4>(p + at, (f4)0.0f);
+    for (; at + kWide <= L.dim; at += 64 * kWide) store_run<GT, kWide>(p + at, (typename Run<GT, kWide>::F)0.0f);
     if (at < L.dim)
         for (; at < L.dim; ++at) global(p)[at] = (G)0.0f;
 }
