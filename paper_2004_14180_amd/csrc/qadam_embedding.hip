@@ -85,11 +85,12 @@ static int64_t early_rows(int64_t tokens, int64_t rows, int64_t row_bytes)
     return n < rows ? n : rows;
 }
 
-// Lists of up to kGroupTokens tokens are sorted in one launch: workgroup b takes the rows with row % kGroups = b, so the order is by
-// row % kGroups, then by row.  Every workgroup reads the whole list, a part per wavefront: it counts the tokens of smaller b, which
-// gives the place of its own, and keeps those in LDS as `row / kGroups << bits | position`.  They are ordered by
-// counting row / kGroups.  One more workgroup writes `rows` behind the last one, for the tokens without a row.
-constexpr int kGroupBits = 8, kGroups = 1 << kGroupBits;
+// Lists of up to kGroupTokens tokens are sorted in one launch: workgroup b takes the rows with row % groups = b, so the order is by
+// row % groups, then by row.  Every workgroup reads the whole list, a part per wavefront: it counts the tokens of smaller b, which
+// gives the place of its own, and keeps those in LDS as `row / groups << bits | position`.  They are ordered by counting row / groups.
+// One more workgroup writes `rows` behind the last one, for the tokens without a row.  256 groups, one per CU, as long as row / groups
+// has no more than kSortBits bits; up to 1024 for more rows.
+constexpr int kGroupBits = 8, kMostGroupBits = 10;
 constexpr int kGroupThreads = 1024, kGroupWaves = kGroupThreads / 64;
 constexpr int64_t kGroupTokens = 1 << 17;
 constexpr int kKept = 752;              // tokens of a wavefront in LDS; a part with more of the workgroup's is read again.  Two
@@ -125,15 +126,16 @@ __device__ __forceinline__ int lanes_below(uint64_t mask)
 }
 
 template <bool WIDE, int GT>
-__global__ void __launch_bounds__(kGroupThreads) k_group(EmbeddingGradLaunch L, int bits, int digit_bits, int64_t clear_from)
+__global__ void __launch_bounds__(kGroupThreads) k_group(EmbeddingGradLaunch L, int bits, int digit_bits, int group_bits, int64_t clear_from)
 {
     __shared__ uint32_t kept[kGroupWaves][kKept];
     __shared__ uint32_t place[kGroupWaves][1 << kSortBits];
     __shared__ uint32_t wave_count[kGroupWaves], wave_smaller[kGroupWaves], wave_ahead[kGroupWaves];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), group = blockIdx.x;
-    if (group > kGroups) {
+    const int groups = 1 << group_bits;
+    if (group > groups) {
         // the GPU's memory has little to do meanwhile: the last rows of the gradient, whether or not they have tokens
-        const int64_t first = clear_from + ((int64_t)(group - kGroups - 1) * kGroupWaves + wave) * kClearRows;
+        const int64_t first = clear_from + ((int64_t)(group - groups - 1) * kGroupWaves + wave) * kClearRows;
         for (int64_t r = first; r < first + kClearRows && r < L.t.rows; ++r) clear_row<GT>(L, r, lane);
         return;
     }
@@ -155,11 +157,11 @@ __global__ void __launch_bounds__(kGroupThreads) k_group(EmbeddingGradLaunch L, 
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) {
             any_outside |= outside[k];
-            const uint64_t own = __ballot(row[k] != ~0u && (int)(row[k] % kGroups) == group);
-            smaller += __popcll(__ballot(row[k] != ~0u && (int)(row[k] % kGroups) < group));
+            const uint64_t own = __ballot(row[k] != ~0u && (int)(row[k] & (groups - 1)) == group);
+            smaller += __popcll(__ballot(row[k] != ~0u && (int)(row[k] & (groups - 1)) < group));
             if (!own) continue;
             const int at = count + lanes_below(own);
-            if (own >> lane & 1 && at < kKept) kept[wave][at] = row[k] / kGroups << bits | (uint32_t)(i0 + k * 64 + lane);
+            if (own >> lane & 1 && at < kKept) kept[wave][at] = row[k] >> group_bits << bits | (uint32_t)(i0 + k * 64 + lane);
             count += __popcll(own);
         }
     }
@@ -174,7 +176,7 @@ __global__ void __launch_bounds__(kGroupThreads) k_group(EmbeddingGradLaunch L, 
         all_kept &= n <= kKept;
     }
     int32_t *keys = L.w.keys[0], *order = L.w.order[0];
-    if (group == kGroups) {
+    if (group == groups) {
         // every token with a row is smaller
         for (int i = base + threadIdx.x; i < num; i += kGroupThreads) global(keys)[i] = (int)L.t.rows;
         if (any_outside) atomicOr(L.t.status, QADAM_STATUS_TOKEN_RANGE);
@@ -182,7 +184,7 @@ __global__ void __launch_bounds__(kGroupThreads) k_group(EmbeddingGradLaunch L, 
     }
     if (total == 0) return;
     const uint32_t position = (1u << bits) - 1;
-    // the wavefront's tokens, 64 at a time: body(whether the lane has one, row / kGroups << bits | position)
+    // the wavefront's tokens, 64 at a time: body(whether the lane has one, row / groups << bits | position)
     auto each = [&](auto&& body) {
         if (all_kept) {
             for (int i = 0; i < count; i += 64) body(i + lane < count, kept[wave][i + lane < count ? i + lane : 0]);
@@ -190,7 +192,7 @@ __global__ void __launch_bounds__(kGroupThreads) k_group(EmbeddingGradLaunch L, 
             for (int i = begin; i < end; i += 64) {
                 bool outside;
                 const uint32_t row = read(i + lane < end ? i + lane : end - 1, &outside);
-                body(i + lane < end && row != ~0u && (int)(row % kGroups) == group, row / kGroups << bits | (uint32_t)(i + lane));
+                body(i + lane < end && row != ~0u && (int)(row & (groups - 1)) == group, row >> group_bits << bits | (uint32_t)(i + lane));
             }
         }
     };
@@ -234,7 +236,7 @@ __global__ void __launch_bounds__(kGroupThreads) k_group(EmbeddingGradLaunch L, 
         const int rank = lanes_below(same);
         if (valid) {
             const uint32_t at = place[wave][digit] + rank;
-            global(keys)[at] = (int)(digit * kGroups + (uint32_t)group);
+            global(keys)[at] = (int)(digit << group_bits | (uint32_t)group);
             global(order)[at] = (int)(c & position);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -442,22 +444,22 @@ __device__ __forceinline__ void join_piece(const EmbeddingGradLaunch& L, const i
 }
 
 // what the sorted list is ordered by
-__device__ __forceinline__ uint32_t sorted_by(uint32_t row, bool grouped)
+__device__ __forceinline__ uint32_t sorted_by(uint32_t row, int group_bits)
 {
-    return grouped ? row % kGroups << (32 - kGroupBits) | row / kGroups : row;
+    return group_bits ? row << (32 - group_bits) | row >> group_bits : row;
 }
 
 // Rows without a token become zeros: lane r looks for the wavefront's row r in the sorted list.
 template <int GT>
-__device__ __forceinline__ void clear_absent(const EmbeddingGradLaunch& L, const int* keys, bool grouped, int64_t first, int64_t end, int lane)
+__device__ __forceinline__ void clear_absent(const EmbeddingGradLaunch& L, const int* keys, int group_bits, int64_t first, int64_t end, int lane)
 {
     const int64_t row = first + lane % kClearRows;
-    const uint32_t want = sorted_by((uint32_t)row, grouped);
+    const uint32_t want = sorted_by((uint32_t)row, group_bits);
     int low = 0, high = (int)L.t.num;       // the first one that is not smaller
     while (low < high) {
         const int mid = (low + high) / 2;
         const uint32_t k = (uint32_t)global(keys)[mid];
-        const bool less = k < (uint32_t)L.t.rows && sorted_by(k, grouped) < want;
+        const bool less = k < (uint32_t)L.t.rows && sorted_by(k, group_bits) < want;
         low = less ? mid + 1 : low;
         high = less ? high : mid;
     }
@@ -468,7 +470,7 @@ __device__ __forceinline__ void clear_absent(const EmbeddingGradLaunch& L, const
 }
 
 template <int DT, int GT, int N, bool ACCUMULATE>
-__global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int result, int slices, int sum_groups, bool grouped, int64_t clear_rows)
+__global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int result, int slices, int sum_groups, int group_bits, int64_t clear_rows)
 {
     typedef typename Run<QADAM_F32, N>::F F;
     typedef typename Element<DT>::T D;
@@ -476,7 +478,7 @@ __global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int resu
     const int* keys = L.w.keys[result];
     const int lane = threadIdx.x;
     if (!ACCUMULATE && (int)blockIdx.x >= sum_groups) {
-        clear_absent<GT>(L, keys, grouped, (int64_t)((int)blockIdx.x - sum_groups) * kClearRows, clear_rows, lane);
+        clear_absent<GT>(L, keys, group_bits, (int64_t)((int)blockIdx.x - sum_groups) * kClearRows, clear_rows, lane);
         return;
     }
     const int slice = blockIdx.x % slices, first = blockIdx.x / slices * kChunk, num = (int)L.t.num;
@@ -718,15 +720,16 @@ static hipError_t grad_of(const EmbeddingGradLaunch& L)
     }
     const int row_bits = bits_of((uint64_t)L.t.rows), bits = bits_of((uint64_t)num);
     int result = 0;
-    const bool grouped = num <= kGroupTokens && row_bits <= kGroupBits + kSortBits;
-    if (grouped) {
-        const int digit = row_bits > kGroupBits ? row_bits - kGroupBits : 0;
+    int group_bits = 0;
+    if (num <= kGroupTokens && row_bits <= kMostGroupBits + kSortBits) {
+        group_bits = row_bits - kSortBits > kGroupBits ? row_bits - kSortBits : kGroupBits;
+        const int digit = row_bits > group_bits ? row_bits - group_bits : 0;
         if (!L.accumulate) clear_rows -= early_rows(num, L.t.rows, (int64_t)L.dim * element_size(GT));
         const int64_t early = L.accumulate ? 0 : L.t.rows - clear_rows;
         constexpr int kEach = kGroupWaves * kClearRows;
-        const dim3 grid((unsigned)(kGroups + 1 + (early + kEach - 1) / kEach)), block(kGroupThreads);
-        if (L.t.bytes == 8) hipLaunchKernelGGL((k_group<true, GT>), grid, block, 0, L.stream, L, bits, digit, clear_rows);
-        else hipLaunchKernelGGL((k_group<false, GT>), grid, block, 0, L.stream, L, bits, digit, clear_rows);
+        const dim3 grid((unsigned)((1 << group_bits) + 1 + (early + kEach - 1) / kEach)), block(kGroupThreads);
+        if (L.t.bytes == 8) hipLaunchKernelGGL((k_group<true, GT>), grid, block, 0, L.stream, L, bits, digit, group_bits, clear_rows);
+        else hipLaunchKernelGGL((k_group<false, GT>), grid, block, 0, L.stream, L, bits, digit, group_bits, clear_rows);
         if (const hipError_t e = hipGetLastError()) return e;
     } else {
         const int passes = (row_bits + kSortBits - 1) / kSortBits, digit = (row_bits + passes - 1) / passes;
@@ -743,8 +746,8 @@ static hipError_t grad_of(const EmbeddingGradLaunch& L)
     }
     const int sums = (int)((num + kChunk - 1) / kChunk) * slices;
     const dim3 grid((unsigned)(sums + (clear_rows + kClearRows - 1) / kClearRows)), block(64);
-    if (L.accumulate) hipLaunchKernelGGL((k_sum_runs<DT, GT, N, true>), grid, block, 0, L.stream, L, result, slices, sums, grouped, clear_rows);
-    else hipLaunchKernelGGL((k_sum_runs<DT, GT, N, false>), grid, block, 0, L.stream, L, result, slices, sums, grouped, clear_rows);
+    if (L.accumulate) hipLaunchKernelGGL((k_sum_runs<DT, GT, N, true>), grid, block, 0, L.stream, L, result, slices, sums, group_bits, clear_rows);
+    else hipLaunchKernelGGL((k_sum_runs<DT, GT, N, false>), grid, block, 0, L.stream, L, result, slices, sums, group_bits, clear_rows);
     return hipGetLastError();
 }
 
