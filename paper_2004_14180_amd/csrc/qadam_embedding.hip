@@ -1,4 +1,14 @@
 // gfx950 kernels of the embedding: lookup with scaling, and the gradient by sorted tokens.
+//
+// Both are bound by memory where they are long and by launches and chains of loads where they are short.  The gradient of a row is
+// the sum of the dout of its tokens, so whoever adds must know them: atomics from every token would write each row as often as it
+// occurs and in no fixed order, while a list of positions sorted by row lets every row be written once, from registers, and makes
+// the result the same bits on every run.  Three ways, by sizes alone, us per call (second and third: in all of their launches):
+//   * up to 2048 tokens, one launch that needs no sort: each token looks for its row in the list (k_sum_direct).  1024 tokens of 768
+//     fp32, added to the matrix: 5.6 (sorted: 12);
+//   * up to 131072 tokens and 524 k rows, the sort is one launch (k_group) and the sums another (k_sum_runs).  16384 tokens of 2048
+//     bf16 and a matrix of 50257 rows written whole, 479 MB: 88;
+//   * beyond, the sort takes two launches per digit of up to 9 bits (140 k tokens: 54 for 17 bits of rows).
 #include "qadam_elements.h"
 #include "qadam_operators.h"
 
@@ -15,7 +25,9 @@ __device__ __forceinline__ int64_t token_row(const TokenList& L, int64_t t, bool
     return *out_of_range || tok == L.padding ? -1 : tok;
 }
 
-// Lookup: 1 << log_lanes lanes per row take runs of 8 elements.
+// Lookup: 1 << log_lanes lanes per row take runs of 8 elements.  Rows are read through the caches, since frequent tokens repeat; the
+// output streams past them: 16384 tokens of 2048 bf16 23.0 us without, 16.7 now (93 MB; 5.6 TB/s).  Several rows per lane, under way
+// together, only cost: 17.2 with two, 17.8 with four, 19.3 with eight.
 constexpr int kRun = 8;
 
 template <int WT, int OT>
@@ -78,7 +90,7 @@ __device__ __forceinline__ void clear_row(const EmbeddingGradLaunch& L, int64_t 
 constexpr int kClearRows = 2;           // rows of a wavefront that clears those without a token
 
 // Rows of this size that are cleared while lists are grouped, which leaves the memory idle: about 8 us and 0.6 per 1024 tokens, at 5 TB/s.
-// 16 k tokens, 412 MB: none 99.6 us per call, a quarter of this 99.0, half 96.6, this 93.5
+// 16384 tokens, 412 MB: none 99.6 us per call, a quarter of this 99.0, half 96.6, this 93.5 (then 88 with two rows per wavefront)
 static int64_t early_rows(int64_t tokens, int64_t rows, int64_t row_bytes)
 {
     const int64_t n = (40000000 + 3000 * tokens) / row_bytes;
@@ -93,8 +105,8 @@ static int64_t early_rows(int64_t tokens, int64_t rows, int64_t row_bytes)
 constexpr int kGroupBits = 8, kMostGroupBits = 10;
 constexpr int kGroupThreads = 1024, kGroupWaves = kGroupThreads / 64;
 constexpr int64_t kGroupTokens = 1 << 17;
-constexpr int kKept = 752;              // tokens of a wavefront in LDS; a part with more of the workgroup's is read again.  Two
-                                        // workgroups share a CU
+constexpr int kKept = 752;              // tokens of a wavefront in LDS, so that two workgroups share a CU; a list of more than
+                                        // 12032 tokens of which a wavefront finds more of its workgroup's is read again
 
 template <bool WIDE>
 struct TokenReader {
@@ -366,8 +378,10 @@ __global__ void __launch_bounds__(kThreads) k_move_digits(EmbeddingGradLaunch L,
 }
 
 // Sums.  Positions of the sorted list are cut where a row begins and at multiples of kRunPiece; a wavefront takes the pieces that begin
-// in its kChunk positions, in a slice of the columns.  A piece that is a whole run is finished here; the pieces of a longer run are put
-// down, and the wavefront that arrives last adds them in order.
+// in its kChunk positions, in a slice of the columns.  So the work is even whatever the tokens are: a frequent row is many wavefronts'.
+// A piece that is a whole run is finished here; the pieces of a longer run are put down, and the wavefront that arrives last adds them
+// in order.  Eight rows are under way at a time, when adding with the old values of theirs.  us of the sums, 16384 tokens of 2048 bf16,
+// matrix written / added to, 8191 of 1001 fp16, added: pieces of 24 tokens 75 / 50 / 14.8, of 32 79 / 69 / -, of 48 72 / 52 / 15.5.
 static_assert(kRunPiece % kChunk == 0 && kRunPiece < 64, "a piece ends at most kRunPiece behind the chunk's first position");
 constexpr int kBatch = 8;
 
@@ -385,7 +399,8 @@ __device__ __forceinline__ void store_columns(typename Element<TYPE>::T* p, int 
 
 // Puts down the sum of a piece of a run that other wavefronts have pieces of too, one per block of kRunPiece positions; the last
 // wavefront to arrive adds them in order.  What crosses from one wavefront to another are agent-scope atomics, which need no cache
-// written back: a piece is in memory before its arrival is counted.
+// written back: a piece is in memory before its arrival is counted.  (With a release fence per piece, which writes back the L2, the sums of
+// 16384 tokens of 2048 bf16 took 152 us instead of 35.)
 template <int GT, int N, bool ACCUMULATE>
 __device__ __forceinline__ void join_piece(const EmbeddingGradLaunch& L, const int32_t* keys, int row, int block, int32_t front, int32_t behind,
                                            bool is_head, typename Run<QADAM_F32, N>::F sum, int lane, int slice, int slices, int n, int col)
@@ -552,7 +567,8 @@ __global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int resu
 // where its token is the first of its row adds the dout of all of them, a wavefront per slice; of more than kBatch tokens the
 // wavefronts that a slice has take a part each.  Further workgroups clear the rows without a token.
 constexpr int kDirectTokens = 2048, kDirectWaves = 8, kDirectPart = kDirectTokens / kDirectWaves;
-constexpr int kDirectGroups = 2048;     // most workgroups that look through the list
+constexpr int kDirectGroups = 2048;     // most workgroups that look through the list: us with more of them / sorted, added: 1500 tokens
+                                        // of 2048 bf16 15.2 / 14.0, 1024 10.4 / 12.2; 2000 of 768 fp32 (below) 10.0 / 14.4
 constexpr int kDirectClear = 8;         // rows of a wavefront that clears, which reads the whole list for them
 
 template <bool WIDE, int GT>
