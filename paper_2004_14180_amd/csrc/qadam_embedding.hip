@@ -25,41 +25,39 @@ __device__ __forceinline__ int64_t token_row(const TokenList& L, int64_t t, bool
     return *out_of_range || tok == L.padding ? -1 : tok;
 }
 
-// Lookup: 1 << log_lanes lanes per row take runs of 8 elements.  Rows are read through the caches, since frequent tokens repeat; the
-// output streams past them: 16384 tokens of 2048 bf16 23.0 us without, 16.7 now (93 MB; 5.6 TB/s).  Several rows per lane, under way
-// together, only cost: 17.2 with two, 17.8 with four, 19.3 with eight.
+// Lookup: a lane takes a run of 8 elements of a row, the next lane the next run, and after a row's last run the next row's first.  Rows
+// are read through the caches, since frequent tokens repeat; the output streams past them: 16384 tokens of 2048 bf16 23.0 us without,
+// 16.7 now (93 MB; 5.6 TB/s).  Several rows per lane, under way together, only cost: 17.2 with two, 17.8 with four, 19.3 with eight.
 constexpr int kRun = 8;
 
 template <int WT, int OT>
-__device__ __forceinline__ void lookup_row(const LookupLaunch& L, int64_t t, int64_t row, int lane, int lanes)
+__device__ __forceinline__ void lookup_run(const LookupLaunch& L, int64_t t, int64_t row, int at)
 {
     typedef typename Element<WT>::T W;
     typedef typename Element<OT>::T O;
     const W* from = static_cast<const W*>(L.weight) + row * L.weight_stride;
     O* to = static_cast<O*>(L.out) + t * L.out_stride;
-    for (int at = lane * kRun; at < L.dim; at += lanes * kRun) {
-        if (at + kRun <= L.dim) {
-            typename Run<WT, kRun>::F x = 0.0f;         // zero, whatever the scale
-            if (row >= 0) x = to_float<WT, kRun>(load_raw<WT, kRun, false>(from + at)) * L.scale;
-            store_run<OT, kRun>(to + at, x);
-        } else {
-            for (int k = at; k < L.dim; ++k) global(to)[k] = (O)(row < 0 ? 0.0f : (float)global(from)[k] * L.scale);
-        }
+    if (at + kRun <= L.dim) {
+        typename Run<WT, kRun>::F x = 0.0f;             // zero, whatever the scale
+        if (row >= 0) x = to_float<WT, kRun>(load_raw<WT, kRun, false>(from + at)) * L.scale;
+        store_run<OT, kRun>(to + at, x);
+    } else {
+        for (int k = at; k < L.dim; ++k) global(to)[k] = (O)(row < 0 ? 0.0f : (float)global(from)[k] * L.scale);
     }
 }
 
 template <int WT>
-__global__ void __launch_bounds__(kThreads) k_lookup(LookupLaunch L, int log_lanes)
+__global__ void __launch_bounds__(kThreads) k_lookup(LookupLaunch L, uint32_t runs)
 {
-    const int lanes = 1 << log_lanes, lane = threadIdx.x & (lanes - 1);
-    const int64_t t = (int64_t)blockIdx.x * (kThreads >> log_lanes) + (threadIdx.x >> log_lanes);
+    const uint32_t i = blockIdx.x * kThreads + threadIdx.x, t = i / runs, run = i - t * runs;
     if (t >= L.t.num) return;
     bool outside;
     const int64_t row = token_row(L.t, t, &outside);
-    if (outside && lane == 0) atomicOr(L.t.status, QADAM_STATUS_TOKEN_RANGE);
-    if (L.out_type == QADAM_F32) lookup_row<WT, QADAM_F32>(L, t, row, lane, lanes);
-    else if (L.out_type == QADAM_BF16) lookup_row<WT, QADAM_BF16>(L, t, row, lane, lanes);
-    else lookup_row<WT, QADAM_F16>(L, t, row, lane, lanes);
+    if (outside && run == 0) atomicOr(L.t.status, QADAM_STATUS_TOKEN_RANGE);
+    const int at = (int)run * kRun;
+    if (L.out_type == QADAM_F32) lookup_run<WT, QADAM_F32>(L, t, row, at);
+    else if (L.out_type == QADAM_BF16) lookup_run<WT, QADAM_BF16>(L, t, row, at);
+    else lookup_run<WT, QADAM_F16>(L, t, row, at);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -678,31 +676,29 @@ k_sum_direct(EmbeddingGradLaunch L, int slices, int log_group_slices, int groups
 }  // namespace
 
 template <int WT>
-static hipError_t lookup_of(const LookupLaunch& L)
+static hipError_t lookup_of(const LookupLaunch& L, int64_t runs)
 {
-    int log_lanes = 0;
-    while ((1 << log_lanes) < kThreads && (1 << log_lanes) * kRun < L.dim) ++log_lanes;
-    const int64_t each = kThreads >> log_lanes;
-    hipLaunchKernelGGL(k_lookup<WT>, dim3((unsigned)((L.t.num + each - 1) / each)), dim3(kThreads), 0, L.stream, L, log_lanes);
+    hipLaunchKernelGGL(k_lookup<WT>, dim3((unsigned)((L.t.num * runs + kThreads - 1) / kThreads)), dim3(kThreads), 0, L.stream, L,
+                       (uint32_t)runs);
     return hipGetLastError();
 }
 
 hipError_t launch_embedding_lookup(const LookupLaunch& all)
 {
-    // workgroups times threads of a launch stay below 2^32: parts of 2^23 tokens
-    constexpr int64_t kPart = (int64_t)1 << 23;
-    for (int64_t at = 0; at < all.t.num; at += kPart) {
+    // a launch's runs are counted in 32 bits
+    const int64_t runs = (all.dim + kRun - 1) / kRun, part = ((int64_t)1 << 31) / runs;
+    for (int64_t at = 0; at < all.t.num; at += part) {
         LookupLaunch L = all;
         L.t.tokens = static_cast<const char*>(all.t.tokens) + at * all.t.bytes;
-        L.t.num = all.t.num - at < kPart ? all.t.num - at : kPart;
+        L.t.num = all.t.num - at < part ? all.t.num - at : part;
         L.out = static_cast<char*>(all.out) + at * all.out_stride * element_size(all.out_type);
         hipError_t e = hipErrorInvalidValue;
         switch (L.weight_type) {
-        case QADAM_F32: e = lookup_of<QADAM_F32>(L); break;
-        case QADAM_BF16: e = lookup_of<QADAM_BF16>(L); break;
-        case QADAM_F16: e = lookup_of<QADAM_F16>(L); break;
-        case QADAM_CODES8: e = lookup_of<QADAM_CODES8>(L); break;
-        case QADAM_CODES16: e = lookup_of<QADAM_CODES16>(L); break;
+        case QADAM_F32: e = lookup_of<QADAM_F32>(L, runs); break;
+        case QADAM_BF16: e = lookup_of<QADAM_BF16>(L, runs); break;
+        case QADAM_F16: e = lookup_of<QADAM_F16>(L, runs); break;
+        case QADAM_CODES8: e = lookup_of<QADAM_CODES8>(L, runs); break;
+        case QADAM_CODES16: e = lookup_of<QADAM_CODES16>(L, runs); break;
         }
         if (e != hipSuccess) return e;
     }

@@ -189,6 +189,36 @@ def test_on_another_stream_than_the_tensors():
     assert (params[0] == x.cuda()).all()
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_tensor_beyond_32_bits(bits):
+    """More than 2^31 elements in a slice that begins off every line: windows at both ends and around 2^31, zeros in between."""
+    n, offset = (1 << 31) + 70_001, 3
+    gen = _gen(9)
+    cfg = AdamWConfig(state_bits=bits)
+    dtype = F32 if bits == 32 else BF16
+    params = [torch.zeros(offset + n, dtype=dtype, device="cuda")[offset:]]
+    grads = [torch.zeros(offset + n, dtype=BF16, device="cuda")[offset:]]
+    state = adamw_state(cfg, params)
+    windows = [(0, 5000), ((1 << 31) - 4096, (1 << 31) + 4096), (n - 5000, n)]
+    for a, b in windows:
+        params[0][a:b] = torch.randn(b - a, generator=gen).to(dtype).cuda()
+        grads[0][a:b] = torch.randn(b - a, generator=gen).to(BF16).cuda()
+    before = [params[0][a:b].cpu() for a, b in windows]
+    AdamW(cfg, params, weight_decay=0.1, grad_dtype=BF16, **state).step(1, 1e-2, grads)
+    rest = int((params[0] != 0).sum())
+    for (a, b), x in zip(windows, before):
+        want, m, _, _ = adamw32(x, grads[0][a:b].cpu(), torch.zeros(b - a), torch.zeros(b - a), 1, 1e-2, 0.1)
+        assert torch.equal(params[0][a:b].cpu(), want.to(dtype)), a
+        if bits == 32:
+            assert torch.equal(state["m"][0][a:b].cpu(), m)
+        rest -= int((params[0][a:b] != 0).sum())
+    assert rest == 0
+    out = torch.zeros(2, device="cuda")
+    GradNorm([n], BF16).grad_norm(grads, 1.0, out)
+    want = sum(float(grads[0][a:b].double().square().sum()) for a, b in windows) ** 0.5
+    assert abs(float(out[0]) - want) <= 2.0 ** -23 * want
+
+
 def test_refusals():
     f32 = lambda n=8: torch.zeros(n, device="cuda")  # noqa: E731
     p = [f32()]
