@@ -378,8 +378,11 @@ __global__ void __launch_bounds__(kThreads) k_move_digits(EmbeddingGradLaunch L,
 // Sums.  Positions of the sorted list are cut where a row begins and at multiples of kRunPiece; a wavefront takes the pieces that begin
 // in its kChunk positions, in a slice of the columns.  So the work is even whatever the tokens are: a frequent row is many wavefronts'.
 // A piece that is a whole run is finished here; the pieces of a longer run are put down, and the wavefront that arrives last adds them
-// in order.  Eight rows are under way at a time, when adding with the old values of theirs.  us of the sums, 16384 tokens of 2048 bf16,
-// matrix written / added to, 8191 of 1001 fp16, added: pieces of 24 tokens 75 / 50 / 14.8, of 32 79 / 69 / -, of 48 72 / 52 / 15.5.
+// in order.  Eight rows are under way at a time, when adding with the old values of theirs.
+// Where a row is frequent the wavefronts with a whole piece are every (kRunPiece / kChunk)-th: an odd number, or they meet on a few CUs.
+// us of the sums, 16384 tokens of 2048 bf16, matrix written / added to, 8191 of 1001 fp16 added, 131 k of 512 bf16 added; chunks of 8
+// tokens with pieces of 24 75 / 50 / 14.9 / 83, 32 79 / 69 / - / 153, 40 73.6 / 48.6 / 14.4 / 74, 48 72 / 52 / 15.5 / 91, 56 72.8 /
+// 45.6 / 17.6 / 71; of 6 with 30 74 / 51 / 14.7 / 83; of 4 with 36 75 / 56 / 14.5 / 87.
 static_assert(kRunPiece % kChunk == 0 && kRunPiece < 64, "a piece ends at most kRunPiece behind the chunk's first position");
 constexpr int kBatch = 8;
 

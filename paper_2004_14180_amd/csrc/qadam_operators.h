@@ -102,7 +102,7 @@ hipError_t launch_embedding_lookup(const LookupLaunch& L);
 // Scratch of the gradient, for lists of up to max_tokens (embedding_scratch): the tokens' sorted order, and what joins long runs.
 constexpr int kSortTile = 4096;         // tokens of a workgroup of the sort in passes
 constexpr int kSortBits = 9;            // of a digit, at most
-constexpr int kRunPiece = 48;           // tokens of one row that a wavefront adds at most; longer runs are joined
+constexpr int kRunPiece = 40;           // tokens of one row that a wavefront adds at most; longer runs are joined
 constexpr int kChunk = 8;               // tokens whose pieces a wavefront takes
 
 struct EmbeddingScratch {
