@@ -349,8 +349,9 @@ int qadam_profile_work(qadam_handle_t h, qadam_profile_work_t* out);
  * state_bits = 32: m and v are fp32.  state_bits = 8: m and r = sqrt(v) are kept in blocks of QADAM_STATE_BLOCK consecutive elements
  * of a tensor (the last one may be shorter), each block with an fp32 scale, the elements as 8-bit floats with 4 exponent and 3 mantissa
  * bits (the finite-only kind, largest value 448) of the value divided by the scale:
- *     m_scales[b] = max|m| / 448,    m[i] = nearest(m (448 / max|m|));
- *     v_scales[b] = max r / 448,     v[i] = nearest(max(r (448 / max r), v > 0 ? 2^-9 : 0)).
+ *     m_scales[b] = max|m| (1/448),    m[i] = nearest(m (448 (1 / max|m|)));
+ *     v_scales[b] = max r (1/448),     v[i] = nearest(max(r (448 (1 / max r)), v > 0 ? 2^-9 : 0))
+ * with the reciprocals rounded to fp32.
  * The step itself takes the moments before this rounding.  2^-9 is the smallest positive value of the kind: a second moment above zero
  * never becomes zero, where m / (sqrt(v) + eps) would run away.  A block with max|m| < 2^-116 is kept as zeros.  A moment that is not
  * finite makes its whole block unusable: pass the factor of qadam_grad_norm, which skips such a step. */
@@ -401,7 +402,7 @@ int qadam_grad_norm_destroy(qadam_grad_norm_t h);
 int qadam_grad_norm(qadam_grad_norm_t h, const void* const* grads, float max_norm, float* out_dev, void* stream);
 
 /* Embedding: a matrix of `rows` rows of `dim` elements, looked up by tokens.  max_tokens (at most 2^24) bounds num_tokens of
- * qadam_embedding_grad, whose scratch the handle allocates: about max_tokens (16 + dim / 6) bytes.  Tokens are int32 or int64 (token_bytes 4 or 8).  `padding`: the row of a token that stands for
+ * qadam_embedding_grad, whose scratch the handle allocates: about max_tokens (16 + dim / 5) bytes.  Tokens are int32 or int64 (token_bytes 4 or 8).  `padding`: the row of a token that stands for
  * no text, or a number outside 0..rows-1 for none.  A token outside 0..rows-1 sets QADAM_STATUS_TOKEN_RANGE in the handle's status
  * word.  Both kinds look up zeros and have no gradient.  Strides: elements from one row to the next. */
 typedef struct qadam_embedding_ctx* qadam_embedding_t;

@@ -24,7 +24,7 @@ constexpr int kBlock = QADAM_STATE_BLOCK;       // a wavefront's 64 lanes of 4 e
 constexpr int kBlocksPerTile = kListTile / kBlock;
 static_assert(kBlock == 4 * kWave, "");
 
-constexpr float kFp8Max = 448.0f, kFp8Least = 0x1p-9f, kTinyBlock = 0x1p-116f;
+constexpr float kFp8Max = 448.0f, kFp8Unit = 1.0f / 448.0f, kFp8Least = 0x1p-9f, kTinyBlock = 0x1p-116f;
 
 // the largest of a wavefront's values, none of them negative, in every lane: within rows of 16 lanes, then from row to row, by DPP
 template <int CTRL>
@@ -82,8 +82,8 @@ __device__ __forceinline__ void adamw(const AdamwScalars& S, float lr_decay, flo
 __device__ __forceinline__ float block_scale(float big, float* inv)
 {
     if (big < kTinyBlock) big = 0.0f;
-    *inv = big > 0.0f ? kFp8Max / big : 0.0f;
-    return big / kFp8Max;
+    *inv = big > 0.0f ? kFp8Max * (1.0f / big) : 0.0f;
+    return big * kFp8Unit;
 }
 
 __device__ __forceinline__ float largest(f4 a)

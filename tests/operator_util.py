@@ -66,10 +66,10 @@ def fp8_blocks(x, positive, block=256):
     y = y.view(-1, block)
     big = y.abs().amax(1, keepdim=True)
     big = torch.where(big < 2.0 ** -116, torch.zeros_like(big), big)
-    q = y * torch.where(big > 0, torch.tensor(448.0) / big, torch.zeros_like(big))
+    q = y * torch.where(big > 0, (torch.ones_like(big) / big) * 448, torch.zeros_like(big))
     if positive:
         q = torch.where((y > 0) & (big > 0), q.clamp_min(2.0 ** -9), q)
-    return q.to(torch.float8_e4m3fn).view(-1)[:n], (big / 448).view(-1)
+    return q.to(torch.float8_e4m3fn).view(-1)[:n], (big * (torch.ones(1) / 448)).view(-1)
 
 
 def embedding_grad64(tokens, dout, rows, scale, padding=None):
