@@ -529,7 +529,7 @@ __global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int resu
             const int64_t t = __builtin_amdgcn_readlane(order, i + j < end ? i + j : end - 1);
             x[j] = load_raw<DT, N, false>(from + t * L.dout_stride);
         }
-        if constexpr (ACCUMULATE)
+        if (ACCUMULATE && (runs >> (i + 1) & ((1ull << kBatch) - 1)))       // some row ends in this batch
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {
                 const int64_t row = __builtin_amdgcn_readlane(key, i + j < end ? i + j : end - 1);
