@@ -7,7 +7,7 @@
 //   * up to 2048 tokens, one launch that needs no sort: each token looks for its row in the list (k_sum_direct).  1024 tokens of 768
 //     fp32, added to the matrix: 5.6 (sorted: 12);
 //   * up to 131072 tokens and 524 k rows, the sort is one launch (k_group) and the sums another (k_sum_runs).  16384 tokens of 2048
-//     bf16 and a matrix of 50257 rows written whole, 479 MB: 88;
+//     bf16 and a matrix of 50257 rows written whole, 479 MB: 90;
 //   * beyond, the sort takes two launches per digit of up to 9 bits (140 k tokens: 54 for 17 bits of rows).
 #include "qadam_elements.h"
 #include "qadam_operators.h"
@@ -27,7 +27,7 @@ __device__ __forceinline__ int64_t token_row(const TokenList& L, int64_t t, bool
 
 // Lookup: a lane takes a run of 8 elements of a row, the next lane the next run, and after a row's last run the next row's first.  Rows
 // are read through the caches, since frequent tokens repeat; the output streams past them: 16384 tokens of 2048 bf16 23.0 us without,
-// 16.7 now (93 MB; 5.6 TB/s).  Several rows per lane, under way together, only cost: 17.2 with two, 17.8 with four, 19.3 with eight.
+// 16.8 now (93 MB; 5.6 TB/s).  Several rows per lane, under way together, only cost: 17.2 with two, 17.8 with four, 19.3 with eight.
 constexpr int kRun = 8;
 
 template <int WT, int OT>
