@@ -32,7 +32,7 @@ struct Run {
     typedef float F __attribute__((ext_vector_type(N)));
 };
 
-// N elements at p; rounding to bfloat16 and half is to nearest, ties to even
+// N elements at p, read past the caches (ONCE) or through them
 template <int TYPE, int N, bool ONCE = true>
 __device__ __forceinline__ typename Run<TYPE, N>::V load_raw(const void* p)
 {
@@ -47,6 +47,7 @@ __device__ __forceinline__ typename Run<TYPE, N>::F to_float(typename Run<TYPE, 
     return __builtin_convertvector(v, typename Run<TYPE, N>::F);
 }
 
+// rounding to bfloat16 and half is to nearest, ties to even
 template <int TYPE, int N, bool ONCE = true>
 __device__ __forceinline__ void store_run(void* p, typename Run<TYPE, N>::F x)
 {
@@ -67,13 +68,6 @@ __device__ __forceinline__ float load_one(const void* p, int type, int64_t i)
     if (type == QADAM_F32) return global(static_cast<const float*>(p))[i];
     if (type == QADAM_BF16) return (float)global(static_cast<const __bf16*>(p))[i];
     return (float)global(static_cast<const _Float16*>(p))[i];
-}
-
-__device__ __forceinline__ void store_one(void* p, int type, int64_t i, float x)
-{
-    if (type == QADAM_F32) global(static_cast<float*>(p))[i] = x;
-    else if (type == QADAM_BF16) global(static_cast<__bf16*>(p))[i] = (__bf16)x;
-    else global(static_cast<_Float16*>(p))[i] = (_Float16)x;
 }
 
 }  // namespace qadam

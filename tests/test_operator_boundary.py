@@ -97,6 +97,28 @@ def test_rows_of_a_matrix():
         operators._on_device = old
 
 
+def test_native_calls_leave_other_forms_to_the_python_checks(lib):
+    """None, and nothing called: the entry points of these plans are address 0."""
+    from paper_2004_14180_amd import binding
+    native = binding._native
+    t = torch.zeros(16)
+    lists, emb = native.list_plan(0, 0, [16], [0]), native.embedding_plan(0, 2, 8, 0, 0)
+    for p in (None, lists):
+        assert native.adamw_step(p, -1, 0, 1, 1e-3, [t], None) is None
+        assert native.grad_norm(p, -1, 0, [t], 1.0, t) is None
+    for p in (None, emb):
+        assert native.embedding_lookup(p, -1, 0, t.view(2, 8), t.long(), t.view(2, 8), 1.0, None, None) is None
+        assert native.embedding_grad(p, -1, 0, t.long(), t.view(2, 8), t.view(2, 8), 1.0, None, False) is None
+    assert native.adamw_step(lists, 0, 0, "1", None, None, 3) is None
+    assert native.embedding_grad(emb, 0, 0, None, [], 2**70, "x", 1.5, None) is None
+    for bad in (lambda: native.list_plan(0, 0, [1], []), lambda: native.list_plan(0, 0, [1], ["a"]), lambda: native.list_plan(0),
+                lambda: native.embedding_plan(0, 1, 2, 3), lambda: native.adamw_step(lists), lambda: native.grad_norm(lists, 0)):
+        with pytest.raises(TypeError):
+            bad()
+    with pytest.raises(ValueError):
+        native.adamw_step(emb, 0, 0, 1, 1e-3, [t], None)               # another plan
+
+
 @pytest.mark.parametrize("source", SOURCES)
 def test_the_kernels_keep_out_of_scratch_and_hold_no_packed_fp32(source):
     from paper_2004_14180_amd.build import device_assembly, device_resource_usage
