@@ -566,8 +566,10 @@ __global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int resu
 
 // Short lists, in one launch without a sort: a workgroup per token and up to four slices of columns.  It looks through the list, and
 // where its token is the first of its row adds the dout of all of them, a wavefront per slice; of more than kBatch tokens the
-// wavefronts that a slice has take a part each.  Further workgroups clear the rows without a token.
-constexpr int kDirectTokens = 2048, kDirectWaves = 8, kDirectPart = kDirectTokens / kDirectWaves;
+// wavefronts that a slice has take a part each.  A row of more than kDirectPiece tokens is added by the workgroups of every
+// kDirectPiece-th of them, and the last one adds their sums.  Further workgroups clear the rows without a token.
+constexpr int kDirectWaves = 8, kDirectPart = kDirectTokens / kDirectWaves;
+constexpr int kDirectPiece = 64;        // us, 2048 tokens of 768 bf16, half of them / all of one row: by one workgroup 63 / 121, now 16 / 24
 constexpr int kDirectGroups = 2048;     // most workgroups that look through the list: us with more of them / sorted, added: 1500 tokens
                                         // of 2048 bf16 15.2 / 14.0, 1024 10.4 / 12.2; 2000 of 768 fp32 (below) 10.0 / 14.4
 constexpr int kDirectClear = 8;         // rows of a wavefront that clears, which reads the whole list for them
@@ -594,7 +596,7 @@ k_sum_direct(EmbeddingGradLaunch L, int slices, int log_group_slices, int groups
     typedef typename Run<QADAM_F32, N>::F F;
     typedef typename Element<DT>::T D;
     typedef typename Element<GT>::T G;
-    __shared__ int list[kDirectWaves][kDirectPart], found[kDirectWaves];
+    __shared__ int list[kDirectWaves][kDirectPart], found[kDirectWaves], in_front[kDirectWaves];
     __shared__ F sums[kDirectWaves][64];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), num = (int)L.t.num;
     if ((int)blockIdx.x >= sum_groups) {
@@ -620,31 +622,37 @@ k_sum_direct(EmbeddingGradLaunch L, int slices, int log_group_slices, int groups
         if (outside && group == 0 && threadIdx.x == 0) atomicOr(L.t.status, QADAM_STATUS_TOKEN_RANGE);
         return;
     }
-    int count = 0;
-    bool earlier = false;
+    int count = 0, front = 0;               // of the row's tokens, those in front of t
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {
         const int i = wave * kDirectPart + k * 64 + lane;
         const uint64_t same = __ballot(other[k] == row);
         if (!same) continue;
-        earlier |= __ballot(other[k] == row && i < t) != 0;
+        front += __popcll(__ballot(other[k] == row && i < t));
         if (same >> lane & 1) list[wave][count + lanes_below(same)] = i;
         count += __popcll(same);
     }
-    if (lane == 0) found[wave] = earlier ? -1 : count;
+    if (lane == 0) { found[wave] = count; in_front[wave] = front; }
     __syncthreads();
-    int total = 0, before[kDirectWaves];
+    int total = 0, index = 0, before[kDirectWaves];
     for (int w = 0; w < kDirectWaves; ++w) {
-        const int n = found[w];
-        if (n < 0) return;
         before[w] = total;
-        total += n;
+        total += found[w];
+        index += in_front[w];
     }
+    if (index % kDirectPiece != 0) return;
+    // the position of the row's token m
+    auto position = [&](int m) {
+        int part = 0;
+        for (int w = 1; w < kDirectWaves; ++w) part = m >= before[w] && found[w] > 0 ? w : part;
+        return list[part][m - before[part]];
+    };
+    const int stop = index + kDirectPiece < total ? index + kDirectPiece : total;
     const int group_slices = 1 << log_group_slices, slice = group * group_slices + wave % group_slices, turn = wave >> log_group_slices;
-    const int turns = total > kBatch ? kDirectWaves >> log_group_slices : 1;
+    const int turns = stop - index > kBatch ? kDirectWaves >> log_group_slices : 1;
     if (turns == 1 && (turn > 0 || slice >= slices)) return;
-    const int share = (total + turns - 1) / turns;
-    const int begin = turn * share, end = begin + share < total ? begin + share : total;
+    const int share = (stop - index + turns - 1) / turns;
+    const int begin = index + turn * share, end = begin + share < stop ? begin + share : stop;
     const int own = (slice * 64 + lane) * N;
     const int n = L.dim - own < 0 ? 0 : L.dim - own < N ? L.dim - own : N, col = n == N ? own : L.dim - N;
     const D* from = static_cast<const D*>(L.dout) + col;
@@ -654,10 +662,7 @@ k_sum_direct(EmbeddingGradLaunch L, int slices, int log_group_slices, int groups
     F sum = 0.0f;
     for (int i = begin; i < end; i += kBatch) {
         // lane j has the position of the batch's token j
-        const int m = i + lane % kBatch < end ? i + lane % kBatch : end - 1;
-        int part = 0;
-        for (int w = 1; w < kDirectWaves; ++w) part = m >= before[w] && found[w] > 0 ? w : part;
-        const int at = list[part][m - before[part]];
+        const int at = position(i + lane % kBatch < end ? i + lane % kBatch : end - 1);
         typename Run<DT, N>::V x[kBatch];
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) x[j] = load_raw<DT, N, false>(from + (int64_t)__builtin_amdgcn_readlane(at, j) * L.dout_stride);
@@ -670,6 +675,36 @@ k_sum_direct(EmbeddingGradLaunch L, int slices, int log_group_slices, int groups
         __syncthreads();
         if (turn > 0) return;
         for (int u = 1; u < turns; ++u) sum += sums[wave + u * group_slices][lane];
+    }
+    if (total > kDirectPiece) {
+        // as in join_piece; a piece's place is its first token's, the row's count that of the row's first token
+        if (slice >= slices) return;
+        float* put = L.w.pieces + (int64_t)t * L.dim + col;
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (k >= N - n) __hip_atomic_store(global(put + k), sum[k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        uint32_t* arrived = L.w.arrived + (int64_t)__builtin_amdgcn_readfirstlane(position(0)) * slices + slice;
+        const int pieces = (total + kDirectPiece - 1) / kDirectPiece;
+        int come = 0;
+        if (lane == 0) come = (int)__hip_atomic_fetch_add(global(arrived), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (__builtin_amdgcn_readfirstlane(come) != pieces - 1) return;
+        asm volatile("" ::: "memory");
+        if (lane == 0) __hip_atomic_store(global(arrived), 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        sum = 0.0f;
+        for (int b = 0; b < pieces; b += kBatch) {
+            const int at = position((b + lane % kBatch < pieces ? b + lane % kBatch : pieces - 1) * kDirectPiece);
+            F x[kBatch];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                const float* get = L.w.pieces + (int64_t)__builtin_amdgcn_readlane(at, j) * L.dim + col;
+#pragma unroll
+                for (int k = 0; k < N; ++k) x[j][k] = __hip_atomic_load(global(get + k), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j)
+                if (b + j < pieces) sum += x[j];
+        }
     }
     F y = sum * L.scale;
     if (L.accumulate) y = to_float<GT, N>(old) + y;

@@ -105,12 +105,14 @@ constexpr int kSortBits = 9;            // of a digit, at most
 constexpr int kRunPiece = 40;           // tokens of one row that a wavefront adds at most; longer runs are joined
 constexpr int kChunk = 8;               // tokens whose pieces a wavefront takes
 
+constexpr int kDirectTokens = 2048;     // most tokens of a list that is not sorted
+
 struct EmbeddingScratch {
     int32_t*  keys[2];      // [max_tokens] rows in ascending order, `rows` for tokens without one
     int32_t*  order[2];     // [max_tokens] their positions in the list
     uint32_t* counts;       // [tiles][1 << kSortBits]
-    float*    pieces;       // [2 (max_tokens / kRunPiece + 1)][dim]
-    uint32_t* arrived;      // [max_tokens / kRunPiece + 1][slices of columns], zero between launches
+    float*    pieces;       // [piece_places(max_tokens)][dim]
+    uint32_t* arrived;      // [arrival_places(max_tokens)][slices of columns], zero between launches
 };
 
 struct EmbeddingGradLaunch {
@@ -126,7 +128,17 @@ struct EmbeddingGradLaunch {
 hipError_t launch_embedding_grad(const EmbeddingGradLaunch& L);
 
 inline int64_t sort_tiles(int64_t tokens) { return (tokens + kSortTile - 1) / kSortTile; }
-inline int64_t run_blocks(int64_t tokens) { return tokens / kRunPiece + 1; }
+// sorted lists have two pieces per block of kRunPiece tokens, others one per token
+inline int64_t arrival_places(int64_t tokens)
+{
+    const int64_t blocks = tokens / kRunPiece + 1, direct = tokens < kDirectTokens ? tokens : kDirectTokens;
+    return blocks > direct ? blocks : direct;
+}
+inline int64_t piece_places(int64_t tokens)
+{
+    const int64_t blocks = 2 * (tokens / kRunPiece + 1), direct = tokens < kDirectTokens ? tokens : kDirectTokens;
+    return blocks > direct ? blocks : direct;
+}
 // a lane's columns: 4, or as few as leave no lane of a narrow matrix idle
 inline int lane_columns(int dim) { return dim > 128 ? 4 : dim > 64 ? 2 : 1; }
 inline int column_slices(int dim) { return (dim + 64 * lane_columns(dim) - 1) / (64 * lane_columns(dim)); }

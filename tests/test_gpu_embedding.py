@@ -96,7 +96,7 @@ def test_lookup_of_the_codes_that_the_step_emits():
 
 GRAD_SHAPES = [(7, 1, 1, 0, 0), (50, 8, 3, 0, 0), (301, 257, 130, 3, 1), (1000, 768, 1024, 0, 1), (129, 1000, 333, 8, 3),
                (2000, 64, 5000, 0, 0), (70_000, 40, 9000, 0, 0), (600, 130, 20_011, 2, 1), (64, 2048, 2500, 0, 0), (3, 5000, 700, 1, 1),
-               (200_000, 9, 3000, 0, 1), (300_007, 12, 5001, 0, 0), (530_001, 7, 2500, 0, 0), (900, 20, 140_001, 1, 0), (11, 129, 2049, 0, 0), (255, 65, 2100, 2, 1)]
+               (200_000, 9, 3000, 0, 1), (300_007, 12, 5001, 0, 0), (530_001, 7, 2500, 0, 0), (900, 20, 140_001, 1, 0), (11, 129, 2049, 0, 0), (5, 1025, 2000, 0, 0), (40, 70, 2048, 0, 0), (255, 65, 2100, 2, 1)]
 
 
 @pytest.mark.parametrize("rows,dim,n,gap,offset", GRAD_SHAPES)
