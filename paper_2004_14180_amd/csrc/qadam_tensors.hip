@@ -26,7 +26,7 @@ static_assert(kBlock == 4 * kWave, "");
 
 constexpr float kFp8Max = 448.0f, kFp8Unit = 1.0f / 448.0f, kFp8Least = 0x1p-9f, kTinyBlock = 0x1p-116f;
 
-// the largest of a wavefront's values, none of them negative, in every lane: within rows of 16 lanes, then from row to row, by DPP
+// the largest of a wavefront's numbers, in every lane: within rows of 16 lanes, then from row to row, by DPP
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp_max(uint32_t x)
 {
@@ -34,9 +34,8 @@ __device__ __forceinline__ uint32_t dpp_max(uint32_t x)
     return y > x ? y : x;
 }
 
-__device__ __forceinline__ float wave_max(float value)
+__device__ __forceinline__ float wave_max(uint32_t x)
 {
-    uint32_t x = __float_as_uint(value);        // orders like the values; a NaN is above every number
     x = dpp_max<0x111>(x);      // one lane to the right, two, four, eight
     x = dpp_max<0x112>(x);
     x = dpp_max<0x114>(x);
@@ -86,10 +85,16 @@ __device__ __forceinline__ float block_scale(float big, float* inv)
     return big * kFp8Unit;
 }
 
-__device__ __forceinline__ float largest(f4 a)
+// The largest magnitude, as bits: they order like the values, and a NaN is above every number, where a maximum of floats drops it.
+__device__ __forceinline__ uint32_t largest(f4 a)
 {
-    const float b = fmaxf(fabsf(a[0]), fabsf(a[1])), c = fmaxf(fabsf(a[2]), fabsf(a[3]));
-    return fmaxf(b, c);
+    uint32_t x = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t y = __float_as_uint(fabsf(a[k]));
+        x = y > x ? y : x;
+    }
+    return x;
 }
 
 // Of a ragged block a lane has the elements in [low, end); the others repeat the nearest one and are not stored.

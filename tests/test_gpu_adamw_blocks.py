@@ -1,0 +1,39 @@
+"""Blocks of 8-bit moments that hold values which are not finite, against the header's formulas."""
+import pytest
+import torch
+
+from operator_util import adamw32, fp8_blocks
+from paper_2004_14180_amd import AdamW, AdamWConfig, adamw_state
+
+pytestmark = pytest.mark.gpu
+NAN, INF = float("nan"), float("inf")
+
+
+def _same(got, want, what):
+    got, want = got.float().cpu(), want.float()
+    assert torch.equal(got.isnan(), want.isnan()), what
+    assert torch.equal(got.nan_to_num(nan=0.0, posinf=3e38), want.nan_to_num(nan=0.0, posinf=3e38)), what
+
+
+# (elements of the block, value): alone among a lane's four, a whole lane, beside an infinity, in a lane of zeros
+BAD = [([5], NAN), ([4, 5, 6, 7], NAN), ([0], NAN), ([255], -NAN), ([9, 40, 41], NAN), ([8], NAN), ([3], INF), ([200, 201], -INF)]
+
+
+@pytest.mark.parametrize("size", [256 * (len(BAD) + 1), 256 * len(BAD) + 37])
+def test_values_that_are_not_finite_spread_over_their_block(size):
+    gen = torch.Generator().manual_seed(size)
+    g = torch.randn(size, generator=gen)
+    for b, (at, value) in enumerate(BAD):
+        g[[256 * b + i for i in at]] = value
+    g[256 * 4 + 100], g[256 * 5:256 * 5 + 8], g[256 * 5 + 8] = INF, 0.0, NAN
+    cfg = AdamWConfig(state_bits=8)
+    params = [torch.ones(size, device="cuda")]
+    state = adamw_state(cfg, params)
+    AdamW(cfg, params, **state).step(1, 1e-3, [g.cuda()])
+    _, m, _, r = adamw32(torch.ones(size), g, torch.zeros(size), torch.zeros(size), 1, 1e-3, 0.0)
+    for name, x in (("m", m), ("v", r)):
+        q, scale = fp8_blocks(x, name == "v")
+        assert scale[:6].isnan().all() and scale[6:8].isinf().all() and scale[8].isfinite()
+        _same(state[name + "_scales"][0], scale, name + "_scales")
+        for a, b in ((0, 6 * 256), (8 * 256, size)):
+            _same(state[name][0][a:b], q[a:b], name)
