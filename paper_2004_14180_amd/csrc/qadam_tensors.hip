@@ -191,8 +191,9 @@ __device__ __forceinline__ void step_block(const AdamwScalars& S, const ListTens
         float im, iv;
         const float nm = block_scale(wave_max(largest(m)), &im), nv = block_scale(wave_max(largest(r)), &iv);
         f4 q = r * iv;
+        const float least = nv > 0.0f ? kFp8Least : 0.0f;       // (not where the block is kept as zeros or holds a NaN; a NaN stays one)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) q[k] = r[k] > 0.0f && iv > 0.0f ? fmaxf(q[k], kFp8Least) : q[k];
+        for (int k = 0; k < 4; ++k) q[k] = r[k] > 0.0f && q[k] < least ? least : q[k];
         store_bytes<WHOLE>(mp, at, end, to_fp8(m * im));
         store_bytes<WHOLE>(vp, at, end, to_fp8(q));
         if (lane == 0) {

@@ -37,3 +37,31 @@ def test_values_that_are_not_finite_spread_over_their_block(size):
         _same(state[name + "_scales"][0], scale, name + "_scales")
         for a, b in ((0, 6 * 256), (8 * 256, size)):
             _same(state[name][0][a:b], q[a:b], name)
+
+
+def test_a_second_moment_beyond_fp32():
+    """Squares beyond fp32 beside gradients that are finite: in their block the other second moments keep the smallest code, so they are
+    infinite from then on and its weights rest, and nothing happens to the weights of other blocks."""
+    gen = torch.Generator().manual_seed(2)
+    n = 1000
+    g = torch.randn(n, generator=gen)
+    g[[3, 300, 301, 302, 303, 999]] = torch.tensor([1e20, 1e20, -3e19, 2e19, 1e38, -1e21])
+    g[:2] = 0.0
+    cfg = AdamWConfig(state_bits=8)
+    params = [torch.ones(n, device="cuda")]
+    state = adamw_state(cfg, params)
+    opt = AdamW(cfg, params, **state)
+    m = v = torch.zeros(n)
+    x = torch.ones(n)
+    for step in (1, 2):
+        opt.step(step, 1e-3, [g.cuda()])
+        x, m, v, r = adamw32(x, g, m, v, step, 1e-3, 0.0)
+        _same(params[0], x, "x")
+        for name, value in (("m", m), ("v", r)):
+            q, scale = fp8_blocks(value, name == "v")
+            _same(state[name + "_scales"][0], scale, name + "_scales")
+            _same(state[name][0], q, name)
+            held = q.float() * scale.repeat_interleave(256)[:n]
+            m, v = (held, v) if name == "m" else (m, held.square())
+        g = torch.randn(n, generator=gen)
+    assert x[512:768].isfinite().all() and x[4:256].isfinite().all()
