@@ -85,8 +85,6 @@ __device__ __forceinline__ void clear_row(const EmbeddingGradLaunch& L, int64_t 
         for (; at < L.dim; ++at) global(p)[at] = (G)0.0f;
 }
 
-constexpr int kClearRows = 2;           // rows of a wavefront that clears those without a token
-
 // Rows of this size that are cleared while lists are grouped, which leaves the memory idle: about 8 us and 0.6 per 1024 tokens, at 5 TB/s.
 // 16384 tokens, 412 MB: none 99.6 us per call, a quarter of this 99.0, half 96.6, this 93.5 (then 88 with two rows per wavefront)
 static int64_t early_rows(int64_t tokens, int64_t rows, int64_t row_bytes)
@@ -494,7 +492,9 @@ __global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int resu
     const int* keys = L.w.keys[result];
     const int lane = threadIdx.x;
     if (!ACCUMULATE && (int)blockIdx.x >= sum_groups) {
-        clear_absent<GT>(L, keys, group_bits, (int64_t)((int)blockIdx.x - sum_groups) * kClearRows, clear_rows, lane);
+        const int64_t turn = (int64_t)((int)gridDim.x - sum_groups) * kClearRows;
+        for (int64_t r = (int64_t)((int)blockIdx.x - sum_groups) * kClearRows; r < clear_rows; r += turn)
+            clear_absent<GT>(L, keys, group_bits, r, clear_rows, lane);
         return;
     }
     const int slice = blockIdx.x % slices, first = blockIdx.x / slices * kChunk, num = (int)L.t.num;
@@ -794,8 +794,8 @@ static hipError_t grad_of(const EmbeddingGradLaunch& L)
             result = k & 1;
         }
     }
-    const int sums = (int)((num + kChunk - 1) / kChunk) * slices;
-    const dim3 grid((unsigned)(sums + (clear_rows + kClearRows - 1) / kClearRows)), block(64);
+    const int sums = (int)qadam::sum_groups(num, L.dim);
+    const dim3 grid((unsigned)(sums + clear_groups(clear_rows))), block(64);
     if (L.accumulate) hipLaunchKernelGGL((k_sum_runs<DT, GT, N, true>), grid, block, 0, L.stream, L, result, slices, sums, group_bits, clear_rows);
     else hipLaunchKernelGGL((k_sum_runs<DT, GT, N, false>), grid, block, 0, L.stream, L, result, slices, sums, group_bits, clear_rows);
     return hipGetLastError();

@@ -1,0 +1,47 @@
+// How the work of the operators beside the step is divided over launches, and the sizes of their scratch: arithmetic that the host
+// and the kernels share.  Plain C++, so that it can be checked on the CPU at sizes no test allocates.
+#pragma once
+
+#include <stdint.h>
+
+namespace qadam {
+
+constexpr int64_t kMostItems = (int64_t)1 << 32;    // work-items of a launch: fewer
+
+// ---- embedding gradient -------------------------------------------------------------------------
+constexpr int kSortTile = 4096;         // tokens of a workgroup of the sort in passes
+constexpr int kSortBits = 9;            // of a digit, at most
+constexpr int kRunPiece = 40;           // tokens of one row that a wavefront adds at most; longer runs are joined
+constexpr int kChunk = 8;               // tokens whose pieces a wavefront takes
+
+constexpr int kDirectTokens = 2048;     // most tokens of a list that is not sorted
+
+inline int64_t sort_tiles(int64_t tokens) { return (tokens + kSortTile - 1) / kSortTile; }
+// sorted lists have two pieces per block of kRunPiece tokens, others one per token
+inline int64_t arrival_places(int64_t tokens)
+{
+    const int64_t blocks = tokens / kRunPiece + 1, direct = tokens < kDirectTokens ? tokens : kDirectTokens;
+    return blocks > direct ? blocks : direct;
+}
+inline int64_t piece_places(int64_t tokens)
+{
+    const int64_t blocks = 2 * (tokens / kRunPiece + 1), direct = tokens < kDirectTokens ? tokens : kDirectTokens;
+    return blocks > direct ? blocks : direct;
+}
+// a lane's columns: 4, or as few as leave no lane of a narrow matrix idle
+inline int lane_columns(int dim) { return dim > 128 ? 4 : dim > 64 ? 2 : 1; }
+inline int column_slices(int dim) { return (dim + 64 * lane_columns(dim) - 1) / (64 * lane_columns(dim)); }
+
+// The sums of a sorted list: a wavefront per chunk of tokens and slice of columns (a handle's largest list has fewer than kMostSums), and
+// those that look through rows to clear the ones without a token, kClearRows at a time; of more rows than kMostSums of them take at
+// once, each takes several turns.
+constexpr int kClearRows = 2;
+constexpr int64_t kMostSums = (int64_t)1 << 25;
+inline int64_t sum_groups(int64_t tokens, int dim) { return (tokens + kChunk - 1) / kChunk * column_slices(dim); }
+inline int64_t clear_groups(int64_t rows)
+{
+    const int64_t n = (rows + kClearRows - 1) / kClearRows;
+    return n < kMostSums ? n : kMostSums;
+}
+
+}  // namespace qadam

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "qadam_internal.h"
+#include "qadam_operator_work.h"
 
 namespace qadam {
 
@@ -99,14 +100,7 @@ struct LookupLaunch {
 };
 hipError_t launch_embedding_lookup(const LookupLaunch& L);
 
-// Scratch of the gradient, for lists of up to max_tokens (embedding_scratch): the tokens' sorted order, and what joins long runs.
-constexpr int kSortTile = 4096;         // tokens of a workgroup of the sort in passes
-constexpr int kSortBits = 9;            // of a digit, at most
-constexpr int kRunPiece = 40;           // tokens of one row that a wavefront adds at most; longer runs are joined
-constexpr int kChunk = 8;               // tokens whose pieces a wavefront takes
-
-constexpr int kDirectTokens = 2048;     // most tokens of a list that is not sorted
-
+// Scratch of the gradient, for lists of up to max_tokens: the tokens' sorted order, and what joins long runs.
 struct EmbeddingScratch {
     int32_t*  keys[2];      // [max_tokens] rows in ascending order, `rows` for tokens without one
     int32_t*  order[2];     // [max_tokens] their positions in the list
@@ -126,21 +120,5 @@ struct EmbeddingGradLaunch {
     hipStream_t stream;
 };
 hipError_t launch_embedding_grad(const EmbeddingGradLaunch& L);
-
-inline int64_t sort_tiles(int64_t tokens) { return (tokens + kSortTile - 1) / kSortTile; }
-// sorted lists have two pieces per block of kRunPiece tokens, others one per token
-inline int64_t arrival_places(int64_t tokens)
-{
-    const int64_t blocks = tokens / kRunPiece + 1, direct = tokens < kDirectTokens ? tokens : kDirectTokens;
-    return blocks > direct ? blocks : direct;
-}
-inline int64_t piece_places(int64_t tokens)
-{
-    const int64_t blocks = 2 * (tokens / kRunPiece + 1), direct = tokens < kDirectTokens ? tokens : kDirectTokens;
-    return blocks > direct ? blocks : direct;
-}
-// a lane's columns: 4, or as few as leave no lane of a narrow matrix idle
-inline int lane_columns(int dim) { return dim > 128 ? 4 : dim > 64 ? 2 : 1; }
-inline int column_slices(int dim) { return (dim + 64 * lane_columns(dim) - 1) / (64 * lane_columns(dim)); }
 
 }  // namespace qadam

@@ -68,3 +68,18 @@ def test_long_runs(n, kind):
     rows, dim = 211, 6
     tok = torch.arange(n) // 9973 % rows if kind == "runs" else _tokens(kind, n, rows, _gen(n))
     _check(Embedding(rows, dim, n), tok, _integers(n, dim, 0, 0, n, F16), rows, dim, None, kind == "last")
+
+
+@pytest.mark.parametrize("rows", [1 << 28, (1 << 27) + 3])
+def test_as_many_rows_as_a_handle_takes(rows):
+    """Written whole: more rows than wavefronts of a launch."""
+    n = 4099
+    tok = torch.randint(0, rows, (n,), generator=_gen(1))
+    tok[:3] = torch.tensor([0, rows - 1, rows - 1])
+    dout = _integers(n, 1, 0, 0, 5, F32)
+    grad = torch.ones(rows, 1, dtype=BF16, device="cuda")
+    Embedding(rows, 1, n).grad(tok.cuda(), dout, grad)
+    got = grad.view(-1).nonzero()[:, 0]
+    row, place = tok.unique(return_inverse=True)
+    want = torch.zeros(len(row), dtype=torch.int64).index_add_(0, place, dout.cpu().long()[:, 0])
+    assert torch.equal(got.cpu(), row[want != 0]) and torch.equal(grad.view(-1)[got].long().cpu(), want[want != 0])
