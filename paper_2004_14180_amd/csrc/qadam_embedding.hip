@@ -407,22 +407,24 @@ __device__ __forceinline__ void join_piece(const EmbeddingGradLaunch& L, const i
     typedef typename Run<QADAM_F32, N>::F F;
     typedef typename Element<GT>::T G;
     const int num = (int)L.t.num;
-    // the run's blocks are [head, tail]: 64 boundaries between blocks are looked at together
+    // the run's blocks are [head, tail]; `key` holds the boundaries of the first look
+    auto length = [&](int32_t key, auto&& boundary) {
+        for (RunSearch search;;) {
+            const uint64_t other = __ballot(key != row);
+            if (!search.next(other ? __builtin_ctzll(other) : 64)) return search.count;
+            key = boundary(search.place(lane));
+        }
+    };
     int head = block, tail = block;
-    for (int32_t k = front; !is_head;) {
-        const uint64_t other = __ballot(k != row);
-        head -= other ? __builtin_ctzll(other) : 64;
-        if (other) break;
-        const int at = (head - lane) * kRunPiece - 1;
-        k = at < 0 ? -1 : global(keys)[at];
-    }
-    for (int32_t k = behind;;) {
-        const uint64_t other = __ballot(k != row);
-        tail += other ? __builtin_ctzll(other) : 64;
-        if (other) break;
-        const int64_t at = (int64_t)(tail + 1 + lane) * kRunPiece;
-        k = at < num ? global(keys)[at] : -1;
-    }
+    if (!is_head)
+        head -= length(front, [&](int d) {
+            const int at = (block - d) * kRunPiece - 1;
+            return at < 0 ? -1 : global(keys)[at];
+        });
+    tail += length(behind, [&](int d) {
+        const int64_t at = (int64_t)(block + 1 + d) * kRunPiece;
+        return at < num ? global(keys)[at] : -1;
+    });
     float* put = L.w.pieces + (int64_t)(2 * block + is_head) * L.dim + col;
 #pragma unroll
     for (int k = 0; k < N; ++k)

@@ -44,4 +44,28 @@ inline int64_t clear_groups(int64_t rows)
     return n < kMostSums ? n : kMostSums;
 }
 
+// How many boundaries between blocks lie within a run, counted from the nearest one: they are the first of all, so 64 are looked at
+// together, and while all of a look belong to the run the next one is 64 times as wide, then narrower again.
+struct RunSearch {
+    int32_t count = 0, step = 1;
+    bool widen = true;
+
+    // the boundary that a lane looks at
+    constexpr int32_t place(int lane) const { return count + (lane + 1) * step - 1; }
+
+    // `matched` lanes, the first ones, found theirs within the run: whether there is another look
+    constexpr bool next(int matched)
+    {
+        count += matched * step;
+        if (widen && matched == 64) {
+            step *= 64;
+            return true;
+        }
+        widen = false;
+        if (step == 1) return false;
+        step /= 64;
+        return true;
+    }
+};
+
 }  // namespace qadam

@@ -32,3 +32,23 @@ def test_sums_of_a_sorted_list_fit_a_launch(tmp_path):
             }
     CHECK((sum_groups((1 << 24), 512) + clear_groups(1 << 28)) * 64 < kMostItems, "the largest");
     CHECK(clear_groups(0) == 0 && clear_groups(1) == 1 && clear_groups(50257) == 25129, "a wavefront for every two rows");""")
+
+
+def test_the_ends_of_a_run_are_found_in_few_looks(tmp_path):
+    """Boundaries within the run from none to those of 2^24 tokens of one row: found, in one look up to 63 and in seven at most."""
+    _run(tmp_path, """
+    const int most = (1 << 24) / kRunPiece + 1;
+    int worst = 0;
+    for (int count = 0; count <= most; count += count < 300000 && count > 9000 ? 997 : 1) {
+        RunSearch s;
+        int looks = 0;
+        for (bool more = true; more; ++looks) {
+            int matched = 0;
+            while (matched < 64 && s.place(matched) < count) ++matched;
+            for (int lane = matched; lane < 64; ++lane) CHECK(s.place(lane) >= count && (long long)s.place(lane) * kRunPiece < 1ll << 30, "%d", count);
+            more = s.next(matched);
+        }
+        CHECK(s.count == count && (count > 63 || looks == 1), "%d: %d in %d looks", count, s.count, looks);
+        worst = looks > worst ? looks : worst;
+    }
+    CHECK(worst <= 7, "%d looks", worst);""")
