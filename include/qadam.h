@@ -422,8 +422,8 @@ int qadam_embedding_lookup(qadam_embedding_t h, const void* weight, int32_t weig
 
 /* Gradient of the lookup: grad[r] = scale * (sum of dout[t] over the t with tokens[t] = r), for every row r; accumulate = 1: added to
  * what grad[r] holds, and rows without a token are not touched.
- * The tokens are sorted, and each row's sum is taken in fp32 over its dout[t] in an order that depends on the tokens alone: the same
- * bits on every run.
+ * Each row's sum is taken over its dout[t] in an order that depends on the tokens alone, the same bits on every run: in fp32 over
+ * pieces of up to 64 tokens, and over the pieces' sums in fp32 in a short list (up to 2048 tokens) and in fp64 in a long one.
  *   dout        QADAM_F32, QADAM_BF16 or QADAM_F16; dout_stride >= 0 (0: one row for all tokens)
  *   grad        QADAM_F32, QADAM_BF16 or QADAM_F16, rows x dim; grad_stride >= dim: may be the layer's part of a flat gradient vector */
 int qadam_embedding_grad(qadam_embedding_t h, const void* tokens, int32_t token_bytes, int64_t num_tokens, int64_t padding,

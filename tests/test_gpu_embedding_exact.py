@@ -83,3 +83,17 @@ def test_as_many_rows_as_a_handle_takes(rows):
     row, place = tok.unique(return_inverse=True)
     want = torch.zeros(len(row), dtype=torch.int64).index_add_(0, place, dout.cpu().long()[:, 0])
     assert torch.equal(got.cpu(), row[want != 0]) and torch.equal(grad.view(-1)[got].long().cpu(), want[want != 0])
+
+
+@pytest.mark.parametrize("n", [3000, 131_072, (1 << 20) + 3])
+@pytest.mark.parametrize("value", [0.51, 1.1])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_equal_rows_add_up(n, value, accumulate):
+    """One row for every token, all of them of one row: roundings of equal sums, which all go the same way, must not add up.  A piece of
+    up to 64 tokens has 63 roundings; the joined sum, the scale, the product and the addition have one each."""
+    dout = torch.full((1, 5), value, device="cuda")
+    grad = torch.full((3, 5), 2.0, device="cuda")
+    Embedding(3, 5, n).grad(torch.ones(n, dtype=torch.int32, device="cuda"), dout.expand(n, 5), grad, scale=0.3, accumulate=accumulate)
+    want = n * float(dout[0, 0]) * 0.3 + (2.0 if accumulate else 0.0)
+    assert ((grad[1].double() - want).abs() <= 67 * 2.0 ** -24 * want).all()
+    assert (grad[[0, 2]] == (2.0 if accumulate else 0.0)).all()
