@@ -4,8 +4,8 @@
 // the sum of the dout of its tokens, so whoever adds must know them: atomics from every token would write each row as often as it
 // occurs and in no fixed order, while a list of positions sorted by row lets every row be written once, from registers, and makes
 // the result the same bits on every run.  Three ways, by sizes alone, us per call (second and third: in all of their launches):
-//   * up to 2048 tokens, one launch that needs no sort: each token looks for its row in the list (k_sum_direct).  1024 tokens of 768
-//     fp32, added to the matrix: 5.6 (sorted: 12);
+//   * up to 2048 tokens, fewer beyond 1024 columns (direct_tokens), one launch that needs no sort: each token looks for its row in the
+//     list (k_sum_direct).  1024 tokens of 768 fp32, added to the matrix: 5.6 (sorted: 12);
 //   * up to 131072 tokens and 524 k rows, the sort is one launch (k_group) and the sums another (k_sum_runs).  16384 tokens of 2048
 //     bf16 and a matrix of 50257 rows written whole, 479 MB: 90;
 //   * beyond, the sort takes two launches per digit of up to 9 bits (140 k tokens: 54 for 17 bits of rows).
@@ -572,11 +572,8 @@ __global__ void __launch_bounds__(64) k_sum_runs(EmbeddingGradLaunch L, int resu
 // where its token is the first of its row adds the dout of all of them, a wavefront per slice; of more than kBatch tokens the
 // wavefronts that a slice has take a part each.  A row of more than kDirectPiece tokens is added by the workgroups of every
 // kDirectPiece-th of them, and the last one adds their sums.  Further workgroups clear the rows without a token.
-constexpr int kDirectWaves = 8, kDirectPart = kDirectTokens / kDirectWaves;
+constexpr int kDirectPart = kDirectTokens / kDirectWaves;
 constexpr int kDirectPiece = 64;        // us, 2048 tokens of 768 bf16, half of them / all of one row: by one workgroup 63 / 121, now 16 / 24
-constexpr int kDirectGroups = 2048;     // most workgroups that look through the list: us with more of them / sorted, added: 1500 tokens
-                                        // of 2048 bf16 15.2 / 14.0, 1024 10.4 / 12.2; 2000 of 768 fp32 (below) 10.0 / 14.4
-constexpr int kDirectClear = 8;         // rows of a wavefront that clears, which reads the whole list for them
 
 template <bool WIDE, int GT>
 __device__ __forceinline__ void clear_absent_direct(const EmbeddingGradLaunch& L, int64_t first, int lane)
@@ -760,16 +757,14 @@ static hipError_t grad_of(const EmbeddingGradLaunch& L)
     const int64_t num = L.t.num;
     const int slices = column_slices(L.dim);
     int64_t clear_rows = L.accumulate ? 0 : L.t.rows;       // of the gradient, the first ones: if they have no token
-    const int log_group_slices = slices > 2 ? 2 : slices - 1, groups_per_token = (slices + (1 << log_group_slices) - 1) >> log_group_slices;
-    if (num <= kDirectTokens && num * groups_per_token <= kDirectGroups) {
-        const int64_t clear = (clear_rows + kDirectClear - 1) / kDirectClear;       // wavefronts
-        const int sums = (int)num * groups_per_token;
-        const dim3 grid((unsigned)(sums + (clear + kDirectWaves - 1) / kDirectWaves)), block(64 * kDirectWaves);
+    if (num <= direct_tokens(L.dim)) {
+        const int log_slices = log_group_slices(L.dim), groups = groups_per_token(L.dim), sums = (int)num * groups;
+        const dim3 grid((unsigned)(sums + direct_clear_groups(clear_rows))), block(64 * kDirectWaves);
         if (grid.x == 0) return hipSuccess;
         if (L.t.bytes == 8)
-            hipLaunchKernelGGL((k_sum_direct<true, DT, GT, N>), grid, block, 0, L.stream, L, slices, log_group_slices, groups_per_token, sums);
+            hipLaunchKernelGGL((k_sum_direct<true, DT, GT, N>), grid, block, 0, L.stream, L, slices, log_slices, groups, sums);
         else
-            hipLaunchKernelGGL((k_sum_direct<false, DT, GT, N>), grid, block, 0, L.stream, L, slices, log_group_slices, groups_per_token, sums);
+            hipLaunchKernelGGL((k_sum_direct<false, DT, GT, N>), grid, block, 0, L.stream, L, slices, log_slices, groups, sums);
         return hipGetLastError();
     }
     const int row_bits = bits_of((uint64_t)L.t.rows), bits = bits_of((uint64_t)num);

@@ -14,23 +14,39 @@ constexpr int kSortBits = 9;            // of a digit, at most
 constexpr int kRunPiece = 40;           // tokens of one row that a wavefront adds at most; longer runs are joined
 constexpr int kChunk = 8;               // tokens whose pieces a wavefront takes
 
-constexpr int kDirectTokens = 2048;     // most tokens of a list that is not sorted
-
-inline int64_t sort_tiles(int64_t tokens) { return (tokens + kSortTile - 1) / kSortTile; }
-// sorted lists have two pieces per block of kRunPiece tokens, others one per token
-inline int64_t arrival_places(int64_t tokens)
-{
-    const int64_t blocks = tokens / kRunPiece + 1, direct = tokens < kDirectTokens ? tokens : kDirectTokens;
-    return blocks > direct ? blocks : direct;
-}
-inline int64_t piece_places(int64_t tokens)
-{
-    const int64_t blocks = 2 * (tokens / kRunPiece + 1), direct = tokens < kDirectTokens ? tokens : kDirectTokens;
-    return blocks > direct ? blocks : direct;
-}
 // a lane's columns: 4, or as few as leave no lane of a narrow matrix idle
 inline int lane_columns(int dim) { return dim > 128 ? 4 : dim > 64 ? 2 : 1; }
 inline int column_slices(int dim) { return (dim + 64 * lane_columns(dim) - 1) / (64 * lane_columns(dim)); }
+
+// Lists that are not sorted: up to kDirectTokens tokens, and kDirectGroups workgroups of up to four slices of a token's columns.
+constexpr int kDirectTokens = 2048;
+constexpr int kDirectGroups = 2048;     // which all look through the list: us with more of them / sorted, added: 1500 tokens of 2048 bf16
+                                        // 15.2 / 14.0, 1024 10.4 / 12.2; 2000 of 768 fp32 (below) 10.0 / 14.4
+constexpr int kDirectWaves = 8;         // of a workgroup
+constexpr int kDirectClear = 8;         // rows of a wavefront that clears, which reads the whole list for them
+inline int log_group_slices(int dim)
+{
+    const int slices = column_slices(dim);
+    return slices > 2 ? 2 : slices - 1;
+}
+inline int groups_per_token(int dim) { return (column_slices(dim) + (1 << log_group_slices(dim)) - 1) >> log_group_slices(dim); }
+// the most tokens of a list that is not sorted: 2048 up to 1024 columns, 1024 up to 2048, 512 up to 4096
+inline int64_t direct_tokens(int dim)
+{
+    const int64_t n = kDirectGroups / groups_per_token(dim);
+    return n < kDirectTokens ? n : kDirectTokens;
+}
+inline int64_t direct_clear_groups(int64_t rows) { return (rows + kDirectWaves * kDirectClear - 1) / (kDirectWaves * kDirectClear); }
+
+// Scratch: sorted lists have two pieces per block of kRunPiece tokens and one count of arrivals, others one of each per token.
+inline int64_t sort_tiles(int64_t tokens) { return (tokens + kSortTile - 1) / kSortTile; }
+inline int64_t places(int64_t tokens, int dim, int64_t per_block)
+{
+    const int64_t most = direct_tokens(dim), blocks = per_block * (tokens / kRunPiece + 1), direct = tokens < most ? tokens : most;
+    return blocks > direct ? blocks : direct;
+}
+inline int64_t arrival_places(int64_t tokens, int dim) { return places(tokens, dim, 1); }
+inline int64_t piece_places(int64_t tokens, int dim) { return places(tokens, dim, 2); }
 
 // The sums of a sorted list: a wavefront per chunk of tokens and slice of columns (a handle's largest list has fewer than kMostSums), and
 // those that look through rows to clear the ones without a token, kClearRows at a time; of more rows than kMostSums of them take at

@@ -311,11 +311,11 @@ int qadam_embedding_init(qadam_embedding_t* out, int64_t rows, int32_t dim, int6
         QADAM_HIP(hipGetDevice(&h->device));
         QADAM_CHECK(allocate(h->status, 1));
         QADAM_HIP(hipMemset(h->status.get(), 0, sizeof(uint32_t)));
-        const size_t n = (size_t)max_tokens, arrivals = (size_t)arrival_places(max_tokens) * (size_t)column_slices(dim);
+        const size_t n = (size_t)max_tokens, arrivals = (size_t)arrival_places(max_tokens, dim) * (size_t)column_slices(dim);
         if (n > 0) {
             QADAM_CHECK(allocate(h->sorted, 4 * n));
             QADAM_CHECK(allocate(h->counts, (size_t)sort_tiles(max_tokens) << kSortBits));
-            QADAM_CHECK(allocate(h->pieces, (size_t)piece_places(max_tokens) * (size_t)dim));
+            QADAM_CHECK(allocate(h->pieces, (size_t)piece_places(max_tokens, dim) * (size_t)dim));
             QADAM_CHECK(allocate(h->arrived, arrivals));
             QADAM_HIP(hipMemset(h->arrived.get(), 0, arrivals * sizeof(uint32_t)));
         }

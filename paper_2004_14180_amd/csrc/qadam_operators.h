@@ -105,8 +105,8 @@ struct EmbeddingScratch {
     int32_t*  keys[2];      // [max_tokens] rows in ascending order, `rows` for tokens without one
     int32_t*  order[2];     // [max_tokens] their positions in the list
     uint32_t* counts;       // [tiles][1 << kSortBits]
-    float*    pieces;       // [piece_places(max_tokens)][dim]
-    uint32_t* arrived;      // [arrival_places(max_tokens)][slices of columns], zero between launches
+    float*    pieces;       // [piece_places(max_tokens, dim)][dim]
+    uint32_t* arrived;      // [arrival_places(max_tokens, dim)][slices of columns], zero between launches
 };
 
 struct EmbeddingGradLaunch {

@@ -52,3 +52,26 @@ def test_the_ends_of_a_run_are_found_in_few_looks(tmp_path):
         worst = looks > worst ? looks : worst;
     }
     CHECK(worst <= 7, "%d looks", worst);""")
+
+
+def test_scratch_of_the_gradient(tmp_path):
+    """Every piece and every arrival has its place, whichever way the list's length takes, and none is reserved for a way that no list takes."""
+    _run(tmp_path, """
+    for (long long dim = 1; dim <= 1 << 20; dim = dim < 10000 ? dim + 1 : dim + dim / 7) {
+        const int d = (int)dim, slices = column_slices(d), groups = groups_per_token(d);
+        CHECK(slices * 64 * lane_columns(d) >= d && (slices - 1) * 64 * lane_columns(d) < d && d >= lane_columns(d), "dim %d", d);
+        CHECK((groups << log_group_slices(d)) >= slices && ((groups - 1) << log_group_slices(d)) < slices && kDirectWaves >> log_group_slices(d), "dim %d", d);
+        const long long direct = direct_tokens(d);
+        CHECK(direct >= 1 && direct <= kDirectTokens && direct * groups <= kDirectGroups, "dim %d", d);
+        CHECK(direct == kDirectTokens || (direct + 1) * groups > kDirectGroups, "dim %d", d);
+        CHECK((direct * groups + direct_clear_groups(1 << 28)) * 64 * kDirectWaves < kMostItems, "dim %d", d);
+        for (long long most : {1ll, 2ll, 39ll, 40ll, 41ll, 500ll, 512ll, 1023ll, 1024ll, 2047ll, 2048ll, 2049ll, 50000ll, 1ll << 24}) {
+            const long long pieces = piece_places(most, d), arrivals = arrival_places(most, d);
+            const long long shorter = most < direct ? most : direct, last = (most - 1) / kRunPiece;
+            CHECK(pieces >= shorter && arrivals >= shorter, "dim %d, %lld tokens", d, most);
+            CHECK(pieces >= 2 * last + 2 && arrivals >= last + 1, "dim %d, %lld tokens", d, most);
+            CHECK(4 * pieces * dim <= (most * dim) / 5 + 8 * dim + (8 << 20), "dim %d, %lld tokens", d, most);
+        }
+    }
+    CHECK(direct_tokens(768) == 2048 && direct_tokens(1024) == 2048 && direct_tokens(1025) == 1024 && direct_tokens(2048) == 1024 &&
+          direct_tokens(4096) == 512, "the lengths that the comments name");""")
