@@ -401,8 +401,9 @@ int qadam_grad_norm_init(qadam_grad_norm_t* out, const int64_t* numels, const in
 int qadam_grad_norm_destroy(qadam_grad_norm_t h);
 int qadam_grad_norm(qadam_grad_norm_t h, const void* const* grads, float max_norm, float* out_dev, void* stream);
 
-/* Embedding: a matrix of `rows` rows of `dim` elements, looked up by tokens.  max_tokens (at most 2^24) bounds num_tokens of
- * qadam_embedding_grad, whose scratch the handle allocates: about max_tokens (16 + dim / 5) bytes, and up to 8 MB for short lists.
+/* Embedding: a matrix of `rows` (up to 2^28) rows of `dim` (up to 2^20) elements, looked up by tokens.  max_tokens (up to 2^24, and
+ * max_tokens / 8 times ceil(dim / 256) below 2^25) bounds num_tokens of qadam_embedding_grad, whose scratch the handle allocates:
+ * about max_tokens (16 + dim / 5) bytes, and up to 8 MB for short lists.
  * Tokens are int32 or int64 (token_bytes 4 or 8).  `padding`: the row of a token that stands for no text, or a number outside
  * 0..rows-1 for none.  A token outside 0..rows-1 sets QADAM_STATUS_TOKEN_RANGE in the handle's status word.  Both kinds look up zeros
  * and have no gradient.  Strides: elements from one row to the next. */

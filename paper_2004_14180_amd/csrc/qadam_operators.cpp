@@ -303,8 +303,9 @@ int qadam_embedding_init(qadam_embedding_t* out, int64_t rows, int32_t dim, int6
     if (rows > (int64_t)1 << 28) return fail(QADAM_ERANGE, "more than 2^28 rows");
     if (max_tokens > (int64_t)1 << 24) return fail(QADAM_ERANGE, "more than 2^24 tokens");
     if (dim > 1 << 20) return fail(QADAM_ERANGE, "more than 2^20 columns");
+    static_assert(kChunk == 8 && kMostSums == 1 << 25, "the text below");
     if (sum_groups(max_tokens, dim) >= kMostSums)
-        return fail(QADAM_ERANGE, "too many wavefronts for one launch (max_tokens * dim / 4096 must stay below 2^25)");
+        return fail(QADAM_ERANGE, "too many wavefronts for one launch (max_tokens / 8 times the slices of 256 columns must stay below 2^25)");
     return guarded([&]() -> int {
         std::unique_ptr<qadam_embedding_ctx> h(new qadam_embedding_ctx);
         h->rows = rows; h->dim = dim; h->max_tokens = max_tokens;

@@ -119,6 +119,14 @@ def test_native_calls_leave_other_forms_to_the_python_checks(lib):
         native.adamw_step(emb, 0, 0, 1, 1e-3, [t], None)               # another plan
 
 
+def test_the_rule_that_a_refusal_states_is_the_one_that_it_follows(lib):
+    h = C.c_void_p()
+    for rows, dim, tokens in [(1, 4096, 1 << 24), (1, 8000, 1 << 24), (1, 1 << 20, 1 << 16)]:
+        assert tokens // 8 * -(-dim // 256) >= 1 << 25
+        assert lib.qadam_embedding_init(C.byref(h), rows, dim, tokens) == -3
+        assert b"max_tokens / 8 times the slices of 256 columns must stay below 2^25" in lib.qadam_last_error()
+
+
 @pytest.mark.parametrize("source", SOURCES)
 def test_the_kernels_keep_out_of_scratch_and_hold_no_packed_fp32(source):
     from paper_2004_14180_amd.build import device_assembly, device_resource_usage
