@@ -369,7 +369,7 @@ typedef struct {
 /* One tensor.  The buffers stay the caller's; their addresses are read at qadam_adamw_init and the handle steps these buffers from then
  * on, so they live as long as it does. */
 typedef struct {
-    int64_t numel;          /* >= 0 */
+    int64_t numel;          /* 0 to 2^34 - 8192; up to 2^38 in all of a list */
     void*   param;          /* x: QADAM_F32, QADAM_BF16 or QADAM_F16; without fp32 weights an update below half a unit of x's last
                                place is lost */
     void*   m;              /* fp32, or one byte per element */
@@ -395,7 +395,7 @@ int qadam_adamw_step(qadam_adamw_t h, int64_t step, float lr, const void* const*
  *     out[0] = n = sqrt(sum of all squares),   out[1] = n > max_norm ? max_norm / n : 1;  NaN if n is not finite.
  * out_dev: two fp32 on the device.  Squares and sums in fp64 and in a fixed order: the same bits on every run, and no overflow (n itself
  * may be beyond fp32: out[0] is then infinite, out[1] is not).  grads: as in qadam_adamw_step; NULL counts as zeros.  max_norm >= 0;
- * infinite: the norm alone.  May be recorded into a graph. */
+ * infinite: the norm alone.  numels: as in qadam_adamw_tensor_t.  May be recorded into a graph. */
 typedef struct qadam_grad_norm_ctx* qadam_grad_norm_t;
 int qadam_grad_norm_init(qadam_grad_norm_t* out, const int64_t* numels, const int32_t* grad_types, int32_t num_tensors);
 int qadam_grad_norm_destroy(qadam_grad_norm_t h);

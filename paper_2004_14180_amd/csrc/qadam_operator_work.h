@@ -8,6 +8,19 @@ namespace qadam {
 
 constexpr int64_t kMostItems = (int64_t)1 << 32;    // work-items of a launch: fewer
 
+// ---- lists of tensors ---------------------------------------------------------------------------
+constexpr int kListTile = 4096;         // elements of one tensor that a record of the list's table stands for
+constexpr int kListGrads = 448;         // gradients' addresses of one launch: they travel as kernel arguments (4 KB in all)
+constexpr int kTileBlocks = kListTile / 256;        // wavefronts of AdamW per record
+
+// A launch takes the next tensors of the list, as many as their gradients' addresses and their wavefronts allow.
+constexpr int64_t kMostLaunchTiles = kMostItems / (64 * kTileBlocks) - 1;
+constexpr int64_t kMostListTiles = (int64_t)1 << 26;        // 2^38 elements, more than the memory holds in any type
+constexpr bool list_launch_takes(int64_t tensors, int64_t tiles, int64_t next)
+{
+    return tensors < kListGrads && tiles + next <= kMostLaunchTiles;
+}
+
 // ---- embedding gradient -------------------------------------------------------------------------
 constexpr int kSortTile = 4096;         // tokens of a workgroup of the sort in passes
 constexpr int kSortBits = 9;            // of a digit, at most

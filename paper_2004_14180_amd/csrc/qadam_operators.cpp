@@ -75,7 +75,7 @@ int upload(DeviceArray<T>& out, const std::vector<T>& host)
     return QADAM_OK;
 }
 
-// A list's tensors and tiles on the device, and its launches: kListGrads tensors each.
+// A list's tensors and tiles on the device, and its launches.
 struct List {
     struct Part {
         int32_t first_tensor, num_tensors, first_tile, num_tiles;
@@ -95,14 +95,18 @@ struct List {
     int build(const std::vector<ListTensor>& host)
     {
         int64_t count = 0;
-        for (const ListTensor& t : host) count += tiles_of(t);
-        // a launch has a wavefront per block of 256 elements, 16 per tile
-        if (count >= ((int64_t)1 << 32) / (64 * 16)) return fail(QADAM_ERANGE, "too many tiles for one launch (elements / 4096 must stay below 2^22)");
+        for (const ListTensor& t : host) {
+            static_assert(kMostLaunchTiles == (1 << 22) - 1 && kMostListTiles == 1 << 26 && kListTile == 4096, "the texts below");
+            if (tiles_of(t) > kMostLaunchTiles) return fail(QADAM_ERANGE, "a tensor too large for one launch (elements / 4096 must stay below 2^22)");
+            count += tiles_of(t);
+            if (count > kMostListTiles) return fail(QADAM_ERANGE, "more than 2^38 elements in all");
+        }
         std::vector<ListTile> all;
         all.reserve((size_t)count);
         for (size_t i = 0; i < host.size(); ++i) {
-            if (i % kListGrads == 0) parts.push_back({(int32_t)i, 0, (int32_t)all.size(), 0});
             const int32_t n = (int32_t)tiles_of(host[i]);
+            if (parts.empty() || !list_launch_takes(parts.back().num_tensors, parts.back().num_tiles, n))
+                parts.push_back({(int32_t)i, 0, (int32_t)all.size(), 0});
             for (int32_t k = 0; k < n; ++k) {
                 const int64_t left = host[i].numel - (int64_t)k * kListTile;
                 all.push_back({(int32_t)i, k, (int32_t)(left < kListTile ? left : kListTile), host[i].types >> 2 & 3});

@@ -11,9 +11,6 @@
 namespace qadam {
 
 // ---- lists of tensors ---------------------------------------------------------------------------
-constexpr int kListTile = 4096;         // elements of one tensor that a record of the list's table stands for
-constexpr int kListGrads = 448;         // gradients' addresses of one launch: they travel as kernel arguments (4 KB in all)
-
 struct ListTile {
     int32_t tensor;         // of the list
     int32_t tile;           // of the tensor
@@ -55,7 +52,7 @@ struct AdamwScalars {
     float lr, lr1, inv_sbc2, eps;       // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
 };
 
-// tiles [first_tile, first_tile + num_tiles) of the list, whose tensors are [first_tensor, first_tensor + kListGrads)
+// tiles [first_tile, first_tile + num_tiles) of the list, whose tensors are at most kListGrads from first_tensor on
 struct ListLaunch {
     const ListTile*   tiles;
     const ListTensor* tensors;

@@ -21,8 +21,8 @@ namespace {
 
 constexpr int kWave = 64;
 constexpr int kBlock = QADAM_STATE_BLOCK;       // a wavefront's 64 lanes of 4 elements
-constexpr int kBlocksPerTile = kListTile / kBlock;
-static_assert(kBlock == 4 * kWave, "");
+constexpr int kBlocksPerTile = kTileBlocks;
+static_assert(kBlock == 4 * kWave && kBlocksPerTile * kBlock == kListTile, "");
 
 constexpr float kFp8Max = 448.0f, kFp8Unit = 1.0f / 448.0f, kFp8Least = 0x1p-9f, kTinyBlock = 0x1p-116f;
 

@@ -119,6 +119,21 @@ def test_native_calls_leave_other_forms_to_the_python_checks(lib):
         native.adamw_step(emb, 0, 0, 1, 1e-3, [t], None)               # another plan
 
 
+def test_a_list_may_be_larger_than_a_launch(lib):
+    """17 tensors of 2^30 elements are not refused for their sum: without a GPU the first call of the runtime is what fails."""
+    h = C.c_void_p()
+
+    def init(numels):
+        return lib.qadam_grad_norm_init(C.byref(h), (C.c_int64 * len(numels))(*numels), (C.c_int32 * len(numels))(*[1] * len(numels)), len(numels))
+
+    rc = init([1 << 30] * 17)
+    assert rc == (0 if torch.cuda.is_available() else -4)
+    if rc == 0:
+        lib.qadam_grad_norm_destroy(h)
+    assert init([5, (1 << 34) - 4095]) == -3 and b"2^22" in lib.qadam_last_error()
+    assert init([1 << 33] * 33) == -3 and b"2^38" in lib.qadam_last_error()
+
+
 def test_the_rule_that_a_refusal_states_is_the_one_that_it_follows(lib):
     h = C.c_void_p()
     for rows, dim, tokens in [(1, 4096, 1 << 24), (1, 8000, 1 << 24), (1, 1 << 20, 1 << 16)]:

@@ -75,3 +75,15 @@ def test_scratch_of_the_gradient(tmp_path):
     }
     CHECK(direct_tokens(768) == 2048 && direct_tokens(1024) == 2048 && direct_tokens(1025) == 1024 && direct_tokens(2048) == 1024 &&
           direct_tokens(4096) == 512, "the lengths that the comments name");""")
+
+
+def test_launches_of_a_list_fit(tmp_path):
+    """Whatever the tensors' sizes: fewer than 2^32 work-items of AdamW per launch, and its gradients' addresses fit."""
+    _run(tmp_path, """
+    CHECK(kMostLaunchTiles * kTileBlocks * 64 < kMostItems && (kMostLaunchTiles + 1) * kTileBlocks * 64 == kMostItems, "the most");
+    for (long long tiles : {0ll, 1ll, 1000ll, 9362ll, 9363ll, 1ll << 18, (1ll << 22) - 1}) {
+        long long tensors = 0, sum = 0;
+        while (list_launch_takes(tensors, sum, tiles)) { ++tensors; sum += tiles; }
+        CHECK(tensors >= 1 && tensors <= kListGrads && sum * kTileBlocks * 64 < kMostItems, "%lld tiles", tiles);
+        CHECK(tensors == kListGrads || sum + tiles > kMostLaunchTiles, "%lld tiles: %lld tensors", tiles, tensors);
+    }""")
