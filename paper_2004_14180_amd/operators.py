@@ -62,6 +62,13 @@ def _rows(t, name, rows, dim):
     return dim if step is None else step
 
 
+def _integer(value, name, bits=64):
+    """`value` where the boundary takes an integer of so many bits: ctypes drops what lies above them."""
+    if not -(1 << (bits - 1)) <= value < 1 << (bits - 1):
+        raise ValueError("%s: %d does not fit %d bits" % (name, value, bits))
+    return value
+
+
 class _Handle:
     """Owner of one handle of the library."""
     _destroy = None
@@ -170,7 +177,7 @@ class AdamW(_TensorList):
                     raise ValueError("copies[%d]: expected bfloat16 or float16" % i)
                 r.copy, r.copy_type = _list_tensor(copies[i], "copies[%d]" % i, copies[i].dtype, r.numel), types[copies[i].dtype]
             r.weight_decay = decays[i]
-        c = _AdamWConfig(C.sizeof(_AdamWConfig), cfg.state_bits, cfg.beta1, cfg.beta2, cfg.eps)
+        c = _AdamWConfig(C.sizeof(_AdamWConfig), _integer(cfg.state_bits, "state_bits", 32), cfg.beta1, cfg.beta2, cfg.eps)
         h = C.c_void_p()
         self._check(self._lib.qadam_adamw_init(C.byref(h), C.byref(c), table, n))
         self._h = h
@@ -183,7 +190,7 @@ class AdamW(_TensorList):
         if rc is not None:
             return self._check(rc)
         factor = None if grad_scale is None else _list_tensor(grad_scale, "grad_scale", _F32(), 1)
-        self._check(self._lib.qadam_adamw_step(self._h, step, lr, self._grads(grads), factor, _stream(stream)))
+        self._check(self._lib.qadam_adamw_step(self._h, _integer(step, "step"), lr, self._grads(grads), factor, _stream(stream)))
 
 
 def _F32():
@@ -198,7 +205,7 @@ class GradNorm(_TensorList):
     def __init__(self, numels: Sequence[int], grad_dtype=None):
         super().__init__()
         types = _types()
-        numels = [int(n) for n in numels]
+        numels = [_integer(int(n), "numels") for n in numels]
         dtypes = _per_tensor(_F32() if grad_dtype is None else grad_dtype, len(numels), "grad_dtype")
         for t in dtypes:
             if t not in types:
@@ -218,6 +225,10 @@ class GradNorm(_TensorList):
         self._check(self._lib.qadam_grad_norm(self._h, self._grads(grads), max_norm, _list_tensor(out, "out", _F32(), 2), _stream(stream)))
 
 
+def _padding(index):
+    return -1 if index is None else _integer(index, "padding_idx")
+
+
 class Embedding(_Handle):
     """A matrix of `rows` rows of `dim` elements, looked up by tokens, and its gradient (qadam_embedding_*).  `max_tokens`: the most
     tokens of one gradient."""
@@ -225,7 +236,7 @@ class Embedding(_Handle):
 
     def __init__(self, rows: int, dim: int, max_tokens: int):
         super().__init__()
-        self.rows, self.dim, self.max_tokens = int(rows), int(dim), int(max_tokens)
+        self.rows, self.dim, self.max_tokens = _integer(int(rows), "rows"), _integer(int(dim), "dim", 32), _integer(int(max_tokens), "max_tokens")
         h = C.c_void_p()
         self._check(self._lib.qadam_embedding_init(C.byref(h), self.rows, self.dim, self.max_tokens))
         self._h = h
@@ -263,7 +274,7 @@ class Embedding(_Handle):
             raise ValueError("out: expected float32, bfloat16 or float16, got %s" % out.dtype)
         os = _rows(out, "out", n, self.dim)
         self._check(self._lib.qadam_embedding_lookup(
-            self._h, weight.data_ptr(), wt, 0 if k_x is None else k_x, ws, at, size, n, -1 if padding_idx is None else padding_idx, scale,
+            self._h, weight.data_ptr(), wt, 0 if k_x is None else _integer(k_x, "k_x", 32), ws, at, size, n, _padding(padding_idx), scale,
             out.data_ptr(), types[out.dtype], os, _stream(stream)))
 
     def grad(self, tokens, dout, grad, scale: float = 1.0, padding_idx: Optional[int] = None, accumulate: bool = False, stream=None):
@@ -278,7 +289,7 @@ class Embedding(_Handle):
             raise ValueError("dout, grad: expected float32, bfloat16 or float16")
         ds, gs = _rows(dout, "dout", n, self.dim), _rows(grad, "grad", self.rows, self.dim)
         self._check(self._lib.qadam_embedding_grad(
-            self._h, at, size, n, -1 if padding_idx is None else padding_idx, scale, dout.data_ptr(), types[dout.dtype], ds,
+            self._h, at, size, n, _padding(padding_idx), scale, dout.data_ptr(), types[dout.dtype], ds,
             grad.data_ptr(), types[grad.dtype], gs, int(accumulate), _stream(stream)))
 
     def get_status(self, clear=False, stream=None) -> int:

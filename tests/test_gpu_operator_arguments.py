@@ -1,0 +1,29 @@
+"""Arguments that the operators' calls refuse, whichever checks a call goes through, and what they take alike."""
+import pytest
+import torch
+
+from paper_2004_14180_amd import AdamW, AdamWConfig, Embedding, GradNorm, adamw_state, binding
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(params=["native checks", "checks in Python"])
+def ways(request, monkeypatch):
+    binding.load_library()
+    if request.param == "checks in Python":
+        monkeypatch.setattr(binding, "_native", binding._Unavailable())
+
+
+def test_integers_beyond_the_boundary_types(ways):
+    codes, tok = torch.ones(4, 8, dtype=torch.int8, device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda")
+    out, grad = torch.full((3, 8), 7.0, device="cuda"), torch.full((4, 8), 7.0, device="cuda")
+    emb = Embedding(4, 8, 3)
+    for kw in (dict(k_x=(1 << 32) + 3), dict(k_x=3, padding_idx=1 << 64), dict(k_x=-(1 << 32))):
+        with pytest.raises(ValueError, match="does not fit"):
+            emb.lookup(codes, tok, out, **kw)
+    with pytest.raises(ValueError, match="does not fit"):
+        emb.grad(tok, out, grad, padding_idx=(1 << 64) + 2)
+    params, cfg = [torch.ones(5, device="cuda")], AdamWConfig()
+    with pytest.raises(ValueError, match="does not fit"):
+        AdamW(cfg, params, **adamw_state(cfg, params)).step((1 << 64) + 1, 1e-3, [torch.ones(5, device="cuda")])
+    assert (out == 7).all() and (grad == 7).all() and (params[0] == 1).all()

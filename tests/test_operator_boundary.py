@@ -69,6 +69,21 @@ def test_tensors_that_are_not_on_the_device_are_refused(lib):
             AdamW(cfg, p, **adamw_state(cfg, p))
 
 
+def test_integers_beyond_the_boundary_types_are_refused(lib):
+    """ctypes would drop their upper bits: dim = 2^32 + 4 would be a handle of 4 columns."""
+    from paper_2004_14180_amd import AdamW, AdamWConfig, Embedding, GradNorm
+    from paper_2004_14180_amd.operators import _integer
+    for v, bits in [(0, 32), (-(1 << 31), 32), ((1 << 31) - 1, 32), ((1 << 63) - 1, 64), (-(1 << 63), 64)]:
+        assert _integer(v, "v", bits) == v
+    for v, bits in [(1 << 31, 32), ((1 << 32) + 3, 32), (-(1 << 31) - 1, 32), (1 << 63, 64), ((1 << 64) + 1, 64)]:
+        with pytest.raises(ValueError, match="does not fit"):
+            _integer(v, "v", bits)
+    for make in (lambda: Embedding(10, (1 << 32) + 4, 8), lambda: Embedding((1 << 64) + 10, 4, 8), lambda: Embedding(10, 4, (1 << 64) + 8),
+                 lambda: GradNorm([(1 << 64) + 4]), lambda: AdamW(AdamWConfig(state_bits=(1 << 32) + 32), [], [], [])):
+        with pytest.raises(ValueError, match="does not fit"):
+            make()
+
+
 def test_rows_of_a_matrix():
     """The layouts that stand for rows at one distance, on tensors that pass the check of the device."""
     from paper_2004_14180_amd import operators
