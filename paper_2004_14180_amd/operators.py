@@ -290,7 +290,7 @@ class Embedding(_Handle):
         ds, gs = _rows(dout, "dout", n, self.dim), _rows(grad, "grad", self.rows, self.dim)
         self._check(self._lib.qadam_embedding_grad(
             self._h, at, size, n, _padding(padding_idx), scale, dout.data_ptr(), types[dout.dtype], ds,
-            grad.data_ptr(), types[grad.dtype], gs, int(accumulate), _stream(stream)))
+            grad.data_ptr(), types[grad.dtype], gs, int(bool(accumulate)), _stream(stream)))
 
     def get_status(self, clear=False, stream=None) -> int:
         st = _Status()

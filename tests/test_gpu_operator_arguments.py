@@ -27,3 +27,11 @@ def test_integers_beyond_the_boundary_types(ways):
     with pytest.raises(ValueError, match="does not fit"):
         AdamW(cfg, params, **adamw_state(cfg, params)).step((1 << 64) + 1, 1e-3, [torch.ones(5, device="cuda")])
     assert (out == 7).all() and (grad == 7).all() and (params[0] == 1).all()
+
+
+@pytest.mark.parametrize("accumulate", [True, 1, 2, -1, "yes", [0], False, 0, None, []])
+def test_accumulate_is_a_truth_value(ways, accumulate):
+    tok, dout, grad = torch.zeros(3, dtype=torch.int64, device="cuda"), torch.ones(3, 8, device="cuda"), torch.full((4, 8), 2.0, device="cuda")
+    Embedding(4, 8, 3).grad(tok, dout, grad, accumulate=accumulate)
+    before = 2.0 if accumulate else 0.0
+    assert (grad[0] == 3.0 + before).all() and (grad[1:] == before).all()
