@@ -164,6 +164,7 @@ class AdamW(_TensorList):
         table = (_AdamWTensor * max(1, n))()
         for i, p in enumerate(params):
             r = table[i]
+            _on_device(p, "params[%d]" % i)
             if p.dtype not in types or dtypes[i] not in types:
                 raise ValueError("params[%d], grad_dtype: expected float32, bfloat16 or float16" % i)
             r.numel = p.numel()
@@ -173,6 +174,7 @@ class AdamW(_TensorList):
                 setattr(r, name, _list_tensor(ts[i], "%s[%d]" % (name, i), torch.float8_e4m3fn if state8 and not scales else torch.float32,
                                               -(-r.numel // QADAM_STATE_BLOCK) if scales else r.numel))
             if copies[i] is not None:
+                _on_device(copies[i], "copies[%d]" % i)
                 if copies[i].dtype not in types:
                     raise ValueError("copies[%d]: expected bfloat16 or float16" % i)
                 r.copy, r.copy_type = _list_tensor(copies[i], "copies[%d]" % i, copies[i].dtype, r.numel), types[copies[i].dtype]
@@ -270,9 +272,9 @@ class Embedding(_Handle):
             raise ValueError("weight: expected float32, bfloat16, float16, or codes with k_x, got %s" % weight.dtype)
         else:
             wt = types[weight.dtype]
+        os = _rows(out, "out", n, self.dim)
         if out.dtype not in types:
             raise ValueError("out: expected float32, bfloat16 or float16, got %s" % out.dtype)
-        os = _rows(out, "out", n, self.dim)
         self._check(self._lib.qadam_embedding_lookup(
             self._h, weight.data_ptr(), wt, 0 if k_x is None else _integer(k_x, "k_x", 32), ws, at, size, n, _padding(padding_idx), scale,
             out.data_ptr(), types[out.dtype], os, _stream(stream)))
@@ -285,9 +287,9 @@ class Embedding(_Handle):
             return self._check(rc)
         types = _types()
         at, size, n = self._tokens(tokens)
+        ds, gs = _rows(dout, "dout", n, self.dim), _rows(grad, "grad", self.rows, self.dim)
         if dout.dtype not in types or grad.dtype not in types:
             raise ValueError("dout, grad: expected float32, bfloat16 or float16")
-        ds, gs = _rows(dout, "dout", n, self.dim), _rows(grad, "grad", self.rows, self.dim)
         self._check(self._lib.qadam_embedding_grad(
             self._h, at, size, n, _padding(padding_idx), scale, dout.data_ptr(), types[dout.dtype], ds,
             grad.data_ptr(), types[grad.dtype], gs, int(bool(accumulate)), _stream(stream)))

@@ -35,3 +35,21 @@ def test_accumulate_is_a_truth_value(ways, accumulate):
     Embedding(4, 8, 3).grad(tok, dout, grad, accumulate=accumulate)
     before = 2.0 if accumulate else 0.0
     assert (grad[0] == 3.0 + before).all() and (grad[1:] == before).all()
+
+
+@pytest.mark.parametrize("other", [None, 1.0, [1.0], "x"])
+def test_what_is_no_tensor(ways, other):
+    f32, tok = torch.ones(4, 8, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+    emb, cfg = Embedding(4, 8, 4), AdamWConfig()
+    calls = [lambda: emb.lookup(other, tok, f32), lambda: emb.lookup(f32, other, f32), lambda: emb.lookup(f32, tok, other),
+             lambda: emb.grad(other, f32, f32), lambda: emb.grad(tok, other, f32), lambda: emb.grad(tok, f32, other),
+             lambda: AdamW(cfg, [other], [f32], [f32]), lambda: AdamW(cfg, [f32], [other], [f32]),
+             lambda: GradNorm([32]).grad_norm([f32], 1.0, other)]
+    if other is not None:           # None: no copy, no gradient, no factor
+        opt = AdamW(cfg, [f32], **adamw_state(cfg, [f32]))
+        calls += [lambda: AdamW(cfg, [f32], [f32], [f32], copies=[other]), lambda: opt.step(1, 1e-3, [other]),
+                  lambda: opt.step(1, 1e-3, [f32], grad_scale=other), lambda: GradNorm([32]).grad_norm([other], 1.0, torch.zeros(2, device="cuda"))]
+    for k, call in enumerate(calls):
+        with pytest.raises(ValueError, match="expected a tensor"):
+            call()
+    assert (f32 == 1).all()
