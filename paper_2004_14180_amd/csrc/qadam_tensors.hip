@@ -11,8 +11,9 @@
 //   * element types are known at compile time behind one uniform branch; the last block of a tensor takes the same code with
 //     neighbouring elements repeated, all loads still under way together (a loop over elements: 51 k elements 9.3 us, now 5.2);
 //   * a block of the 8-bit states is a wavefront's block, so its two scales are maxima over lanes, by DPP, with no LDS.
-// GPT-2 small's list (124 M, bf16 gradients and copy) 575 us, 6.06 TB/s; GPT-1.3B's with 8-bit states 3500 us, 6.04 TB/s; the norm of
-// 1.3 G bf16 390 us, 6.75 TB/s.  A large copy in place reaches 5.9 TB/s here.
+// GPT-2 small's list (124 M, bf16 gradients and copy) 573 to 588 us by box, 5.9 to 6.1 TB/s; GPT-1.3B's with 8-bit states 3490 us, 6.05 TB/s;
+// 124 M bf16 weights with states in 32 bits 429 us, in 8 bits 198 us, both 6.3 TB/s; the norm of 1.3 G bf16 390 us, 6.75 TB/s.  torch's
+// addition in place reaches 5.9 TB/s here, this library's streams in place 6.0 to 6.3.
 #include "qadam_elements.h"
 #include "qadam_operators.h"
 

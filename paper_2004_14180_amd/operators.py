@@ -1,6 +1,7 @@
 """Python side of the operators beside the step (``include/qadam.h``, second part): AdamW over a list of tensors, the norm that clips
 their gradients, embedding lookup and its gradient.  Argument checks and marshalling only, as in :mod:`.binding`: every call enqueues on
-the given (default: current) stream and does not synchronise.
+the given (default: current) stream and does not synchronise.  Buffers are written in place behind autograd's back: their version
+counters stay, so a backward pass that saved a tensor before a call has changed it is not refused.
 """
 from __future__ import annotations
 
@@ -141,7 +142,8 @@ class AdamW(_TensorList):
 
     The handle steps the tensors that it is made with, in place: `params`, `m`, `v`, with 8-bit states (torch.float8_e4m3fn)
     `m_scales`, `v_scales`, and where given `copies`, the weights in another type (None for a tensor without one).  They must be
-    contiguous and stay where they are.  `weight_decay` and `grad_dtype`: one for all, or one per tensor.
+    contiguous and stay where they are.  `weight_decay` and `grad_dtype`: one for all, or one per tensor.  8-bit second moments do not
+    follow gradients that shrink against others of their block of 256 (``include/qadam.h`` has figures).
     """
     _destroy = "qadam_adamw_destroy"
 
@@ -256,6 +258,7 @@ class Embedding(_Handle):
 
     def lookup(self, weight, tokens, out, scale: float = 1.0, k_x: Optional[int] = None, padding_idx: Optional[int] = None, stream=None):
         """out[t] = scale * weight[tokens[t]]; zeros for the padding and for tokens out of range (status bit QADAM_STATUS_TOKEN_RANGE).
+        torch's embedding returns the row of its padding_idx: for that, give it to `grad` alone.
         `weight`: (rows, dim) in float32, bfloat16, float16, or weight codes in int8 or int16 with their `k_x`."""
         rc = binding._native.embedding_lookup(self._plan, *_device_and_stream(stream), weight, tokens, out, scale, k_x, padding_idx)
         if rc is not None:
