@@ -439,6 +439,104 @@ int qadam_embedding_grad(qadam_embedding_t h, const void* tokens, int32_t token_
 
 int qadam_embedding_get_status(qadam_embedding_t h, qadam_status_t* out, int32_t clear, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Between the looked-up rows and the next token: layer norm with its gradient, the product of tokens with weight codes, and sampling.
+ * Conventions as of the operators above (device pointers in their elements' alignment, strides in elements, streams, scratch of a
+ * handle, allocation only in the init calls).  The element types are QADAM_F32, QADAM_BF16 and QADAM_F16 where nothing else is said.
+ * All compute calls may be recorded into a graph. */
+
+/* Layer norm over rows of `dim` (1 to 2^20) elements, in fp32:
+ *     mean = sum x / dim;  rstd = 1 / sqrt(sum (x - mean)^2 / dim + eps);  out = (x - mean) rstd weight + bias. */
+typedef struct qadam_layer_norm_ctx* qadam_layer_norm_t;
+
+int qadam_layer_norm_init(qadam_layer_norm_t* out, int32_t dim, float eps);     /* eps >= 0 */
+int qadam_layer_norm_destroy(qadam_layer_norm_t h);
+
+/*   x, out          rows x dim; strides >= dim, x_stride also 0: one row for all.  out may be x itself, in the same type and stride
+ *   weight, bias    dim elements of weight_type each; NULL: ones, zeros
+ *   mean, rstd      fp32 of each row for the gradient, or NULL (each on its own) */
+int qadam_layer_norm(qadam_layer_norm_t h, int64_t rows, const void* x, int32_t x_type, int64_t x_stride, const void* weight,
+                     const void* bias, int32_t weight_type, void* out, int32_t out_type, int64_t out_stride, float* mean, float* rstd,
+                     void* stream);
+
+/* Its gradient.  With xh = (x - mean) rstd and g = dout weight:
+ *     dx = rstd (g - sum g / dim - xh sum (g xh) / dim);  dweight = sum over rows of dout xh;  dbias = sum over rows of dout;
+ * accumulate = 1: the two sums are added to what dweight and dbias hold.  The sums over rows are taken in fp32 over a workgroup's rows and
+ * in fp64 over workgroups, in an order that depends on rows and dim alone: the same bits on every run.  No rows: dweight and dbias become
+ * zeros (accumulate = 1: stay).
+ *   dout            dout_stride >= dim, or 0: one row for all
+ *   mean, rstd      of the forward call
+ *   dx              dx_stride >= dim; may be dout or x itself, in the same type and stride
+ *   dweight, dbias  dim elements of grad_type each, or NULL (each on its own): may be parts of a flat gradient vector */
+int qadam_layer_norm_grad(qadam_layer_norm_t h, int64_t rows, const void* dout, int32_t dout_type, int64_t dout_stride, const void* x,
+                          int32_t x_type, int64_t x_stride, const void* weight, int32_t weight_type, const float* mean, const float* rstd,
+                          void* dx, int32_t dx_type, int64_t dx_stride, void* dweight, void* dbias, int32_t grad_type, int32_t accumulate,
+                          void* stream);
+
+/* Product of tokens with a matrix of 8-bit integers of `outputs` (1 to 2^24) rows of `inputs` (1 to 2^17 - 1) elements, such as the layer's part
+ * of the weight codes that qadam_step_fused emits.  A token x of `inputs` floats becomes integers of its own scale, in fp32 with one
+ * rounding per operation:
+ *     a = max |x_j|;  q_j = round(x_j (127 (1 / a))), ties to even;  s = a (1/127)
+ * (a < 2^-116: q = 0, s = 0; a not finite: q = 0, s = NaN).  The sum over j of q_j w_nj is exact, in 32-bit integers; then, in fp32,
+ *     out[t][n] = ((float) sum * s_t) * r_n + bias_n,    r_n = weight_scales[n], or 2^-(k_x+1) for weight codes.
+ * max_tokens (up to 2^24, and max_tokens * inputs up to 2^36) bounds num_tokens of one call; the handle's scratch holds their integers. */
+typedef struct qadam_linear8_ctx* qadam_linear8_t;
+
+int qadam_linear8_init(qadam_linear8_t* out, int64_t outputs, int32_t inputs, int64_t max_tokens);
+int qadam_linear8_destroy(qadam_linear8_t h);
+
+/* The first line of these formulas alone, for tokens that several products take: codes int8 (codes_stride >= inputs), scales fp32 of each
+ * token.  x_stride >= inputs, or 0. */
+int qadam_linear8_quantize(qadam_linear8_t h, int64_t num_tokens, const void* x, int32_t x_type, int64_t x_stride, int8_t* codes,
+                           int64_t codes_stride, float* scales, void* stream);
+
+/*   x               tokens in a float type, with x_scales NULL; or QADAM_CODES8 with their scales, any integers in int8
+ *   weight          int8, weight_stride >= inputs, at any address: any integers in int8
+ *   weight_scales   fp32 of each output, or NULL with the codes' k_x (0..6)
+ *   bias            outputs elements of bias_type, or NULL
+ *   out             out_stride >= outputs; elements behind a row's last one are left as they are */
+int qadam_linear8_forward(qadam_linear8_t h, int64_t num_tokens, const void* x, int32_t x_type, int64_t x_stride, const float* x_scales,
+                          const int8_t* weight, int64_t weight_stride, const float* weight_scales, int32_t k_x, const void* bias,
+                          int32_t bias_type, void* out, int32_t out_type, int64_t out_stride, void* stream);
+
+/* Sampling of one token per row of `vocab` (1 to 2^24) logits from given random numbers.  Tokens are taken in descending order of their logits,
+ * the lower index first among equals, and every filter keeps the first ones of that order:
+ *     mass_i = round(2^40 exp((logit_i - largest) / temperature)) in fp64, an integer, so that sums are exact;
+ *     top_k > 0      the first top_k;
+ *     top_p < 1      of those the fewest, but one at least, whose masses' sum reaches top_p of all of theirs;
+ *     min_p > 0      of those the ones whose mass reaches min_p 2^40;
+ * of the kept masses' sum S, the token is the first one at which the sum so far is beyond u S (comparisons in fp64).  temperature = 0:
+ * the largest logit, the lowest index among equals.  Logits of minus infinity have no mass; where the largest is infinite, the
+ * logits equal to it have all of it.  u below 0 or NaN counts as 0, from 1 on as the largest fp32 below 1.
+ * A row without a token (a NaN among its logits, all logits minus infinity, a temperature that is negative, infinite or NaN) gives -1 and sets
+ * QADAM_STATUS_NO_TOKEN in the handle's status word. */
+typedef struct qadam_sampler_ctx* qadam_sampler_t;
+#define QADAM_STATUS_NO_TOKEN 8u
+
+/* Filters: for each a device array of one value per row, or NULL and the value for all rows.  top_k <= 0, top_p >= 1 and min_p <= 0 (NaN
+ * too) keep all; min_p > 1 counts as 1. */
+typedef struct {
+    const float*   temperatures;
+    const int32_t* top_ks;
+    const float*   top_ps;
+    const float*   min_ps;
+    float   temperature;    /* >= 0 */
+    int32_t top_k;
+    float   top_p;
+    float   min_p;
+} qadam_filters_t;
+
+int qadam_sampler_init(qadam_sampler_t* out, int64_t vocab, int64_t max_rows);  /* up to 2^24 rows in a call */
+int qadam_sampler_destroy(qadam_sampler_t h);
+
+/*   logits  rows x vocab; logits_stride >= vocab, or 0
+ *   u       fp32 of each row
+ *   out     int32 or int64 (token_bytes 4 or 8) of each row */
+int qadam_sampler_sample(qadam_sampler_t h, int64_t rows, const void* logits, int32_t logits_type, int64_t logits_stride, const float* u,
+                         const qadam_filters_t* filters, void* out, int32_t token_bytes, void* stream);
+
+int qadam_sampler_get_status(qadam_sampler_t h, qadam_status_t* out, int32_t clear, void* stream);
+
 /* Text of the last HIP error seen by this thread's calls (static storage). */
 const char* qadam_last_error(void);
 

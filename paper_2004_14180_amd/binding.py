@@ -22,6 +22,7 @@ QADAM_IDENTITY = -1          # k_g or k_x: that quantizer is the identity
 QADAM_STATUS_NONFINITE_SCALE = 1
 QADAM_STATUS_ERR_BOUND_VIOLATED = 2
 QADAM_STATUS_TOKEN_RANGE = 4
+QADAM_STATUS_NO_TOKEN = 8
 QADAM_F32, QADAM_BF16, QADAM_F16, QADAM_CODES8, QADAM_CODES16 = range(5)    # element types
 QADAM_STATE_BLOCK = 256
 
@@ -36,6 +37,9 @@ EXPORTS = [
     "qadam_grad_norm_init", "qadam_grad_norm_destroy", "qadam_grad_norm",
     "qadam_embedding_init", "qadam_embedding_destroy", "qadam_embedding_lookup", "qadam_embedding_grad",
     "qadam_embedding_get_status",
+    "qadam_layer_norm_init", "qadam_layer_norm_destroy", "qadam_layer_norm", "qadam_layer_norm_grad",
+    "qadam_linear8_init", "qadam_linear8_destroy", "qadam_linear8_quantize", "qadam_linear8_forward",
+    "qadam_sampler_init", "qadam_sampler_destroy", "qadam_sampler_sample", "qadam_sampler_get_status",
 ]
 
 
@@ -77,6 +81,11 @@ class _AdamWConfig(C.Structure):
 class _AdamWTensor(C.Structure):
     _fields_ = [("numel", C.c_int64)] + [(n, C.c_void_p) for n in ("param", "m", "v", "m_scales", "v_scales", "copy")] + \
                [("param_type", C.c_int32), ("grad_type", C.c_int32), ("copy_type", C.c_int32), ("weight_decay", C.c_float)]
+
+
+class _Filters(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("temperatures", "top_ks", "top_ps", "min_ps")] + \
+               [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float)]
 
 
 @dataclass
@@ -177,6 +186,18 @@ def load_library():
     lib.qadam_embedding_lookup.argtypes = [vp, vp, i32, i32, i64, vp, i32, i64, i64, f32, vp, i32, i64, vp]
     lib.qadam_embedding_grad.argtypes = [vp, vp, i32, i64, i64, f32, vp, i32, i64, vp, i32, i64, i32, vp]
     lib.qadam_embedding_get_status.argtypes = [vp, C.POINTER(_Status), i32, vp]
+    lib.qadam_layer_norm_init.argtypes = [C.POINTER(vp), i32, f32]
+    lib.qadam_layer_norm_destroy.argtypes = [vp]
+    lib.qadam_layer_norm.argtypes = [vp, i64, vp, i32, i64, vp, vp, i32, vp, i32, i64, vp, vp, vp]
+    lib.qadam_layer_norm_grad.argtypes = [vp, i64, vp, i32, i64, vp, i32, i64, vp, i32, vp, vp, vp, i32, i64, vp, vp, i32, i32, vp]
+    lib.qadam_linear8_init.argtypes = [C.POINTER(vp), i64, i32, i64]
+    lib.qadam_linear8_destroy.argtypes = [vp]
+    lib.qadam_linear8_quantize.argtypes = [vp, i64, vp, i32, i64, vp, i64, vp, vp]
+    lib.qadam_linear8_forward.argtypes = [vp, i64, vp, i32, i64, vp, vp, i64, vp, i32, vp, i32, vp, i32, i64, vp]
+    lib.qadam_sampler_init.argtypes = [C.POINTER(vp), i64, i64]
+    lib.qadam_sampler_destroy.argtypes = [vp]
+    lib.qadam_sampler_sample.argtypes = [vp, i64, vp, i32, i64, vp, C.POINTER(_Filters), vp, i32, vp]
+    lib.qadam_sampler_get_status.argtypes = [vp, C.POINTER(_Status), i32, vp]
     _native, _segment = _load_native(torch), _address(lib.qadam_quantize_segment_noalloc)
     _lib, _torch = lib, torch
     return lib

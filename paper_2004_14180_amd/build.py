@@ -9,7 +9,8 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libqadam_hip.so")
-SOURCES = ["qadam_kernels.hip", "qadam_api.cpp", "qadam_tensors.hip", "qadam_embedding.hip", "qadam_operators.cpp"]
+SOURCES = ["qadam_kernels.hip", "qadam_api.cpp", "qadam_tensors.hip", "qadam_embedding.hip", "qadam_operators.cpp",
+           "qadam_layer_norm.hip", "qadam_linear8.hip", "qadam_sampler.hip", "qadam_layers.cpp"]
 
 # -ffp-contract=off: one rounding per operation, so integer codes are reproducible bit for bit.
 # The target-feature switch keeps the gfx950 pass from forming packed-fp32 instructions (v_pk_add_f32,

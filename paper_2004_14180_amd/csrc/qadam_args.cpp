@@ -13,7 +13,7 @@
 
 namespace {
 
-constexpr char kPlanName[] = "qadam plan", kListName[] = "qadam list of tensors", kEmbeddingName[] = "qadam embedding";
+constexpr char kPlanName[] = "qadam plan", kListName[] = "qadam list of tensors", kEmbeddingName[] = "qadam embedding", kLayerName[] = "qadam layer";
 
 struct Plan {
     qadam_handle_t h;
@@ -387,6 +387,146 @@ PyObject* embedding_grad(PyObject*, PyObject* const* argv, Py_ssize_t argc)
     });
 }
 
+// Layer norm, the product in 8-bit integers, sampling: rows of `dim` elements, the product's results of `outputs`.
+struct LayerPlan {
+    void* h;
+    int64_t dim, outputs;
+    void *entry, *entry2;
+};
+
+#define QADAM_ENTRY(address, function) reinterpret_cast<decltype(&function)>(address)
+
+// rows of `dim` elements whose number the tensor itself gives
+Rows first_rows(Args& a, int64_t dim, int64_t device, int64_t& num)
+{
+    num = 0;
+    if (a.ok && THPVariable_CheckExact(*a.next)) {
+        const at::Tensor& t = THPVariable_Unpack(*a.next);
+        if (t.dim() >= 2) num = t.numel() / dim;
+    }
+    return rows(a, num, dim, device);
+}
+
+struct Vector {
+    void* at;
+    int32_t type;
+};
+
+// an optional vector of a float type; `like` (>= 0): the type that it has to have
+Vector vector(Args& a, int64_t count, int64_t device, int like = -1)
+{
+    PyObject* o = *a.next++;
+    if (o == Py_None) return {nullptr, like < 0 ? 0 : like};
+    const at::Tensor* t = on_device(a, o, device);
+    const int type = t ? element_type(*t) : -1;
+    if (type < 0 || type > QADAM_F16 || (like >= 0 && type != like) || t->numel() != count || !t->is_contiguous()) { a.ok = false; return {}; }
+    return {t->data_ptr(), type};
+}
+
+PyObject* layer_norm(PyObject*, PyObject* const* argv, Py_ssize_t argc)
+{
+    return planned<LayerPlan, kLayerName>(argv, argc, 9, [](Args& a, const LayerPlan& p, int64_t device, void* stream) {
+        int64_t num;
+        const Rows x = first_rows(a, p.dim, device, num);
+        const Vector w = vector(a, p.dim, device), b = vector(a, p.dim, device, w.at ? w.type : -1);
+        const Rows out = rows(a, num, p.dim, device);
+        float* mean = floats(a, num, device, true);
+        float* rstd = floats(a, num, device, true);
+        if (x.type > QADAM_F16 || out.type > QADAM_F16) a.ok = false;
+        return call(a, [&] {
+            return QADAM_ENTRY(p.entry, qadam_layer_norm)(static_cast<qadam_layer_norm_t>(p.h), num, x.at, x.type, x.stride, w.at, b.at, b.type,
+                                                          out.at, out.type, out.stride, mean, rstd, stream);
+        });
+    });
+}
+
+PyObject* layer_norm_grad(PyObject*, PyObject* const* argv, Py_ssize_t argc)
+{
+    return planned<LayerPlan, kLayerName>(argv, argc, 12, [](Args& a, const LayerPlan& p, int64_t device, void* stream) {
+        int64_t num;
+        const Rows dout = first_rows(a, p.dim, device, num), x = rows(a, num, p.dim, device);
+        const Vector w = vector(a, p.dim, device);
+        const float* mean = floats(a, num, device);
+        const float* rstd = floats(a, num, device);
+        const Rows dx = rows(a, num, p.dim, device);
+        const Vector dw = vector(a, p.dim, device), db = vector(a, p.dim, device, dw.at ? dw.type : -1);
+        const int64_t accumulate = a.integer();
+        if (dout.type > QADAM_F16 || x.type > QADAM_F16 || dx.type > QADAM_F16) a.ok = false;
+        return call(a, [&] {
+            return QADAM_ENTRY(p.entry2, qadam_layer_norm_grad)(
+                static_cast<qadam_layer_norm_t>(p.h), num, dout.at, dout.type, dout.stride, x.at, x.type, x.stride, w.at, w.type, mean, rstd,
+                dx.at, dx.type, dx.stride, dw.at, db.at, db.type, accumulate != 0, stream);
+        });
+    });
+}
+
+PyObject* linear8_quantize(PyObject*, PyObject* const* argv, Py_ssize_t argc)
+{
+    return planned<LayerPlan, kLayerName>(argv, argc, 6, [](Args& a, const LayerPlan& p, int64_t device, void* stream) {
+        int64_t num;
+        const Rows x = first_rows(a, p.dim, device, num), codes = rows(a, num, p.dim, device);
+        float* scales = floats(a, num, device);
+        if (x.type > QADAM_F16 || codes.type != QADAM_CODES8) a.ok = false;
+        return call(a, [&] {
+            return QADAM_ENTRY(p.entry2, qadam_linear8_quantize)(static_cast<qadam_linear8_t>(p.h), num, x.at, x.type, x.stride,
+                                                                 static_cast<int8_t*>(codes.at), codes.stride, scales, stream);
+        });
+    });
+}
+
+PyObject* linear8_forward(PyObject*, PyObject* const* argv, Py_ssize_t argc)
+{
+    return planned<LayerPlan, kLayerName>(argv, argc, 10, [](Args& a, const LayerPlan& p, int64_t device, void* stream) {
+        int64_t num;
+        const Rows x = first_rows(a, p.dim, device, num), w = rows(a, p.outputs, p.dim, device), out = rows(a, num, p.outputs, device);
+        const float* scales = floats(a, p.outputs, device, true);
+        if ((*a.next == Py_None) == (scales == nullptr)) a.ok = false;
+        const int64_t k_x = padding(a);
+        const float* x_scales = floats(a, num, device, true);
+        const Vector b = vector(a, p.outputs, device);
+        if ((x_scales ? x.type != QADAM_CODES8 : x.type > QADAM_F16) || w.type != QADAM_CODES8 || out.type > QADAM_F16 || k_x < INT32_MIN || k_x > INT32_MAX)
+            a.ok = false;
+        return call(a, [&] {
+            return QADAM_ENTRY(p.entry, qadam_linear8_forward)(
+                static_cast<qadam_linear8_t>(p.h), num, x.at, x.type, x.stride, x_scales, static_cast<int8_t*>(w.at), w.stride, scales,
+                (int32_t)k_x, b.at, b.type, out.at, out.type, out.stride, stream);
+        });
+    });
+}
+
+PyObject* sample(PyObject*, PyObject* const* argv, Py_ssize_t argc)
+{
+    return planned<LayerPlan, kLayerName>(argv, argc, 10, [](Args& a, const LayerPlan& p, int64_t device, void* stream) {
+        int64_t num;
+        const Rows logits = first_rows(a, p.dim, device, num);
+        const float* u = floats(a, num, device);
+        const at::Tensor* out = on_device(a, *a.next++, device);
+        if (!out || (out->scalar_type() != at::kInt && out->scalar_type() != at::kLong) || out->numel() != num || !out->is_contiguous()) a.ok = false;
+        qadam_filters_t f{};
+        auto one = [&](const float*& each, float& all) {
+            if (PyFloat_Check(*a.next) || PyLong_Check(*a.next)) all = a.number();
+            else each = floats(a, num, device);
+        };
+        one(f.temperatures, f.temperature);
+        if (PyLong_Check(*a.next)) {
+            const int64_t k = a.integer();
+            if (k < INT32_MIN || k > INT32_MAX) a.ok = false;
+            f.top_k = (int32_t)k;
+        } else {
+            const at::Tensor* t = on_device(a, *a.next++, device);
+            if (!t || t->scalar_type() != at::kInt || t->numel() != num || !t->is_contiguous()) a.ok = false;
+            else f.top_ks = static_cast<const int32_t*>(t->data_ptr());
+        }
+        one(f.top_ps, f.top_p);
+        one(f.min_ps, f.min_p);
+        if (logits.type > QADAM_F16) a.ok = false;
+        return call(a, [&] {
+            return QADAM_ENTRY(p.entry, qadam_sampler_sample)(static_cast<qadam_sampler_t>(p.h), num, logits.at, logits.type, logits.stride, u, &f,
+                                                              out->data_ptr(), (int32_t)out->element_size(), stream);
+        });
+    });
+}
+
 template <typename Plan, const char* kPlanName>
 PyObject* capsule_of(Plan* p)
 {
@@ -440,6 +580,20 @@ PyObject* embedding_plan(PyObject*, PyObject* const* argv, Py_ssize_t argc)
         reinterpret_cast<decltype(&qadam_embedding_grad)>(v[4])});
 }
 
+// (handle, elements of a row, outputs, addresses of the two entry points)
+PyObject* layer_plan(PyObject*, PyObject* const* argv, Py_ssize_t argc)
+{
+    Args a{argv, argc == 5};
+    int64_t v[5];
+    for (int i = 0; i < 5 && a.ok; ++i) v[i] = a.integer();
+    if (!a.ok || v[1] < 1) {
+        PyErr_SetString(PyExc_TypeError, "five integers expected, the second one above 0");
+        return nullptr;
+    }
+    return capsule_of<LayerPlan, kLayerName>(new LayerPlan{reinterpret_cast<void*>(v[0]), v[1], v[2], reinterpret_cast<void*>(v[3]),
+                                                           reinterpret_cast<void*>(v[4])});
+}
+
 void free_plan(PyObject* capsule) { delete static_cast<Plan*>(PyCapsule_GetPointer(capsule, kPlanName)); }
 
 // (handle, workers, params, segments, code bytes, weight code bytes, weight_ef, addresses of the five entry points)
@@ -467,7 +621,9 @@ PyMethodDef kFunctions[] = {QADAM_FUNCTION(plan), QADAM_FUNCTION(worker_quantize
                             QADAM_FUNCTION(weight_quantize), QADAM_FUNCTION(step_fused), QADAM_FUNCTION(step_fused_w),
                             QADAM_FUNCTION(quantize_segment), QADAM_FUNCTION(list_plan), QADAM_FUNCTION(adamw_step),
                             QADAM_FUNCTION(grad_norm), QADAM_FUNCTION(embedding_plan), QADAM_FUNCTION(embedding_lookup),
-                            QADAM_FUNCTION(embedding_grad), {nullptr, nullptr, 0, nullptr}};
+                            QADAM_FUNCTION(embedding_grad), QADAM_FUNCTION(layer_plan), QADAM_FUNCTION(layer_norm),
+                            QADAM_FUNCTION(layer_norm_grad), QADAM_FUNCTION(linear8_quantize), QADAM_FUNCTION(linear8_forward),
+                            QADAM_FUNCTION(sample), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_args", "Calls of the library with tensors of the common form.", -1, kFunctions,
                        nullptr, nullptr, nullptr, nullptr};
