@@ -187,9 +187,12 @@ int qadam_linear8_forward(qadam_linear8_t h, int64_t num_tokens, const void* x, 
     if (bias) QADAM_CHECK(check_address(bias, element_size(bias_type), "bias"));
     QADAM_CHECK(check_rows(out, out_type, num_tokens, out_stride, h->outputs, true, "out"));
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    QADAM_HIP(launch_tokens({num_tokens, x, x_stride, h->codes.get(), padded, h->scales.get(), K, padded, x_type, s}));
-    QADAM_HIP(launch_product({num_tokens, h->outputs, h->codes.get(), padded, x_scales ? x_scales : h->scales.get(), weight, weight_stride,
-                              weight_scales, bias, out, out_stride, std::ldexp(1.0f, -(k_x + 1)), K, bias_type, out_type, s}));
+    // integers that lie as the kernels want them are taken where they are
+    const bool there = x_type == QADAM_CODES8 && K == padded && x_stride % 16 == 0 && x_stride <= 1 << 22 && reinterpret_cast<uintptr_t>(x) % 16 == 0;
+    const TokensLaunch X{num_tokens, x, x_stride, there ? nullptr : h->codes.get(), padded, h->scales.get(), K, padded, x_type, s};
+    QADAM_HIP(launch_product({num_tokens, h->outputs, there ? static_cast<const int8_t*>(x) : h->codes.get(), there ? x_stride : padded,
+                              x_scales ? x_scales : h->scales.get(), weight, weight_stride, weight_scales, bias, out, out_stride,
+                              std::ldexp(1.0f, -(k_x + 1)), K, bias_type, out_type, s}, X));
     return QADAM_OK;
 }
 

@@ -69,7 +69,8 @@ struct ProductLaunch {
     int32_t inputs, bias_type, out_type;
     hipStream_t stream;
 };
-hipError_t launch_product(const ProductLaunch& L);
+// X: how the tokens become L.codes, its own `codes` null where they need not.
+hipError_t launch_product(const ProductLaunch& L, const TokensLaunch& X);
 
 // ---- sampling -----------------------------------------------------------------------------------
 struct SampleLaunch {

@@ -1,4 +1,10 @@
 // gfx950 kernels of the product of tokens with a matrix of 8-bit integers.
+//
+// Sums of products of 8-bit integers are exact in 32 bits in whatever order they are taken, so that the work may be split over wavefronts
+// in any way and the result stays the same bits.  Two ways, by sizes alone (Linear8Plan):
+//   * few tokens: bound by reading the weights.  They go from memory straight into the matrix instructions' registers, once, by as many
+//     wavefronts as keep enough loads under way (k_product_rows);
+//   * many tokens: bound by the matrix instructions and by what feeds them.  Tiles of both operands pass through LDS (k_product_tiles).
 #include "qadam_layers.h"
 #include "qadam_row.h"
 
@@ -25,129 +31,541 @@ struct TokenScale {
     __device__ __forceinline__ int code(float x) const { return inverse == 0.0f ? 0 : (int)rintf(x * inverse); }
 };
 
-// One workgroup per token, which reads it twice; codes up to `padded` are written, zeros from `inputs` on.
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ uint32_t moved_bits(uint32_t x)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+}
+
+// Largest of a wavefront's values, the same in all lanes
+__device__ __forceinline__ uint32_t wave_largest(uint32_t x)
+{
+    x = larger(x, moved_bits<0xb1>(x));
+    x = larger(x, moved_bits<0x4e>(x));
+    x = larger(x, moved_bits<0x141>(x));
+    x = larger(x, moved_bits<0x140>(x));
+    x = larger(x, moved_bits<0x142, 0xa>(x));
+    x = larger(x, moved_bits<0x143, 0xc>(x));
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+
+__device__ __forceinline__ uint32_t largest_of(f8 x)
+{
+    typedef uint32_t u8 __attribute__((ext_vector_type(kRowRun)));
+    const u8 bits = __builtin_bit_cast(u8, x) & 0x7fffffffu;       // of the whole vector: of an element it takes the first one's
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < kRowRun; ++i) m = larger(m, bits[i]);
+    return m;
+}
+
+__device__ __forceinline__ uint64_t codes_of(const TokenScale& s, f8 x)
+{
+    uint32_t w[2] = {};
+#pragma unroll
+    for (int i = 0; i < kRowRun; ++i) w[i / 4] |= (uint32_t)(s.code(x[i]) & 0xff) << 8 * (i % 4);
+    return (uint64_t)w[1] << 32 | w[0];
+}
+
+// 8 integers at an address of any alignment, `n` of them
+__device__ __forceinline__ void store_codes(int8_t* p, uint64_t v, int n)
+{
+    typedef uint64_t u8 __attribute__((aligned(1)));
+    if (n >= kRowRun) {
+        *(QADAM_GLOBAL u8*)p = v;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < kRowRun - 1; ++i)
+        if (i < n) global(p)[i] = (int8_t)(v >> 8 * i);
+}
+
+// One workgroup per token; up to HELD * 2048 inputs stay in registers between the maximum and the integers, beyond that the row is read
+// again.  Integers up to `padded` are written, zeros from `inputs` on.
+template <int HELD>
 __global__ void __launch_bounds__(kThreads) k_tokens(TokensLaunch L)
 {
-    __shared__ uint32_t most[kThreads / 64];
-    for (int64_t t = blockIdx.x; t < L.tokens; t += gridDim.x) {
+    __shared__ uint32_t most[2][kThreads / 64];
+    constexpr int kAcross = kThreads * kRowRun;
+    int turn = 0;
+    for (int64_t t = blockIdx.x; t < L.tokens; t += gridDim.x, turn ^= 1) {
         int8_t* to = L.codes + t * L.codes_stride;
+        const int first = threadIdx.x * kRowRun;
         if (L.x_type == QADAM_CODES8) {
             const int8_t* from = static_cast<const int8_t*>(L.x) + t * L.x_stride;
-            for (int at = threadIdx.x; at < L.padded; at += kThreads) global(to)[at] = at < L.inputs ? global(from)[at] : 0;
+            for (int at = first; at < L.padded; at += kAcross) {
+                uint64_t v = 0;
+                if (L.inputs - at >= kRowRun) v = __builtin_bit_cast(uint64_t, load_raw<QADAM_CODES8, kRowRun>(from + at));
+                else
+                    for (int i = 0; i < L.inputs - at; ++i) v |= (uint64_t)(uint8_t)global(from)[at + i] << 8 * i;
+                store_codes(to + at, v, L.padded - at);
+            }
             continue;
         }
+        f8 x[HELD];
         uint32_t m = 0;
-        for (int at = threadIdx.x; at < L.inputs; at += kThreads) {
-            const uint32_t bits = __builtin_bit_cast(uint32_t, load_one(L.x, L.x_type, t * L.x_stride + at)) & 0x7fffffffu;
-            m = m > bits ? m : bits;
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) {
+            x[k] = 0.0f;
+            const int at = first + k * kAcross;
+            if (at < L.inputs) x[k] = load_part(L.x, L.x_type, t * L.x_stride + at, L.inputs - at);
         }
-        for (int k = 32; k > 0; k /= 2) {
-            const uint32_t other = (uint32_t)__shfl_xor((int)m, k);
-            m = m > other ? m : other;
-        }
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) m = larger(m, largest_of(x[k]));
+        for (int at = first + HELD * kAcross; at < L.inputs; at += kAcross)
+            m = larger(m, largest_of(load_part(L.x, L.x_type, t * L.x_stride + at, L.inputs - at)));
+        m = wave_largest(m);
+        if (threadIdx.x % 64 == 0) most[turn][threadIdx.x / 64] = m;
         __syncthreads();
-        if (threadIdx.x % 64 == 0) most[threadIdx.x / 64] = m;
-        __syncthreads();
-        for (int w = 0; w < kThreads / 64; ++w) m = m > most[w] ? m : most[w];
+        for (int w = 0; w < kThreads / 64; ++w) m = larger(m, most[turn][w]);
         const TokenScale s(m);
-        for (int at = threadIdx.x; at < L.padded; at += kThreads)
-            global(to)[at] = at < L.inputs ? (int8_t)s.code(load_one(L.x, L.x_type, t * L.x_stride + at)) : 0;
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) {
+            const int at = first + k * kAcross;
+            if (at < L.padded) store_codes(to + at, codes_of(s, x[k]), L.padded - at);
+        }
+        for (int at = first + HELD * kAcross; at < L.padded; at += kAcross) {
+            f8 y = 0.0f;
+            if (at < L.inputs) y = load_part(L.x, L.x_type, t * L.x_stride + at, L.inputs - at);
+            store_codes(to + at, codes_of(s, y), L.padded - at);
+        }
         if (threadIdx.x == 0) global(L.scales)[t] = s.scale;
     }
 }
 
-// ---- the product ----------------------------------------------------------------------------------
-constexpr int kTile = 128, kStep = 64, kPitch = kStep + 16;
-
-// 16 integers of row n of the weights from k on, zeros from `inputs` on; nothing behind the matrix's last element is read
-__device__ __forceinline__ i4 load_weights(const ProductLaunch& L, int64_t n, int k)
+// ---- what both products share ---------------------------------------------------------------------
+// 16 integers of a row of the weights from k on, zeros from `inputs` on; nothing behind the row's end is read
+__device__ __forceinline__ i4 load_weights(const int8_t* row, int k, int inputs)
 {
-    if (n >= L.outputs || k >= L.inputs) return 0;
-    const int8_t* p = L.weight + n * L.weight_stride + k;
-    const int left = L.inputs - k;
-    if (left >= 16) return *(const QADAM_GLOBAL i4u*)p;
+    const int left = inputs - k;
+    if (left >= 16) return *(const QADAM_GLOBAL i4u*)(row + k);
     uint32_t w[4] = {};
+    if (left > 0) {
 #pragma unroll
-    for (int i = 0; i < 15; ++i)
-        if (i < left) w[i / 4] |= (uint32_t)(uint8_t)global(p)[i] << 8 * (i % 4);
+        for (int i = 0; i < 15; ++i)
+            if (i < left) w[i / 4] |= (uint32_t)(uint8_t)global(row)[k + i] << 8 * (i % 4);
+    }
     return {(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
 }
 
-__device__ __forceinline__ void store_out(const ProductLaunch& L, int64_t t, int64_t n, int sum, float token_scale)
-{
-    float y = (float)sum * token_scale;
-    y *= L.weight_scales ? global(L.weight_scales)[n] : L.code_scale;
-    if (L.bias) y += load_one(L.bias, L.bias_type, n);
-    const int64_t at = t * L.out_stride + n;
-    if (L.out_type == QADAM_F32) global(static_cast<float*>(L.out))[at] = y;
-    else if (L.out_type == QADAM_BF16) global(static_cast<__bf16*>(L.out))[at] = (__bf16)y;
-    else global(static_cast<_Float16*>(L.out))[at] = (_Float16)y;
-}
+typedef float f4u __attribute__((ext_vector_type(4), aligned(4)));
 
-__global__ void __launch_bounds__(kThreads) k_product(ProductLaunch L, int64_t first)
-{
-    __shared__ __attribute__((aligned(16))) int8_t a_tile[kTile * kPitch], b_tile[kTile * kPitch];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t across = (L.outputs + kTile - 1) / kTile, n0 = blockIdx.x % across * kTile, t0 = first + blockIdx.x / across * kTile;
-    const int m0 = wave / 2 * 64, c0 = wave % 2 * 64;
-    i16 acc[2][2];
-    for (auto& r : acc)
-        for (auto& c : r) c = 0;
-    for (int k0 = 0; k0 < L.inputs; k0 += kStep) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < kTile * (kStep / 16); i += kThreads) {
-            const int row = i / (kStep / 16), k = i % (kStep / 16) * 16;
-            i4 v = 0;
-            if (t0 + row < L.tokens) v = *(const QADAM_GLOBAL i4*)(L.codes + (t0 + row) * L.codes_stride + k0 + k);
-            *(i4*)(a_tile + row * kPitch + k) = v;
-            *(i4*)(b_tile + row * kPitch + k) = load_weights(L, n0 + row, k0 + k);
+// Scales and biases of four outputs; those behind the last one repeat it
+struct Columns {
+    f4 scale, bias;
+    __device__ __forceinline__ Columns(const ProductLaunch& L, int64_t n)
+    {
+        if (n + 4 <= L.outputs) {
+            scale = L.weight_scales ? *(const QADAM_GLOBAL f4u*)(L.weight_scales + n) : (f4)L.code_scale;
+            if (!L.bias) bias = 0.0f;
+            else if (L.bias_type == QADAM_F32) bias = *(const QADAM_GLOBAL f4u*)(static_cast<const float*>(L.bias) + n);
+            else if (L.bias_type == QADAM_BF16) bias = to_float<QADAM_BF16, 4>(load_raw<QADAM_BF16, 4, false>(static_cast<const __bf16*>(L.bias) + n));
+            else bias = to_float<QADAM_F16, 4>(load_raw<QADAM_F16, 4, false>(static_cast<const _Float16*>(L.bias) + n));
+            return;
         }
-        __syncthreads();
 #pragma unroll
-        for (int k = 0; k < kStep; k += 32) {
-            i4 a[2], b[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                a[i] = *(const i4*)(a_tile + (m0 + i * 32 + lane % 32) * kPitch + k + lane / 32 * 16);
-                b[i] = *(const i4*)(b_tile + (c0 + i * 32 + lane % 32) * kPitch + k + lane / 32 * 16);
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[i], b[j], acc[i][j], 0, 0, 0);
+        for (int i = 0; i < 4; ++i) {
+            const int64_t m = n + i < L.outputs ? n + i : L.outputs - 1;
+            scale[i] = L.weight_scales ? global(L.weight_scales)[m] : L.code_scale;
+            bias[i] = L.bias ? load_one(L.bias, L.bias_type, m) : 0.0f;
         }
     }
+    // one rounding per operation
+    __device__ __forceinline__ f4 operator()(const ProductLaunch& L, i4 sum, float token) const
+    {
+        f4 y = __builtin_convertvector(sum, f4) * token * scale;
+        if (L.bias) y += bias;
+        return y;
+    }
+};
+
+template <int OT, int N>
+__device__ __forceinline__ void store_some(typename Element<OT>::T* p, typename Run<OT, N>::F y, int64_t n)
+{
+    if (n >= N) return store_run<OT, N, false>(p, y);
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int64_t n = n0 + c0 + j * 32 + lane % 32;
-            if (n >= L.outputs) continue;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int64_t t = t0 + m0 + i * 32 + r % 4 + 8 * (r / 4) + 4 * (lane / 32);
-                if (t < L.tokens) store_out(L, t, n, acc[i][j][r], global(L.token_scales)[t]);
+    for (int i = 0; i < N - 1; ++i)
+        if (i < n) global(p)[i] = (typename Element<OT>::T)y[i];
+}
+
+// ---- few tokens -----------------------------------------------------------------------------------
+// A wavefront takes ROWS tiles of 16 rows of the weights and COLS tiles of 16 tokens, and a part of the inputs; `split` of a workgroup's
+// wavefronts share the rows and add their sums in LDS.  A lane's 16 integers of a matrix instruction are 16 bytes of one row, so the
+// weights come from memory into their places, at any address.
+// MADE: the workgroup makes the tokens' integers itself, in LDS, which saves the launch that would.
+constexpr int kRowWaves = 4;
+
+template <int ROWS, int COLS, bool MADE>
+__global__ void __launch_bounds__(64 * kRowWaves) k_product_rows(ProductLaunch L, TokensLaunch X, int split, int64_t first)
+{
+    extern __shared__ __attribute__((aligned(16))) int8_t lds[];
+    __shared__ uint32_t most[kRowWaves];
+    __shared__ float made_scales[16];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int padded = X.padded;
+    const int64_t per = (L.outputs + 16 * ROWS * (kRowWaves / split) - 1) / (16 * ROWS * (kRowWaves / split));
+    const int64_t group = blockIdx.x % per, t0 = first + blockIdx.x / per * (16 * COLS);
+    if constexpr (MADE) {
+        for (int t = 0; t < (int)L.tokens; ++t) {
+            uint32_t m = 0;
+            for (int at = threadIdx.x * kRowRun; at < L.inputs; at += 64 * kRowWaves * kRowRun)
+                m = larger(m, largest_of(load_part(X.x, X.x_type, t * X.x_stride + at, L.inputs - at)));
+            m = wave_largest(m);
+            __syncthreads();
+            if (lane == 0) most[wave] = m;
+            __syncthreads();
+            for (int w = 0; w < kRowWaves; ++w) m = larger(m, most[w]);
+            const TokenScale s(m);
+            if (threadIdx.x == 0) made_scales[t] = s.scale;
+            for (int at = threadIdx.x * kRowRun; at < padded; at += 64 * kRowWaves * kRowRun) {
+                f8 x = 0.0f;
+                if (at < L.inputs) x = load_part(X.x, X.x_type, t * X.x_stride + at, L.inputs - at);
+                *(uint64_t*)(lds + t * padded + at) = codes_of(s, x);
             }
         }
+        __syncthreads();
+    }
+    const int part = wave % split, chunks = (L.inputs + 63) / 64, each = (chunks + split - 1) / split;
+    const int begin = part * each, end = begin + each < chunks ? begin + each : chunks;
+    const int64_t n0 = (group * (kRowWaves / split) + wave / split) * (16 * ROWS);
+    const int8_t* row[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int64_t n = n0 + i * 16 + lane % 16;
+        row[i] = L.weight + (n < L.outputs ? n : L.outputs - 1) * L.weight_stride;
+    }
+    const int8_t* token[COLS];
+    bool there[COLS];
+#pragma unroll
+    for (int j = 0; j < COLS; ++j) {
+        const int64_t t = t0 + j * 16 + lane % 16;
+        there[j] = t < L.tokens;
+        token[j] = MADE ? lds + (there[j] ? t : 0) * padded : L.codes + (there[j] ? t : 0) * L.codes_stride;
+    }
+    const int k0 = lane / 16 * 16;
+    i4 acc[ROWS][COLS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) acc[i][j] = 0;
+    constexpr int kAhead = ROWS == 1 ? 8 : 4;       // chunks of the weights under way together
+    i4 w[ROWS][kAhead];
+    auto load = [&](int c) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) w[i][u] = c + u < end ? load_weights(row[i], (c + u) * 64 + k0, L.inputs) : (i4)0;
+    };
+    load(begin);
+    for (int c = begin; c < end; c += kAhead) {
+        i4 now[ROWS][kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) now[i][u] = w[i][u];
+        if (c + kAhead < end) load(c + kAhead);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (c + u >= end) break;
+#pragma unroll
+            for (int j = 0; j < COLS; ++j) {
+                i4 x = 0;
+                if (there[j]) {
+                    if constexpr (MADE) x = *(const i4*)(token[j] + (c + u) * 64 + k0);
+                    else x = *(const QADAM_GLOBAL i4*)(token[j] + (c + u) * 64 + k0);
+                }
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now[i][u], x, acc[i][j], 0, 0, 0);
+            }
+        }
+    }
+    if (split > 1) {
+        __syncthreads();
+        i4* sums = (i4*)lds;
+        if (part > 0) {
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+                for (int j = 0; j < COLS; ++j) sums[((wave * ROWS + i) * COLS + j) * 64 + lane] = acc[i][j];
+        }
+        __syncthreads();
+        if (part > 0) return;
+        for (int p = 1; p < split; ++p)
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+                for (int j = 0; j < COLS; ++j) acc[i][j] += sums[(((wave + p) * ROWS + i) * COLS + j) * 64 + lane];
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int64_t n = n0 + i * 16 + lane / 16 * 4;
+        if (n >= L.outputs) continue;
+        const Columns columns(L, n);
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) {
+            const int64_t t = t0 + j * 16 + lane % 16;
+            if (t >= L.tokens) continue;
+            const f4 y = columns(L, acc[i][j], MADE ? made_scales[t] : global(L.token_scales)[t]);
+            const int64_t at = t * L.out_stride + n;
+            if (L.out_type == QADAM_F32) store_some<QADAM_F32, 4>(static_cast<float*>(L.out) + at, y, L.outputs - n);
+            else if (L.out_type == QADAM_BF16) store_some<QADAM_BF16, 4>(static_cast<__bf16*>(L.out) + at, y, L.outputs - n);
+            else store_some<QADAM_F16, 4>(static_cast<_Float16*>(L.out) + at, y, L.outputs - n);
+        }
+    }
+}
+
+// ---- many tokens ----------------------------------------------------------------------------------
+// A workgroup makes a tile of BM tokens and BN outputs, its wavefronts WM by WN parts of it, in steps of 128 inputs.  Both operands of a
+// step pass through LDS, two steps' worth of it: while one is multiplied, the next is loaded straight from memory into the other.  A row
+// of 128 integers takes its 8 runs of 16 bytes in an order of its own, run ^ (row % 8), so that the 8 lanes that LDS serves together
+// find theirs in different banks although rows are 128 bytes apart.
+//
+// A step's products are four blocks of 32 inputs.  Between the matrix instructions of one block the next block's operands are read from
+// LDS and the next step's are loaded, one instruction after each, as the source has them (sched_barrier): left to the compiler, reads
+// and products alternate with waits.  The step changes in front of its last block, whose operands are in registers by then.
+//
+// DIRECT: rows of the weights lie at addresses of 16 bytes and are loaded into LDS directly; else they pass through registers.
+constexpr int kStep = 128;
+
+template <int BM, int BN, int WM, int WN>
+struct Tiles {
+    static constexpr int threads = 64 * WM * WN, mt = BM / WM / 32, nt = BN / WN / 32;
+    static constexpr int a_bytes = BM * kStep, stage = (BM + BN) * kStep;
+    static constexpr int a_loads = BM * 8 / threads, b_loads = BN * 8 / threads;
+    static constexpr int pitch(int size) { return BN / WN * size + 16; }        // of a row of results in LDS
+    static constexpr int lds = 2 * stage > WM * WN * 32 * pitch(4) ? 2 * stage : WM * WN * 32 * pitch(4);
+};
+
+template <int BM, int BN, int WM, int WN, bool DIRECT, int OT>
+__global__ void __launch_bounds__(64 * WM * WN) k_product_tiles(ProductLaunch L, int64_t first, int across, int down)
+{
+    typedef Tiles<BM, BN, WM, WN> S;
+    extern __shared__ __attribute__((aligned(16))) int8_t lds[];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    int tm, tn;
+    tile_place(blockIdx.x, across, down, &tm, &tn);
+    const int64_t t0 = first + (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+    const int steps = (L.inputs + kStep - 1) / kStep;
+
+    // where this thread's runs of a step come from: rows behind the last one repeat it, inputs behind the last one repeat the row's first
+    // ones (the tokens' integers are zeros there)
+    const int8_t* a_base = L.codes + t0 * L.codes_stride;
+    const int8_t* b_base = L.weight + n0 * L.weight_stride;
+    const int a_rows = (int)(L.tokens - t0 < BM ? L.tokens - t0 : BM), b_rows = (int)(L.outputs - n0 < BN ? L.outputs - n0 : BN);
+    int a_at[S::a_loads], b_at[S::b_loads], b_run[S::b_loads];
+#pragma unroll
+    for (int i = 0; i < S::a_loads; ++i) {
+        const int c = i * S::threads + threadIdx.x, row = c / 8, run = (c % 8 ^ (row & 7)) * 16;
+        a_at[i] = (row < a_rows ? row : a_rows - 1) * (int)L.codes_stride + run;
+    }
+    const int8_t* b_row[S::b_loads];
+#pragma unroll
+    for (int i = 0; i < S::b_loads; ++i) {
+        const int c = i * S::threads + threadIdx.x, row = c / 8;
+        b_run[i] = (c % 8 ^ (row & 7)) * 16;
+        if constexpr (DIRECT) b_at[i] = (row < b_rows ? row : b_rows - 1) * (int)L.weight_stride;
+        else b_row[i] = b_base + (int64_t)(row < b_rows ? row : b_rows - 1) * L.weight_stride;
+    }
+    i4 b_held[DIRECT ? 1 : S::b_loads];
+    constexpr int kLoads = S::a_loads + S::b_loads;
+    auto load = [&](int step, int buffer, int i) {
+        int8_t* to = lds + buffer * S::stage;
+        if (i < S::a_loads) {
+            __builtin_amdgcn_global_load_lds((const QADAM_GLOBAL void*)(a_base + step * kStep + a_at[i]),
+                                             (__attribute__((address_space(3))) void*)(to + (i * S::threads + wave * 64) * 16), 16, 0, 0);
+        } else if constexpr (DIRECT) {
+            const int b = i - S::a_loads, k = step * kStep + b_run[b];
+            __builtin_amdgcn_global_load_lds((const QADAM_GLOBAL void*)(b_base + b_at[b] + (k < L.inputs ? k : 0)),
+                                             (__attribute__((address_space(3))) void*)(to + S::a_bytes + (b * S::threads + wave * 64) * 16), 16, 0, 0);
+        } else {
+            const int b = i - S::a_loads;
+            b_held[b] = load_weights(b_row[b], step * kStep + b_run[b], L.inputs);
+        }
+    };
+    // what was loaded into registers goes to LDS
+    auto place = [&](int buffer) {
+        if constexpr (!DIRECT) {
+#pragma unroll
+            for (int b = 0; b < S::b_loads; ++b) *(i4*)(lds + buffer * S::stage + S::a_bytes + (b * S::threads + threadIdx.x) * 16) = b_held[b];
+        }
+    };
+    // all of this wavefront's loads into LDS have arrived, and all wavefronts are here: the instructions that load into LDS are not
+    // waited for by a barrier alone
+    auto meet = [] {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    i16 acc[S::mt][S::nt];
+#pragma unroll
+    for (int i = 0; i < S::mt; ++i)
+#pragma unroll
+        for (int j = 0; j < S::nt; ++j) acc[i][j] = 0;
+    const int m0 = wave / WN * (BM / WM), c0 = wave % WN * (BN / WN);
+    i4 a[2][S::mt], b[2][S::nt];
+    constexpr int kOperands = S::mt + S::nt, kProducts = S::mt * S::nt;
+    auto read = [&](int buffer, int block, int into, int i) {
+        const int row = lane % 32, run = (block * 2 + lane / 32 ^ (row & 7)) * 16;
+        const int8_t* from = lds + buffer * S::stage + run;
+        if (i < S::mt) a[into][i] = *(const i4*)(from + (m0 + i * 32 + row) * kStep);
+        else b[into][i - S::mt] = *(const i4*)(from + S::a_bytes + (c0 + (i - S::mt) * 32 + row) * kStep);
+    };
+    // the products of the operands in a[from], b[from]; between them the reads of the next block's and the loads [begin, begin + count)
+    auto block = [&](int from, bool reads, int buffer, int next, bool loads, int step, int into, int begin, int count) {
+#pragma unroll
+        for (int m = 0; m < kProducts; ++m) {
+            const int i = m / S::nt, j = m % S::nt;
+            acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(b[from][j], a[from][i], acc[i][j], 0, 0, 0);
+            if (reads) {
+#pragma unroll
+                for (int q = 0; q < kOperands; ++q)
+                    if (q * kProducts / kOperands == m) read(buffer, next, from ^ 1, q);
+            }
+            if (loads) {
+#pragma unroll
+                for (int q = 0; q < kLoads; ++q)
+                    if (q < count && q * kProducts / count == m) load(step, into, begin + q);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    static_assert(DIRECT || S::a_loads == S::b_loads, "the second half of the loads are the weights', which are placed before the next step's");
+    constexpr int kFirst = kLoads / 2;          // of a step's loads: the ones in front of the block in which the others are issued
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load(0, 0, i);
+    place(0);
+    meet();
+    const int last = steps - 1;
+#pragma unroll
+    for (int i = 0; i < kFirst; ++i) load(last > 0 ? 1 : 0, 1, i);
+#pragma unroll
+    for (int q = 0; q < kOperands; ++q) read(0, 0, 0, q);
+    for (int s = 0; s < last; ++s) {
+        const int buffer = s & 1;
+        block(0, true, buffer, 1, true, s + 1, buffer ^ 1, kFirst, kLoads - kFirst);
+        block(1, true, buffer, 2, false, 0, 0, 0, 0);
+        block(0, true, buffer, 3, false, 0, 0, 0, 0);
+        place(buffer ^ 1);
+        meet();
+        block(1, true, buffer ^ 1, 0, true, s + 2 < last ? s + 2 : last, buffer, 0, kFirst);     // at the end the last step once more, unused
+    }
+    block(0, true, last & 1, 1, false, 0, 0, 0, 0);
+    block(1, true, last & 1, 2, false, 0, 0, 0, 0);
+    block(0, true, last & 1, 3, false, 0, 0, 0, 0);
+    block(1, false, 0, 0, false, 0, 0, 0, 0);
+
+    // Results through LDS, 32 tokens of a wavefront at a time, so that whole lines are stored: a lane holds 4 outputs of a token, and
+    // 8 bytes each in 32 rows cost a quarter of the call.
+    meet();
+    typedef typename Element<OT>::T O;
+    constexpr int kPitch = S::pitch(sizeof(O)), kRun = 16 / sizeof(O), kRuns = BN / WN / kRun;
+    int8_t* own = lds + wave * 32 * kPitch;
+#pragma unroll
+    for (int i = 0; i < S::mt; ++i) {
+        const int64_t t = t0 + m0 + i * 32;
+        const float token = global(L.token_scales)[t + lane % 32 < L.tokens ? t + lane % 32 : L.tokens - 1];
+#pragma unroll
+        for (int j = 0; j < S::nt; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int at = j * 32 + 8 * q + lane / 32 * 4;
+                const Columns columns(L, n0 + c0 + at);
+                const i4 sum = {acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
+                typedef O o4 __attribute__((ext_vector_type(4)));
+                *(o4*)(own + lane % 32 * kPitch + at * sizeof(O)) = __builtin_convertvector(columns(L, sum, token), o4);
+            }
+#pragma unroll
+        for (int q = 0; q < 32 * kRuns / 64; ++q) {
+            const int c = q * 64 + lane, row = c / kRuns, at = c % kRuns * kRun;
+            const int64_t n = n0 + c0 + at, left = L.outputs - n;
+            typedef O on __attribute__((ext_vector_type(kRun)));
+            typedef on onu __attribute__((aligned(sizeof(O))));
+            const on v = *(const on*)(own + row * kPitch + at * sizeof(O));
+            if (t + row >= L.tokens || left <= 0) continue;
+            O* p = static_cast<O*>(L.out) + (t + row) * L.out_stride + n;
+            if (left >= kRun) {
+                __builtin_nontemporal_store(v, (QADAM_GLOBAL onu*)p);
+            } else {
+#pragma unroll
+                for (int e = 0; e < kRun - 1; ++e)
+                    if (e < left) global(p)[e] = v[e];
+            }
+        }
+    }
+}
+
+template <int BM, int BN, int WM, int WN, bool DIRECT>
+hipError_t tiles(const ProductLaunch& L)
+{
+    typedef Tiles<BM, BN, WM, WN> S;
+    // a launch takes as many rows of tiles as keep it below 2^22 workgroups
+    const int across = (int)((L.outputs + BN - 1) / BN), most = (1 << 22) / across;
+    for (int64_t t = 0; t < L.tokens; t += (int64_t)most * BM) {
+        const int64_t rest = (L.tokens - t + BM - 1) / BM;
+        const int down = (int)(rest < most ? rest : most);
+        auto run = [&](auto kernel) {
+            if constexpr (S::lds > 65536) {
+                const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::lds);
+                if (e != hipSuccess) return e;
+            }
+            kernel<<<dim3(across * down), dim3(S::threads), S::lds, L.stream>>>(L, t, across, down);
+            return hipGetLastError();
+        };
+        const hipError_t e = L.out_type == QADAM_F32    ? run(k_product_tiles<BM, BN, WM, WN, DIRECT, QADAM_F32>)
+                             : L.out_type == QADAM_BF16 ? run(k_product_tiles<BM, BN, WM, WN, DIRECT, QADAM_BF16>)
+                                                        : run(k_product_tiles<BM, BN, WM, WN, DIRECT, QADAM_F16>);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <int ROWS, int COLS, bool MADE>
+hipError_t rows(const ProductLaunch& L, const TokensLaunch& X, int split)
+{
+    const int64_t across = (L.outputs + 16 * ROWS * (kRowWaves / split) - 1) / (16 * ROWS * (kRowWaves / split)), most = ((int64_t)1 << 23) / across;
+    int lds = split > 1 ? kRowWaves * ROWS * COLS * 64 * 16 : 0;
+    if (MADE && lds < (int)L.tokens * X.padded) lds = (int)L.tokens * X.padded;
+    for (int64_t t = 0; t < L.tokens; t += most * 16 * COLS) {
+        const int64_t rest = (L.tokens - t + 16 * COLS - 1) / (16 * COLS);
+        k_product_rows<ROWS, COLS, MADE><<<dim3((int)(across * (rest < most ? rest : most))), dim3(64 * kRowWaves), lds, L.stream>>>(L, X, split, t);
+    }
+    return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_tokens(const TokensLaunch& L)
 {
-    k_tokens<<<dim3((int)(L.tokens < 4096 ? L.tokens : 4096)), dim3(kThreads), 0, L.stream>>>(L);
+    const dim3 grid((int)(L.tokens < 8192 ? L.tokens : 8192));
+    if (L.inputs <= 2048) k_tokens<1><<<grid, dim3(kThreads), 0, L.stream>>>(L);
+    else k_tokens<4><<<grid, dim3(kThreads), 0, L.stream>>>(L);
     return hipGetLastError();
 }
 
-hipError_t launch_product(const ProductLaunch& L)
+hipError_t launch_product(const ProductLaunch& L, const TokensLaunch& X)
 {
-    // tiles of a launch: fewer than 2^32 work-items
-    const int64_t across = (L.outputs + kTile - 1) / kTile, most = ((int64_t)1 << 22) / across;
-    for (int64_t t = 0; t < L.tokens; t += most * kTile) {
-        const int64_t down = (L.tokens - t + kTile - 1) / kTile;
-        k_product<<<dim3((int)(across * (down < most ? down : most))), dim3(kThreads), 0, L.stream>>>(L, t);
+    const Linear8Plan p(L.tokens, L.outputs, L.inputs, X.x_type != QADAM_CODES8);
+    if (!p.made) {
+        if (X.codes) {
+            const hipError_t e = launch_tokens(X);
+            if (e != hipSuccess) return e;
+        }
+    } else {
+        return rows<1, 1, true>(L, X, p.split);
     }
-    return hipGetLastError();
+    const bool direct = reinterpret_cast<uintptr_t>(L.weight) % 16 == 0 && L.weight_stride % 16 == 0 && L.inputs % 16 == 0 && L.weight_stride <= 1 << 22;
+    switch (p.kind) {
+    case Linear8Plan::kRows16: return rows<1, 1, false>(L, X, p.split);
+    case Linear8Plan::kRows32: return rows<2, 2, false>(L, X, p.split);
+    case Linear8Plan::kRows64: return rows<2, 4, false>(L, X, p.split);
+    case Linear8Plan::kTiles256:
+        if (direct) return tiles<256, 256, 4, 2, true>(L);
+        [[fallthrough]];
+    default: return direct ? tiles<128, 128, 2, 2, true>(L) : tiles<128, 128, 2, 2, false>(L);
+    }
 }
 
 }  // namespace qadam

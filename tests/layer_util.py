@@ -81,7 +81,7 @@ def token_codes(x):
 
 def linear8(codes, scales, weight, unit, bias, dtype):
     """The product by the header's operations in fp32, on the CPU: exact sums, then one rounding per operation."""
-    sums = codes.cpu().numpy().astype(np.int64) @ weight.cpu().numpy().astype(np.int64).T
+    sums = codes.double().cpu().numpy() @ weight.double().cpu().numpy().T         # whole numbers below 2^31: exact
     with np.errstate(all="ignore"):
         y = sums.astype(np.float32) * scales.cpu().numpy()[:, None]
         y = y * (unit.cpu().numpy()[None, :] if isinstance(unit, torch.Tensor) else np.float32(unit))

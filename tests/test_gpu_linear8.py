@@ -74,6 +74,13 @@ def test_large(tokens, inputs, outputs):
     _check(tokens, inputs, outputs, F16, F32)
 
 
+@pytest.mark.parametrize("tokens,inputs,outputs,gap,offset", [(5003, 272, 5001, 0, 0), (5000, 128, 5120, 0, 0), (4800, 1040, 5300, 48, 32), (5003, 272, 5001, 0, 3),
+                                                             (5003, 250, 5001, 6, 0), (12800, 16, 2048, 0, 0), (130, 400, 99_999, 0, 0)])
+def test_many_tiles(tokens, inputs, outputs, gap, offset):
+    _check(tokens, inputs, outputs, BF16, BF16, bias=F32, gap=gap, offset=offset, out_gap=1)
+    _check(tokens, inputs, outputs, BF16, F32, scales=False, gap=gap, offset=offset)
+
+
 def test_the_largest_sums():
     """Sums of -128 * -128 over the most inputs: just below 2^31."""
     inputs = (1 << 17) - 1
