@@ -1,4 +1,15 @@
-// gfx950 kernel of sampling.
+// gfx950 kernel of sampling: a workgroup per row, which is read a few times, from the caches after the first.
+//
+// All filters keep the first tokens of one order, so none of them needs the tokens sorted: what a filter leaves is known by its sum of
+// masses, and the token is where the sum in that order passes u times the smallest of them.  Masses are integers, whose sums are the
+// same in any order: workgroups add them in LDS with atomics and the result is the same on every run.  The logits are sorted into
+// kBins bins of equal width, from the largest on down to where masses vanish.  Bins are in the order of the logits, so that a sum is
+// found by looking through the bins and then through one bin's tokens, which are few and are sorted:
+//   * top_k up to 1024: the largest logit of each thread gives a bin that at least top_k tokens lie in or in front of; those (a few more than
+//     top_k) are sorted, and no mass of another token is taken.  The same where min_p is the only filter: it names the bin;
+//   * else the masses of all tokens are added by bins (about 20 operations in fp64 each, which is most of the time), and each of
+//     the sums that are asked for takes one more pass, which collects a bin's tokens;
+//   * tokens of a bin that are more than kList (thousands of equal logits): by digits of the logits, a pass for each.
 #include "qadam_layers.h"
 #include "qadam_row.h"
 
@@ -7,6 +18,9 @@ namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kDigitBits = 8, kDigits = 1 << kDigitBits;
+constexpr int kBins = 2048, kThreadBins = kBins / kThreads;
+constexpr int kList = 4096, kThreadList = kList / kThreads;
+constexpr int kLoads = 2;               // runs of a thread under way together
 
 // Order of logits as integers: the largest logit has the smallest key, equal logits (0 and -0 too) the same one.
 __device__ __forceinline__ uint32_t key_of(float x)
@@ -20,13 +34,49 @@ __device__ __forceinline__ float logit_of(uint32_t key)
     return __builtin_bit_cast(float, key >> 31 ? key : ~key & 0x7fffffffu);
 }
 
-// round(2^40 exp((x - largest) / temperature))
-__device__ __forceinline__ uint64_t mass_of(float x, float largest, double temperature)
-{
-    if (x == largest) return (uint64_t)1 << 40;
-    const double e = exp(((double)x - (double)largest) / temperature);
-    return (uint64_t)rint(e * 0x1p40);
-}
+constexpr float kInf = __builtin_inff();
+
+// round(2^40 exp((x - largest) / temperature)): 2^y = 2^n e^r with n = round(y) and |r| up to log(2) / 2, e^r by its series up to r^12 / 12!,
+// whose rest is below 2^-52.
+struct Mass {
+    float largest;
+    double per_unit;        // log2(e) / temperature
+
+    __device__ __forceinline__ uint64_t operator()(float x) const
+    {
+        if (x == largest) return (uint64_t)1 << 40;         // both may be infinite
+        const double y = ((double)x - (double)largest) * per_unit;
+        if (!(y > -42.0)) return 0;                         // below half a unit
+        const double n = rint(y), r = (y - n) * 0x1.62e42fefa39efp-1;
+        double e = 1.0 / 479001600.0;
+        e = __builtin_fma(e, r, 1.0 / 39916800.0);
+        e = __builtin_fma(e, r, 1.0 / 3628800.0);
+        e = __builtin_fma(e, r, 1.0 / 362880.0);
+        e = __builtin_fma(e, r, 1.0 / 40320.0);
+        e = __builtin_fma(e, r, 1.0 / 5040.0);
+        e = __builtin_fma(e, r, 1.0 / 720.0);
+        e = __builtin_fma(e, r, 1.0 / 120.0);
+        e = __builtin_fma(e, r, 1.0 / 24.0);
+        e = __builtin_fma(e, r, 1.0 / 6.0);
+        e = __builtin_fma(e, r, 0.5);
+        e = __builtin_fma(e, r, 1.0);
+        e = __builtin_fma(e, r, 1.0);
+        // up to 2^40; beside 2^52 the last place is 1
+        const double m = ldexp(e, (int)n + 40) + 0x1p52;
+        return __builtin_bit_cast(uint64_t, m) & 0xfffffffffffffull;
+    }
+};
+
+// Bin of a logit, 0 for the largest: never falls where logits fall.
+struct Bin {
+    float largest, per_unit;
+
+    __device__ __forceinline__ int operator()(float x) const
+    {
+        const float d = x == largest ? 0.0f : largest - x;
+        return (int)fminf(d * per_unit, (float)(kBins - 1));
+    }
+};
 
 struct Found {
     uint32_t key;           // of the element
@@ -34,35 +84,225 @@ struct Found {
     uint64_t sum;           // of the masses up to it and with it
 };
 
+// where a sum of masses passes `target` (beyond), or reaches it
+struct Target {
+    double value;
+    bool   beyond;
+    __device__ __forceinline__ bool operator()(uint64_t sum) const { return beyond ? (double)sum > value : (double)sum >= value; }
+};
+
+struct RowFilters {
+    double temperature, top_p, min_p;
+    int32_t top_k;
+    float u;
+};
+
+struct Shared {
+    RowFilters filters;
+    uint64_t mass[kBins];
+    uint32_t count[kBins];
+    uint64_t list[kList];
+    uint64_t wave_sum[2][kWaves];
+    uint32_t wave_key[kWaves], wave_low[kWaves], wave_nan[kWaves], wave_equal[kWaves];
+    uint64_t least;             // sum of the masses that reach min_p
+    uint32_t listed, first;
+    // what a search leaves
+    int64_t  place;
+    uint64_t before, sum;
+    Found    found;
+};
+
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ uint64_t moved_sum(uint64_t x)
+{
+    const uint32_t low = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, ROWS, 0xf, false);
+    const uint32_t high = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), CTRL, ROWS, 0xf, false);
+    return x + ((uint64_t)high << 32 | low);
+}
+
+// Sum of x over the threads in front of this one; `total`: of all.  `turn` alternates between uses.
+__device__ __forceinline__ uint64_t sum_ahead(Shared& s, uint64_t x, int turn, uint64_t* total)
+{
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    uint64_t run = x;
+    // the lane 1, 2, 4 and 8 places in front within rows of 16, then the last of the row in front, then lane 31
+    run = moved_sum<0x111>(run);
+    run = moved_sum<0x112>(run);
+    run = moved_sum<0x114>(run);
+    run = moved_sum<0x118>(run);
+    run = moved_sum<0x142, 0xa>(run);
+    run = moved_sum<0x143, 0xc>(run);
+    if (lane == 63) s.wave_sum[turn][wave] = run;
+    __syncthreads();
+    uint64_t before = 0, all = 0;
+#pragma unroll 4
+    for (int w = 0; w < kWaves; ++w) {
+        const uint64_t v = s.wave_sum[turn][w];
+        before += w < wave ? v : 0;
+        all += v;
+    }
+    *total = all;
+    return before + run - x;
+}
+
+// SHORT: a vocabulary below kRowRun
+template <int LT, bool SHORT>
 struct Row {
-    const SampleLaunch& L;
-    int64_t offset;
-    float largest;
-    double temperature;
-    uint64_t* hist_mass;    // [kDigits], in LDS
-    uint32_t* hist_count;
-    Found* found;
+    typedef typename Element<LT>::T T;
+    Shared& s;
+    const T* logits;
+    int vocab;
+    Mass mass;
+    Bin bin;
 
-    __device__ __forceinline__ float logit(int64_t i) const { return load_one(L.logits, L.logits_type, offset + i); }
+    __device__ __forceinline__ float logit(int i) const { return (float)global(logits)[i]; }
 
-    // The first element in descending order at which the count of elements reaches `count` (> 0), or, with count 0, the sum of masses
-    // reaches `target` (`beyond`: is beyond it).
-    __device__ Found find(int64_t count, double target, bool beyond) const
+    // kRowRun logits from `start` on; minus infinity in front of `from`, where another thread has them, and behind the row's end
+    __device__ __forceinline__ typename Run<LT, kRowRun>::V load(int from, int* start) const
+    {
+        *start = SHORT || from + kRowRun <= vocab ? from : vocab - kRowRun;
+        typename Run<LT, kRowRun>::V raw;
+        if constexpr (!SHORT) {
+            raw = load_raw<LT, kRowRun, false>(logits + *start);
+        } else {
+            raw = (T)-kInf;
+#pragma unroll
+            for (int e = 0; e < kRowRun - 1; ++e)
+                if (e < vocab) raw[e] = global(logits)[e];
+        }
+#pragma unroll
+        for (int e = 0; e < kRowRun; ++e)
+            if (!SHORT && *start + e < from) raw[e] = (T)-kInf;
+        return raw;
+    }
+
+    // body(run of logits, index of the first): all of the row
+    template <typename F>
+    __device__ __forceinline__ void each(F&& body) const
+    {
+        constexpr int kAcross = kThreads * kRowRun;
+#pragma unroll 1
+        for (int at = threadIdx.x * kRowRun; at < vocab; at += kLoads * kAcross) {
+            typename Run<LT, kRowRun>::V raw[kLoads];
+            int start[kLoads];
+#pragma unroll
+            for (int k = 0; k < kLoads; ++k) {
+                raw[k] = (T)-kInf;
+                start[k] = 0;
+                if (at + k * kAcross < vocab) raw[k] = load(at + k * kAcross, &start[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < kLoads; ++k)
+                if (at + k * kAcross < vocab) body(to_float<LT, kRowRun>(raw[k]), start[k]);
+        }
+    }
+
+    // The tokens of the bins lo to hi (never those that are minus infinity) into the list, in descending order; their number, which may
+    // be beyond kList: then there is no list.
+    __device__ __forceinline__ int collect(int lo, int hi) const
+    {
+        __syncthreads();
+        if (threadIdx.x == 0) s.listed = 0;
+        __syncthreads();
+        each([&](f8 x, int at) {
+            uint32_t take = 0;
+#pragma unroll
+            for (int e = 0; e < kRowRun; ++e) {
+                const int b = bin(x[e]);
+                take |= (x[e] > -kInf && b >= lo && b <= hi ? 1u : 0u) << e;
+            }
+            // few are taken: one place in the list after the other
+            while (take) {
+                const int e = __builtin_ctz(take);
+                take &= take - 1;
+                float v = x[0];
+#pragma unroll
+                for (int k = 1; k < kRowRun; ++k) v = e == k ? x[k] : v;
+                const uint32_t to = atomicAdd(&s.listed, 1u);
+                if (to < kList) s.list[to] = (uint64_t)key_of(v) << 32 | (uint32_t)(at + e);
+            }
+        });
+        __syncthreads();
+        const int n = (int)s.listed;
+        if (n > kList) return n;
+        int size = 2;
+        while (size < n) size *= 2;
+        for (int i = n + threadIdx.x; i < size; i += kThreads) s.list[i] = ~0ull;
+        // ascending keys, then indexes: by merging runs of which every other one is the other way round
+        for (int run = 2; run <= size; run *= 2)
+            for (int step = run / 2; step > 0; step /= 2) {
+                __syncthreads();
+                for (int p = threadIdx.x; p < size / 2; p += kThreads) {
+                    const int i = p / step * 2 * step + p % step;
+                    const uint64_t a = s.list[i], b = s.list[i + step];
+                    if ((a > b) == ((i & run) == 0)) { s.list[i] = b; s.list[i + step] = a; }
+                }
+            }
+        __syncthreads();
+        return n;
+    }
+
+    __device__ __forceinline__ uint64_t listed_mass(int i, int n) const { return i < n ? mass(logit_of((uint32_t)(s.list[i] >> 32))) : 0; }
+
+    // The token of the list's first n at which the sum, from `before` on, satisfies `target`: s.place (of the list), s.sum
+    __device__ __forceinline__ void search(int n, uint64_t before, Target target, int turn) const
+    {
+        uint64_t m[kThreadList], own = 0, total;
+#pragma unroll
+        for (int k = 0; k < kThreadList; ++k) own += m[k] = listed_mass(threadIdx.x * kThreadList + k, n);
+        uint64_t run = before + sum_ahead(s, own, turn, &total);
+#pragma unroll
+        for (int k = 0; k < kThreadList; ++k) {
+            const uint64_t next = run + m[k];
+            if (m[k] > 0 && target(next) && !target(run)) { s.place = threadIdx.x * kThreadList + k; s.sum = next; }
+            run = next;
+        }
+        __syncthreads();
+    }
+
+    // The bin in which the sum satisfies `target`, or with count > 0 the one in which the count of tokens reaches it: s.place, and in
+    // s.before the sum, in s.sum the count in front of it.  Returns the count of all.
+    __device__ __forceinline__ int64_t search_bins(int64_t count, Target target, int turn) const
+    {
+        uint64_t total;
+        uint64_t m = 0, c = 0;
+        const int first = threadIdx.x * kThreadBins;
+#pragma unroll
+        for (int k = 0; k < kThreadBins; ++k) {
+            m += s.mass[first + k];
+            c += s.count[first + k];
+        }
+        m = sum_ahead(s, m, turn, &total);
+        __syncthreads();
+        c = sum_ahead(s, c, turn, &total);
+#pragma unroll
+        for (int k = 0; k < kThreadBins; ++k) {
+            const uint64_t m2 = m + s.mass[first + k], c2 = c + s.count[first + k];
+            if (count > 0 ? (int64_t)c < count && (int64_t)c2 >= count : target(m2) && !target(m)) { s.place = first + k; s.before = m; s.sum = c; }
+            m = m2; c = c2;
+        }
+        __syncthreads();
+        return (int64_t)total;
+    }
+
+    // The first element in descending order at which the count of elements reaches `count` (> 0), or the sum of masses satisfies `target`:
+    // by digits of the keys, of rows with many equal logits; leaves it in s.found
+    __device__ __forceinline__ void by_digits(int64_t count, Target target) const
     {
         uint32_t prefix = 0;
         uint64_t sum_before = 0;
         int64_t count_before = 0;
         for (int shift = 32 - kDigitBits; shift >= 0; shift -= kDigitBits) {
             __syncthreads();
-            for (int i = threadIdx.x; i < kDigits; i += kThreads) { hist_mass[i] = 0; hist_count[i] = 0; }
+            for (int i = threadIdx.x; i < kDigits; i += kThreads) { s.mass[i] = 0; s.count[i] = 0; }
             __syncthreads();
-            for (int64_t i = threadIdx.x; i < L.vocab; i += kThreads) {
+            for (int i = threadIdx.x; i < vocab; i += kThreads) {
                 const float x = logit(i);
                 const uint32_t key = key_of(x);
                 if (shift + kDigitBits < 32 && key >> (shift + kDigitBits) != prefix) continue;
                 const int d = key >> shift & (kDigits - 1);
-                atomicAdd(&hist_count[d], 1u);
-                atomicAdd((unsigned long long*)&hist_mass[d], (unsigned long long)mass_of(x, largest, temperature));
+                atomicAdd(&s.count[d], 1u);
+                atomicAdd((unsigned long long*)&s.mass[d], (unsigned long long)mass(x));
             }
             __syncthreads();
             if (threadIdx.x == 0) {
@@ -70,128 +310,273 @@ struct Row {
                 uint64_t m = sum_before;
                 int64_t c = count_before;
                 for (; d < kDigits - 1; ++d) {
-                    const uint64_t m2 = m + hist_mass[d];
-                    const int64_t c2 = c + hist_count[d];
-                    if (hist_count[d] && (count > 0 ? c2 >= count : beyond ? (double)m2 > target : (double)m2 >= target)) break;
+                    const uint64_t m2 = m + s.mass[d];
+                    const int64_t c2 = c + s.count[d];
+                    if (s.count[d] && (count > 0 ? c2 >= count : target(m2))) break;
                     m = m2; c = c2;
                 }
-                found->key = (uint32_t)d; found->nth = c; found->sum = m;
+                s.found.key = (uint32_t)d; s.found.nth = c; s.found.sum = m;
             }
             __syncthreads();
-            prefix = prefix << kDigitBits | found->key;
-            count_before = found->nth;
-            sum_before = found->sum;
+            prefix = prefix << kDigitBits | s.found.key;
+            count_before = s.found.nth;
+            sum_before = s.found.sum;
         }
         // equal elements have equal masses
-        const uint64_t m = mass_of(logit_of(prefix), largest, temperature);
+        const uint64_t m = mass(logit_of(prefix));
         int64_t nth = 1;
-        const int64_t equal = hist_count[prefix & (kDigits - 1)];
+        const int64_t equal = s.count[prefix & (kDigits - 1)];
         if (count > 0) {
             nth = count - count_before;
         } else if (m > 0) {
-            const double before = (double)sum_before;
-            nth = (int64_t)((target - before) / (double)m);
+            nth = (int64_t)((target.value - (double)sum_before) / (double)m);
             nth = nth < 1 ? 1 : nth > equal ? equal : nth;
-            auto enough = [&](int64_t n) {
-                const double s = (double)(sum_before + (uint64_t)n * m);
-                return beyond ? s > target : s >= target;
-            };
-            while (nth > 1 && enough(nth - 1)) --nth;
-            while (nth < equal && !enough(nth)) ++nth;
+            while (nth > 1 && target(sum_before + (uint64_t)(nth - 1) * m)) --nth;
+            while (nth < equal && !target(sum_before + (uint64_t)nth * m)) ++nth;
         }
-        return {prefix, nth, sum_before + (uint64_t)nth * m};
+        __syncthreads();
+        if (threadIdx.x == 0) s.found = {prefix, nth, sum_before + (uint64_t)nth * m};
+        __syncthreads();
+    }
+
+    // Index of the nth of the elements with a key, in s.place: wavefronts take parts of the row one behind the other.
+    __device__ __forceinline__ void nth_of(uint32_t key, int64_t nth) const
+    {
+        const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+        const int part = (vocab + kThreads - 1) / kThreads * 64, begin = wave * part, end = begin + part < vocab ? begin + part : vocab;
+        int64_t count = 0;
+        for (int i = begin; i < end; i += 64) count += __popcll(__ballot(i + lane < end && key_of(logit(i + lane < end ? i + lane : begin)) == key));
+        __syncthreads();
+        if (lane == 0) s.wave_equal[wave] = (uint32_t)count;
+        __syncthreads();
+        int64_t before = 0;
+        for (int w = 0; w < wave; ++w) before += s.wave_equal[w];
+        if (before < nth && nth <= before + count)
+            for (int i = begin; i < end; i += 64) {
+                const bool equal = i + lane < end && key_of(logit(i + lane < end ? i + lane : begin)) == key;
+                const uint64_t mask = __ballot(equal);
+                const int ahead = __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+                if (equal && before + ahead + 1 == nth) s.place = i + lane;
+                before += __popcll(mask);
+            }
+        __syncthreads();
     }
 };
 
-__global__ void __launch_bounds__(kThreads) k_sample(SampleLaunch L)
+// what the filters keep by mass, and the draw
+__device__ __forceinline__ double least_mass(const RowFilters& f) { return (f.min_p < 1.0 ? f.min_p : 1.0) * 0x1p40; }
+__device__ __forceinline__ Target target_p(const RowFilters& f, uint64_t sum)
 {
-    __shared__ uint64_t hist_mass[kDigits];
-    __shared__ uint32_t hist_count[kDigits];
-    __shared__ Found found;
-    __shared__ uint32_t wave_key[kWaves], wave_equal[kWaves], wave_nan[kWaves];
-    __shared__ uint64_t kept;
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    for (int64_t row = blockIdx.x; row < L.rows; row += gridDim.x) {
-        const double temperature = L.filters.temperatures ? (double)global(L.filters.temperatures)[row] : (double)L.filters.temperature;
-        const int32_t top_k = L.filters.top_ks ? global(L.filters.top_ks)[row] : L.filters.top_k;
-        const double top_p = L.filters.top_ps ? (double)global(L.filters.top_ps)[row] : (double)L.filters.top_p;
-        const double min_p = L.filters.min_ps ? (double)global(L.filters.min_ps)[row] : (double)L.filters.min_p;
-        Row r{L, row * L.logits_stride, 0.0f, temperature, hist_mass, hist_count, &found};
-        uint32_t smallest = ~0u;
-        bool nan = false;
-        for (int64_t i = threadIdx.x; i < L.vocab; i += kThreads) {
-            const float x = r.logit(i);
-            nan |= x != x;
-            const uint32_t k = key_of(x);
-            smallest = smallest < k ? smallest : k;
-        }
-        for (int k = 32; k > 0; k /= 2) {
-            const uint32_t other = (uint32_t)__shfl_xor((int)smallest, k);
-            smallest = smallest < other ? smallest : other;
-        }
-        const bool any_nan = __ballot(nan) != 0;
-        __syncthreads();
-        if (lane == 0) { wave_key[wave] = smallest; wave_nan[wave] = any_nan; }
-        if (threadIdx.x == 0) kept = 0;
-        __syncthreads();
-        bool none = !(temperature >= 0.0 && temperature < (double)__builtin_inff());
-        for (int w = 0; w < kWaves; ++w) {
-            smallest = smallest < wave_key[w] ? smallest : wave_key[w];
-            none |= wave_nan[w] != 0;
-        }
-        r.largest = logit_of(smallest);
-        none |= r.largest == -__builtin_inff();
-        int64_t token = -1;
-        if (!none) {
-            Found at{smallest, 1, 0};
-            if (temperature > 0.0) {
-                uint64_t total = 0, least = 0;
-                for (int64_t i = threadIdx.x; i < L.vocab; i += kThreads) {
-                    const uint64_t m = mass_of(r.logit(i), r.largest, temperature);
-                    total += m;
-                    if (!(min_p > 0.0) || (double)m >= (min_p < 1.0 ? min_p : 1.0) * 0x1p40) least += m;
-                }
-                atomicAdd((unsigned long long*)&kept, (unsigned long long)total);
-                __syncthreads();
-                uint64_t sum = kept;
-                __syncthreads();
-                if (threadIdx.x == 0) kept = 0;
-                __syncthreads();
-                atomicAdd((unsigned long long*)&kept, (unsigned long long)least);
-                __syncthreads();
-                const uint64_t sum_least = kept;
-                if (top_k > 0 && top_k < L.vocab) sum = r.find(top_k, 0.0, false).sum;
-                if (top_p < 1.0) sum = r.find(0, (top_p > 0.0 ? top_p : 0.0) * (double)sum, false).sum;
-                sum = sum < sum_least ? sum : sum_least;
-                float u = global(L.u)[row];
-                u = !(u > 0.0f) ? 0.0f : u < 1.0f ? u : 0x1.fffffep-1f;
-                at = r.find(0, (double)u * (double)sum, true);
-            }
-            // the nth of the elements with this key: wavefronts take parts of the row one behind the other
-            const int64_t part = (L.vocab + kThreads - 1) / kThreads * 64, begin = wave * part, end = begin + part < L.vocab ? begin + part : L.vocab;
-            int64_t count = 0;
-            for (int64_t i0 = begin; i0 < end; i0 += 64) count += __popcll(__ballot(i0 + lane < end && key_of(r.logit(i0 + lane < end ? i0 + lane : 0)) == at.key));
-            if (lane == 0) wave_equal[wave] = (uint32_t)count;
+    const double v = (f.top_p > 0.0 ? f.top_p : 0.0) * (double)sum;
+    return {v > 1.0 ? v : 1.0, false};          // at least one
+}
+__device__ __forceinline__ Target target_u(const RowFilters& f, uint64_t sum) { return {(double)f.u * (double)sum, true}; }
+
+// The token of a row whose largest logit is known.  `last` >= 0: all tokens that can be drawn lie in the bins 0 to last.
+// Three sums are asked for one after the other, each only where its filter is: that of the first top_k, that of those that top_p leaves, and
+// the token's.
+template <int LT, bool SHORT>
+__device__ __forceinline__ int64_t draw(const Row<LT, SHORT>& r, const RowFilters& f, int last)
+{
+    Shared& s = r.s;
+    const bool counts = f.top_k > 0;
+    bool all_listed = false;        // the list holds all that can be drawn
+    bool binned = true;             // s.mass, s.count hold the bins
+    bool in_list = false;
+    int n = 0, kept = 0;
+    uint64_t sum = 0;
+#pragma unroll 1
+    for (int ask = last >= 0 ? 0 : 1; ask <= 3; ++ask) {
+        int lo = 0, hi = last;
+        uint64_t before = 0, ahead = 0;
+        Target target{};
+        if (ask == 1) {
+            if (all_listed) continue;
             __syncthreads();
-            int64_t before = 0;
-            for (int w = 0; w < wave; ++w) before += wave_equal[w];
-            if (before < at.nth && at.nth <= before + count) {
-                for (int64_t i0 = begin; i0 < end; i0 += 64) {
-                    const bool equal = i0 + lane < end && key_of(r.logit(i0 + lane < end ? i0 + lane : 0)) == at.key;
-                    const uint64_t mask = __ballot(equal);
-                    const int ahead = __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
-                    if (equal && before + ahead + 1 == at.nth) {
-                        if (L.token_bytes == 4) global(static_cast<int32_t*>(L.out))[row] = (int32_t)(i0 + lane);
-                        else global(static_cast<int64_t*>(L.out))[row] = i0 + lane;
+            for (int i = threadIdx.x; i < kBins; i += kThreads) { s.mass[i] = 0; s.count[i] = 0; }
+            __syncthreads();
+            uint64_t own = 0, own_least = 0;
+            r.each([&](f8 x, int) {
+#pragma unroll
+                for (int e = 0; e < kRowRun; ++e) {
+                    if (x[e] > -kInf) {
+                        const int b = r.bin(x[e]);
+                        const uint64_t m = r.mass(x[e]);
+                        if (counts) atomicAdd(&s.count[b], 1u);
+                        if (m > 0) atomicAdd((unsigned long long*)&s.mass[b], (unsigned long long)m);
+                        own += m;
+                        if ((double)m >= least_mass(f)) own_least += m;
                     }
-                    before += __popcll(mask);
+                    __builtin_amdgcn_sched_barrier(0);          // one after the other: 16 at once would not fit the registers
                 }
-            }
-        } else if (threadIdx.x == 0) {
-            if (L.token_bytes == 4) global(static_cast<int32_t*>(L.out))[row] = (int32_t)token;
-            else global(static_cast<int64_t*>(L.out))[row] = token;
-            atomicOr(L.status, QADAM_STATUS_NO_TOKEN);
+            });
+            __syncthreads();
+            sum_ahead(s, own, 0, &sum);
+            uint64_t least;
+            sum_ahead(s, own_least, 1, &least);
+            if (threadIdx.x == 0) s.least = least;
+            if (!counts) continue;
+        } else if (ask == 2) {
+            if (!(f.top_p < 1.0)) continue;
+            target = target_p(f, sum);
+        } else if (ask == 3) {
+            __syncthreads();
+            if (f.min_p > 0.0 && s.least < sum) sum = s.least;
+            target = target_u(f, sum);
         }
+        if (ask > 0 && binned && !all_listed) {
+            const int64_t count = ask == 1 ? f.top_k : 0;
+            if (r.search_bins(count, target, 0) < count) continue;          // fewer tokens than top_k
+            lo = hi = (int)s.place;
+            before = s.before;
+            ahead = s.sum;
+        }
+        if (binned && !all_listed) n = r.collect(lo, hi);
+        if (binned && n <= kList) {
+            if (ask < 2) {
+                // the sum of the list's first ones, and of those of them that reach min_p
+                const int64_t rest = f.top_k - (int64_t)ahead;
+                kept = counts && rest < n ? (int)rest : n;
+                uint64_t own = 0, own_least = 0, total;
+#pragma unroll
+                for (int k = 0; k < kThreadList; ++k) {
+                    const uint64_t m = r.listed_mass(threadIdx.x * kThreadList + k, kept);
+                    own += m;
+                    if ((double)m >= least_mass(f)) own_least += m;
+                }
+                sum_ahead(s, own, 0, &total);
+                sum = before + total;
+                if (ask == 0) {
+                    sum_ahead(s, own_least, 1, &total);
+                    if (threadIdx.x == 0) s.least = total;
+                    all_listed = true;
+                }
+                __syncthreads();
+            } else {
+                r.search(all_listed ? kept : n, before, target, ask & 1);
+                sum = s.sum;
+                in_list = true;
+                __syncthreads();
+            }
+        } else if (ask > 0) {
+            binned = in_list = false;
+            r.by_digits(ask == 1 ? f.top_k : 0, target);
+            sum = s.found.sum;
+        }
+    }
+    if (in_list) return (int64_t)(uint32_t)s.list[s.place];
+    r.nth_of(s.found.key, s.found.nth);
+    return s.place;
+}
+
+// The largest or smallest of a wavefront's values, the same in all lanes; none is NaN where it counts
+template <bool LARGEST, int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ float extreme(float x)
+{
+    const int own = __builtin_bit_cast(int, x);
+    const float other = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(own, own, CTRL, ROWS, 0xf, false));
+    return LARGEST ? fmaxf(x, other) : fminf(x, other);
+}
+
+template <bool LARGEST>
+__device__ __forceinline__ float wave_extreme(float x)
+{
+    x = extreme<LARGEST, 0xb1>(x);
+    x = extreme<LARGEST, 0x4e>(x);
+    x = extreme<LARGEST, 0x141>(x);
+    x = extreme<LARGEST, 0x140>(x);
+    x = extreme<LARGEST, 0x142, 0xa>(x);
+    x = extreme<LARGEST, 0x143, 0xc>(x);
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+
+template <int LT, bool SHORT>
+__global__ void __launch_bounds__(kThreads) k_sample(SampleLaunch L, int64_t first_row)
+{
+    __shared__ Shared s;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int64_t row = first_row + blockIdx.x;
+    // in LDS: not all of it would fit the registers of 16 wavefronts
+    const RowFilters& f = s.filters;
+    if (threadIdx.x == 0) {
+        RowFilters own;
+        own.temperature = L.filters.temperatures ? (double)global(L.filters.temperatures)[row] : (double)L.filters.temperature;
+        own.top_k = L.filters.top_ks ? global(L.filters.top_ks)[row] : L.filters.top_k;
+        own.top_p = L.filters.top_ps ? (double)global(L.filters.top_ps)[row] : (double)L.filters.top_p;
+        own.min_p = L.filters.min_ps ? (double)global(L.filters.min_ps)[row] : (double)L.filters.min_p;
+        own.u = global(L.u)[row];
+        own.u = !(own.u > 0.0f) ? 0.0f : own.u < 1.0f ? own.u : 0x1.fffffep-1f;
+        if (!(own.top_k > 0 && own.top_k < L.vocab)) own.top_k = 0;
+        s.filters = own;
+    }
+    Row<LT, SHORT> r{s, static_cast<const typename Element<LT>::T*>(L.logits) + row * L.logits_stride, (int)L.vocab, {}, {}};
+
+    // largest, smallest that is no minus infinity, NaN
+    float high = -kInf, low = kInf;
+    bool nan = false;
+    r.each([&](f8 x, int) {
+#pragma unroll
+        for (int e = 0; e < kRowRun; ++e) {
+            nan |= x[e] != x[e];
+            high = fmaxf(high, x[e]);
+            low = fminf(low, x[e] == -kInf ? kInf : x[e]);
+        }
+    });
+    float all_high = wave_extreme<true>(high), all_low = wave_extreme<false>(low);
+    const bool any_nan = __ballot(nan) != 0;
+    __syncthreads();
+    if (lane == 0) { s.wave_key[wave] = __builtin_bit_cast(uint32_t, all_high); s.wave_low[wave] = __builtin_bit_cast(uint32_t, all_low); s.wave_nan[wave] = any_nan; }
+    __syncthreads();
+    bool none = !(f.temperature >= 0.0 && f.temperature < (double)kInf);
+    for (int w = 0; w < kWaves; ++w) {
+        all_high = fmaxf(all_high, __builtin_bit_cast(float, s.wave_key[w]));
+        all_low = fminf(all_low, __builtin_bit_cast(float, s.wave_low[w]));
+        none |= s.wave_nan[w] != 0;
+    }
+    all_high += 0.0f;
+    none |= all_high == -kInf;
+    int64_t token = -1;
+    if (!none && f.temperature == 0.0) {
+        // the lowest index of the largest
+        if (threadIdx.x == 0) s.first = ~0u;
+        __syncthreads();
+        uint32_t first = ~0u;
+        r.each([&](f8 x, int at) {
+#pragma unroll
+            for (int e = kRowRun - 1; e >= 0; --e)
+                if (x[e] == all_high && (uint32_t)(at + e) < first) first = (uint32_t)(at + e);
+        });
+        if (first != ~0u) atomicMin(&s.first, first);
+        __syncthreads();
+        token = s.first;
+    } else if (!none) {
+        const double log2e = 0x1.71547652b82fep+0;
+        r.mass = {all_high, log2e / f.temperature};
+        // bins down to where masses vanish, 29 temperatures below the largest, or to the smallest logit; any scale is right
+        const float range = fminf(29.0f * (float)f.temperature, all_high < kInf ? all_high - all_low : 1.0f);
+        const float scale = (float)(kBins - 1) / range;
+        r.bin = {all_high, scale < 1e30f ? scale : 1e30f};
+        const bool by_k = f.top_k > 0 && f.top_k <= kThreads, by_min_p = !by_k && f.top_k == 0 && !(f.top_p < 1.0) && f.min_p > 0.0;
+        int last = -1;
+        if (by_k) {
+            for (int i = threadIdx.x; i < kBins; i += kThreads) { s.mass[i] = 0; s.count[i] = 0; }
+            __syncthreads();
+            atomicAdd(&s.count[r.bin(high)], 1u);
+            __syncthreads();
+            r.search_bins(f.top_k, {}, 0);
+            last = (int)s.place;
+        } else if (by_min_p) {
+            // where masses reach min_p, which they may by being rounded up, and a bin more for the roundings of both sides
+            const double least = (f.min_p < 1.0 ? f.min_p : 1.0) - 0x1p-40;
+            const float below = least > 0.0 ? (float)(-log(least) * f.temperature) * 1.0001f : kInf;
+            last = (int)fminf(below * r.bin.per_unit, (float)(kBins - 1)) + 1;
+        }
+        token = draw(r, f, last);
+    }
+    if (threadIdx.x == 0) {
+        if (L.token_bytes == 4) global(static_cast<int32_t*>(L.out))[row] = (int32_t)token;
+        else global(static_cast<int64_t*>(L.out))[row] = token;
+        if (token < 0) atomicOr(L.status, QADAM_STATUS_NO_TOKEN);
     }
 }
 
@@ -199,7 +584,14 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleLaunch L)
 
 hipError_t launch_sample(const SampleLaunch& L)
 {
-    k_sample<<<dim3((int)(L.rows < 65536 ? L.rows : 65536)), dim3(kThreads), 0, L.stream>>>(L);
+    // rows of a launch: fewer than 2^32 work-items
+    for (int64_t row = 0; row < L.rows; row += 1 << 21) {
+        const dim3 grid((int)(L.rows - row < 1 << 21 ? L.rows - row : 1 << 21));
+        auto run = [&](auto kernel) { kernel<<<grid, dim3(kThreads), 0, L.stream>>>(L, row); };
+        if (L.logits_type == QADAM_F32) L.vocab < kRowRun ? run(k_sample<QADAM_F32, true>) : run(k_sample<QADAM_F32, false>);
+        else if (L.logits_type == QADAM_BF16) L.vocab < kRowRun ? run(k_sample<QADAM_BF16, true>) : run(k_sample<QADAM_BF16, false>);
+        else L.vocab < kRowRun ? run(k_sample<QADAM_F16, true>) : run(k_sample<QADAM_F16, false>);
+    }
     return hipGetLastError();
 }
 
