@@ -506,8 +506,8 @@ int qadam_linear8_forward(qadam_linear8_t h, int64_t num_tokens, const void* x, 
  *     top_p < 1      of those the fewest, but one at least, whose masses' sum reaches top_p of all of theirs;
  *     min_p > 0      of those the ones whose mass reaches min_p 2^40;
  * of the kept masses' sum S, the token is the first one at which the sum so far is beyond u S (comparisons in fp64).  temperature = 0:
- * the largest logit, the lowest index among equals.  Logits of minus infinity have no mass; where the largest is infinite, the
- * logits equal to it have all of it.  u below 0 or NaN counts as 0, from 1 on as the largest fp32 below 1.
+ * the largest logit, the lowest index among equals.  Logits of minus infinity have no mass, those of infinity count as the largest fp32.
+ * u below 0 or NaN counts as 0, from 1 on as the largest fp32 below 1.
  * A row without a token (a NaN among its logits, all logits minus infinity, a temperature that is negative, infinite or NaN) gives -1 and sets
  * QADAM_STATUS_NO_TOKEN in the handle's status word. */
 typedef struct qadam_sampler_ctx* qadam_sampler_t;

@@ -5,11 +5,11 @@
 // same in any order: workgroups add them in LDS with atomics and the result is the same on every run.  The logits are sorted into
 // kBins bins of equal width, from the largest on down to where masses vanish.  Bins are in the order of the logits, so that a sum is
 // found by looking through the bins and then through one bin's tokens, which are few and are sorted:
-//   * top_k up to 1024: the largest logit of each thread gives a bin that at least top_k tokens lie in or in front of; those (a few more than
+//   * top_k up to kMostTopK: the largest logit of each thread gives a bin that at least top_k tokens lie in or in front of; those (a few more than
 //     top_k) are sorted, and no mass of another token is taken.  The same where min_p is the only filter: it names the bin;
 //   * else the masses of all tokens are added by bins (about 20 operations in fp64 each, which is most of the time), and each of
 //     the sums that are asked for takes one more pass, which collects a bin's tokens;
-//   * tokens of a bin that are more than kList (thousands of equal logits): by digits of the logits, a pass for each.
+//   * tokens of a bin that are more than kList (2048, that is many equal logits): by digits of the logits, a pass for each.
 #include "qadam_layers.h"
 #include "qadam_row.h"
 
@@ -19,8 +19,9 @@ namespace {
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kDigitBits = 8, kDigits = 1 << kDigitBits;
 constexpr int kBins = 2048, kThreadBins = kBins / kThreads;
-constexpr int kList = 4096, kThreadList = kList / kThreads;
-constexpr int kLoads = 2;               // runs of a thread under way together
+constexpr int kList = 2048, kThreadList = kList / kThreads;
+constexpr int kPairs = 512;             // tokens of a list that are ordered by comparing pairs
+constexpr int kMostTopK = 512;          // top_k up to which the threads' largest logits name the candidates
 
 // Order of logits as integers: the largest logit has the smallest key, equal logits (0 and -0 too) the same one.
 __device__ __forceinline__ uint32_t key_of(float x)
@@ -36,33 +37,33 @@ __device__ __forceinline__ float logit_of(uint32_t key)
 
 constexpr float kInf = __builtin_inff();
 
-// round(2^40 exp((x - largest) / temperature)): 2^y = 2^n e^r with n = round(y) and |r| up to log(2) / 2, e^r by its series up to r^12 / 12!,
-// whose rest is below 2^-52.
+constexpr float kMost = 0x1.fffffep+127f;       // infinite logits count as this
+
+// round(2^40 exp((x - largest) / temperature)): 2^y = 2^n 2^r with n = round(y) and r from -1/2 to 1/2, where the polynomial of degree 9 that
+// meets 2^r at the ten Chebyshev nodes is within 2^-45 of it: a fortieth of a unit.  Beside 1.5 2^52 the last place of a number is 1, so
+// that adding it rounds, and leaves n in the lower bits.
 struct Mass {
     float largest;
     double per_unit;        // log2(e) / temperature
 
     __device__ __forceinline__ uint64_t operator()(float x) const
     {
-        if (x == largest) return (uint64_t)1 << 40;         // both may be infinite
-        const double y = ((double)x - (double)largest) * per_unit;
-        if (!(y > -42.0)) return 0;                         // below half a unit
-        const double n = rint(y), r = (y - n) * 0x1.62e42fefa39efp-1;
-        double e = 1.0 / 479001600.0;
-        e = __builtin_fma(e, r, 1.0 / 39916800.0);
-        e = __builtin_fma(e, r, 1.0 / 3628800.0);
-        e = __builtin_fma(e, r, 1.0 / 362880.0);
-        e = __builtin_fma(e, r, 1.0 / 40320.0);
-        e = __builtin_fma(e, r, 1.0 / 5040.0);
-        e = __builtin_fma(e, r, 1.0 / 720.0);
-        e = __builtin_fma(e, r, 1.0 / 120.0);
-        e = __builtin_fma(e, r, 1.0 / 24.0);
-        e = __builtin_fma(e, r, 1.0 / 6.0);
-        e = __builtin_fma(e, r, 0.5);
-        e = __builtin_fma(e, r, 1.0);
-        e = __builtin_fma(e, r, 1.0);
-        // up to 2^40; beside 2^52 the last place is 1
-        const double m = ldexp(e, (int)n + 40) + 0x1p52;
+        constexpr double kRound = 0x1.8p52;
+        const double y = fmax(((double)x - (double)largest) * per_unit, -100.0);
+        const double rounded = y + kRound, r = y - (rounded - kRound);
+        double e = 0x1.b6571dbf753eep-24;
+        e = __builtin_fma(e, r, 0x1.63ef969af1055p-20);
+        e = __builtin_fma(e, r, 0x1.ffcb7678c7b33p-17);
+        e = __builtin_fma(e, r, 0x1.43088e257ed10p-13);
+        e = __builtin_fma(e, r, 0x1.5d87fe908f74fp-10);
+        e = __builtin_fma(e, r, 0x1.3b2ab72b175efp-7);
+        e = __builtin_fma(e, r, 0x1.c6b08d704411ap-5);
+        e = __builtin_fma(e, r, 0x1.ebfbdff8149f2p-3);
+        e = __builtin_fma(e, r, 0x1.62e42fefa39f7p-1);
+        e = __builtin_fma(e, r, 0x1.000000000003dp+0);
+        // e is above 2^-1 and below 2^1, n + 40 from -60 to 40: an addition to the exponent
+        const uint64_t bits = __builtin_bit_cast(uint64_t, e) + ((uint64_t)(uint32_t)((int)(uint32_t)__builtin_bit_cast(uint64_t, rounded) + 40) << 52);
+        const double m = __builtin_bit_cast(double, bits) + 0x1p52;
         return __builtin_bit_cast(uint64_t, m) & 0xfffffffffffffull;
     }
 };
@@ -71,11 +72,7 @@ struct Mass {
 struct Bin {
     float largest, per_unit;
 
-    __device__ __forceinline__ int operator()(float x) const
-    {
-        const float d = x == largest ? 0.0f : largest - x;
-        return (int)fminf(d * per_unit, (float)(kBins - 1));
-    }
+    __device__ __forceinline__ int operator()(float x) const { return (int)fminf((largest - x) * per_unit, (float)(kBins - 1)); }
 };
 
 struct Found {
@@ -101,7 +98,9 @@ struct Shared {
     RowFilters filters;
     uint64_t mass[kBins];
     uint32_t count[kBins];
-    uint64_t list[kList];
+    uint64_t list[kList];       // key << 32 | index: smaller in front
+    uint64_t run[kList];        // sum of the masses of the list's up to this one and with it
+    uint16_t rank[kList];       // its place in the order, from 1 on
     uint64_t wave_sum[2][kWaves];
     uint32_t wave_key[kWaves], wave_low[kWaves], wave_nan[kWaves], wave_equal[kWaves];
     uint64_t least;             // sum of the masses that reach min_p
@@ -155,7 +154,7 @@ struct Row {
     Mass mass;
     Bin bin;
 
-    __device__ __forceinline__ float logit(int i) const { return (float)global(logits)[i]; }
+    __device__ __forceinline__ float logit(int i) const { return fminf((float)global(logits)[i], kMost); }
 
     // kRowRun logits from `start` on; minus infinity in front of `from`, where another thread has them, and behind the row's end
     __device__ __forceinline__ typename Run<LT, kRowRun>::V load(int from, int* start) const
@@ -176,29 +175,27 @@ struct Row {
         return raw;
     }
 
-    // body(run of logits, index of the first): all of the row
+    // body(run of logits, index of the first): all of the row, a thread's next run under way meanwhile
     template <typename F>
     __device__ __forceinline__ void each(F&& body) const
     {
         constexpr int kAcross = kThreads * kRowRun;
+        int at = threadIdx.x * kRowRun, next_start = 0;
+        if (at >= vocab) return;
+        typename Run<LT, kRowRun>::V next = load(at, &next_start);
 #pragma unroll 1
-        for (int at = threadIdx.x * kRowRun; at < vocab; at += kLoads * kAcross) {
-            typename Run<LT, kRowRun>::V raw[kLoads];
-            int start[kLoads];
-#pragma unroll
-            for (int k = 0; k < kLoads; ++k) {
-                raw[k] = (T)-kInf;
-                start[k] = 0;
-                if (at + k * kAcross < vocab) raw[k] = load(at + k * kAcross, &start[k]);
-            }
-#pragma unroll
-            for (int k = 0; k < kLoads; ++k)
-                if (at + k * kAcross < vocab) body(to_float<LT, kRowRun>(raw[k]), start[k]);
+        while (true) {
+            const f8 x = to_float<LT, kRowRun>(next);
+            const int start = next_start;
+            at += kAcross;
+            if (at < vocab) next = load(at, &next_start);
+            body(x, start);
+            if (at >= vocab) return;
         }
     }
 
-    // The tokens of the bins lo to hi (never those that are minus infinity) into the list, in descending order; their number, which may
-    // be beyond kList: then there is no list.
+    // The tokens of the bins lo to hi (never those that are minus infinity) into the list, with their places in the order and the sums up
+    // to them; their number, which may be beyond kList: then there is no list.
     __device__ __forceinline__ int collect(int lo, int hi) const
     {
         __syncthreads();
@@ -208,8 +205,8 @@ struct Row {
             uint32_t take = 0;
 #pragma unroll
             for (int e = 0; e < kRowRun; ++e) {
-                const int b = bin(x[e]);
-                take |= (x[e] > -kInf && b >= lo && b <= hi ? 1u : 0u) << e;
+                x[e] = fminf(x[e], kMost);
+                take |= ((uint32_t)(bin(x[e]) - lo) <= (uint32_t)(hi - lo) && x[e] > -kInf ? 1u : 0u) << e;
             }
             // few are taken: one place in the list after the other
             while (take) {
@@ -225,10 +222,36 @@ struct Row {
         __syncthreads();
         const int n = (int)s.listed;
         if (n > kList) return n;
-        int size = 2;
+        if (n <= kPairs) {
+            // `share` threads for a token, each of which looks at a part of the others
+            if ((int)threadIdx.x < n) s.run[threadIdx.x] = listed_mass(threadIdx.x);
+            __syncthreads();
+            int share = 64;
+            while (share > 1 && share * n > kThreads) share /= 2;
+            const int i = threadIdx.x / share;
+            uint64_t sum = 0;
+            uint32_t rank = 0;
+            if (i < n) {
+                const uint64_t own = s.list[i];
+                for (int j = threadIdx.x % share; j < n; j += share) {
+                    const bool ahead = s.list[j] <= own;
+                    sum += ahead ? s.run[j] : 0;
+                    rank += ahead;
+                }
+            }
+            for (int k = 1; k < share; k *= 2) {
+                sum += (uint64_t)(uint32_t)__shfl_xor((int)(sum >> 32), k) << 32 | (uint32_t)__shfl_xor((int)(uint32_t)sum, k);
+                rank += (uint32_t)__shfl_xor((int)rank, k);
+            }
+            __syncthreads();
+            if (i < n && threadIdx.x % share == 0) { s.run[i] = sum; s.rank[i] = (uint16_t)rank; }
+            __syncthreads();
+            return n;
+        }
+        // sorted: by merging runs of which every other one is the other way round
+        int size = 2 * kPairs;
         while (size < n) size *= 2;
         for (int i = n + threadIdx.x; i < size; i += kThreads) s.list[i] = ~0ull;
-        // ascending keys, then indexes: by merging runs of which every other one is the other way round
         for (int run = 2; run <= size; run *= 2)
             for (int step = run / 2; step > 0; step /= 2) {
                 __syncthreads();
@@ -239,50 +262,51 @@ struct Row {
                 }
             }
         __syncthreads();
+        uint64_t m[kThreadList], own = 0, total;
+#pragma unroll
+        for (int k = 0; k < kThreadList; ++k) {
+            const int i = threadIdx.x * kThreadList + k;
+            own += m[k] = i < n ? listed_mass(i) : 0;
+        }
+        uint64_t sum = sum_ahead(s, own, 0, &total);
+#pragma unroll
+        for (int k = 0; k < kThreadList; ++k) {
+            const int i = threadIdx.x * kThreadList + k;
+            s.run[i] = sum += m[k];
+            s.rank[i] = (uint16_t)(i + 1);
+        }
+        __syncthreads();
         return n;
     }
 
-    __device__ __forceinline__ uint64_t listed_mass(int i, int n) const { return i < n ? mass(logit_of((uint32_t)(s.list[i] >> 32))) : 0; }
+    __device__ __forceinline__ uint64_t listed_mass(int i) const { return mass(logit_of((uint32_t)(s.list[i] >> 32))); }
 
-    // The token of the list's first n at which the sum, from `before` on, satisfies `target`: s.place (of the list), s.sum
-    __device__ __forceinline__ void search(int n, uint64_t before, Target target, int turn) const
+    // The token of the list at which the sum, from `before` on, satisfies `target`: s.place (of the list), s.sum
+    __device__ __forceinline__ void search(int n, uint64_t before, Target target) const
     {
-        uint64_t m[kThreadList], own = 0, total;
-#pragma unroll
-        for (int k = 0; k < kThreadList; ++k) own += m[k] = listed_mass(threadIdx.x * kThreadList + k, n);
-        uint64_t run = before + sum_ahead(s, own, turn, &total);
-#pragma unroll
-        for (int k = 0; k < kThreadList; ++k) {
-            const uint64_t next = run + m[k];
-            if (m[k] > 0 && target(next) && !target(run)) { s.place = threadIdx.x * kThreadList + k; s.sum = next; }
-            run = next;
+        for (int i = threadIdx.x; i < n; i += kThreads) {
+            const uint64_t m = listed_mass(i), to = before + s.run[i];
+            if (m > 0 && target(to) && !target(to - m)) { s.place = i; s.sum = to; }
         }
         __syncthreads();
     }
 
-    // The bin in which the sum satisfies `target`, or with count > 0 the one in which the count of tokens reaches it: s.place, and in
-    // s.before the sum, in s.sum the count in front of it.  Returns the count of all.
-    __device__ __forceinline__ int64_t search_bins(int64_t count, Target target, int turn) const
+    // The bin in which the sum of s.mass (or s.count) satisfies `target`: s.place, and in s.before the sum in front of it.  Returns the sum
+    // of all.
+    __device__ __forceinline__ uint64_t search_bins(bool counts, Target target, int turn) const
     {
-        uint64_t total;
-        uint64_t m = 0, c = 0;
+        uint64_t v[kThreadBins], own = 0, total;
         const int first = threadIdx.x * kThreadBins;
 #pragma unroll
-        for (int k = 0; k < kThreadBins; ++k) {
-            m += s.mass[first + k];
-            c += s.count[first + k];
-        }
-        m = sum_ahead(s, m, turn, &total);
-        __syncthreads();
-        c = sum_ahead(s, c, turn, &total);
+        for (int k = 0; k < kThreadBins; ++k) own += v[k] = counts ? s.count[first + k] : s.mass[first + k];
+        uint64_t run = sum_ahead(s, own, turn, &total);
 #pragma unroll
         for (int k = 0; k < kThreadBins; ++k) {
-            const uint64_t m2 = m + s.mass[first + k], c2 = c + s.count[first + k];
-            if (count > 0 ? (int64_t)c < count && (int64_t)c2 >= count : target(m2) && !target(m)) { s.place = first + k; s.before = m; s.sum = c; }
-            m = m2; c = c2;
+            if (target(run + v[k]) && !target(run)) { s.place = first + k; s.before = run; }
+            run += v[k];
         }
         __syncthreads();
-        return (int64_t)total;
+        return total;
     }
 
     // The first element in descending order at which the count of elements reaches `count` (> 0), or the sum of masses satisfies `target`:
@@ -364,7 +388,8 @@ struct Row {
 };
 
 // what the filters keep by mass, and the draw
-__device__ __forceinline__ double least_mass(const RowFilters& f) { return (f.min_p < 1.0 ? f.min_p : 1.0) * 0x1p40; }
+__device__ __forceinline__ uint64_t least_mass(const RowFilters& f) { return (uint64_t)ceil((f.min_p < 1.0 ? f.min_p : 1.0) * 0x1p40); }
+__device__ __forceinline__ Target target_count(int64_t count) { return {(double)count, false}; }
 __device__ __forceinline__ Target target_p(const RowFilters& f, uint64_t sum)
 {
     const double v = (f.top_p > 0.0 ? f.top_p : 0.0) * (double)sum;
@@ -379,85 +404,87 @@ template <int LT, bool SHORT>
 __device__ __forceinline__ int64_t draw(const Row<LT, SHORT>& r, const RowFilters& f, int last)
 {
     Shared& s = r.s;
-    const bool counts = f.top_k > 0;
+    const bool counts = f.top_k > 0, by_min_p = f.min_p > 0.0;
     bool all_listed = false;        // the list holds all that can be drawn
     bool binned = true;             // s.mass, s.count hold the bins
     bool in_list = false;
-    int n = 0, kept = 0;
+    int n = 0;
     uint64_t sum = 0;
 #pragma unroll 1
     for (int ask = last >= 0 ? 0 : 1; ask <= 3; ++ask) {
         int lo = 0, hi = last;
-        uint64_t before = 0, ahead = 0;
+        uint64_t before = 0;
+        int64_t rest = counts ? f.top_k : kList;        // tokens of the list whose sum is asked for
         Target target{};
-        if (ask == 1) {
+        if (ask < 2) {
             if (all_listed) continue;
             __syncthreads();
+            if (threadIdx.x == 0) s.least = 0;
+        }
+        if (ask == 1) {
             for (int i = threadIdx.x; i < kBins; i += kThreads) { s.mass[i] = 0; s.count[i] = 0; }
             __syncthreads();
-            uint64_t own = 0, own_least = 0;
+            const uint64_t least = by_min_p ? least_mass(f) : 0;
+            uint64_t own_least = 0;
             r.each([&](f8 x, int) {
 #pragma unroll
                 for (int e = 0; e < kRowRun; ++e) {
-                    if (x[e] > -kInf) {
-                        const int b = r.bin(x[e]);
-                        const uint64_t m = r.mass(x[e]);
-                        if (counts) atomicAdd(&s.count[b], 1u);
-                        if (m > 0) atomicAdd((unsigned long long*)&s.mass[b], (unsigned long long)m);
-                        own += m;
-                        if ((double)m >= least_mass(f)) own_least += m;
-                    }
-                    __builtin_amdgcn_sched_barrier(0);          // one after the other: 16 at once would not fit the registers
+                    const float v = fminf(x[e], kMost);
+                    const int b = r.bin(v);
+                    const uint64_t m = r.mass(v);
+                    if (counts) atomicAdd(&s.count[b], 1u);
+                    if (by_min_p) own_least += m >= least ? m : 0;
+                    if (m > 0) atomicAdd((unsigned long long*)&s.mass[b], (unsigned long long)m);
                 }
             });
+            if (by_min_p) atomicAdd((unsigned long long*)&s.least, (unsigned long long)own_least);
             __syncthreads();
-            sum_ahead(s, own, 0, &sum);
-            uint64_t least;
-            sum_ahead(s, own_least, 1, &least);
-            if (threadIdx.x == 0) s.least = least;
+            // all of them: no bin is asked for
+            sum = r.search_bins(false, {__builtin_inf(), false}, 0);
             if (!counts) continue;
+            target = target_count(f.top_k);
         } else if (ask == 2) {
             if (!(f.top_p < 1.0)) continue;
             target = target_p(f, sum);
         } else if (ask == 3) {
             __syncthreads();
-            if (f.min_p > 0.0 && s.least < sum) sum = s.least;
+            if (by_min_p && s.least < sum) sum = s.least;
             target = target_u(f, sum);
         }
         if (ask > 0 && binned && !all_listed) {
-            const int64_t count = ask == 1 ? f.top_k : 0;
-            if (r.search_bins(count, target, 0) < count) continue;          // fewer tokens than top_k
+            r.search_bins(ask == 1, target, 1);
             lo = hi = (int)s.place;
             before = s.before;
-            ahead = s.sum;
+            if (ask == 1) {
+                // the masses in front of the bin
+                rest = f.top_k - (int64_t)before;
+                uint64_t own = 0;
+#pragma unroll
+                for (int k = 0; k < kThreadBins; ++k) own += (int)threadIdx.x * kThreadBins + k < lo ? s.mass[threadIdx.x * kThreadBins + k] : 0;
+                sum_ahead(s, own, 0, &before);
+            }
         }
         if (binned && !all_listed) n = r.collect(lo, hi);
         if (binned && n <= kList) {
             if (ask < 2) {
-                // the sum of the list's first ones, and of those of them that reach min_p
-                const int64_t rest = f.top_k - (int64_t)ahead;
-                kept = counts && rest < n ? (int)rest : n;
-                uint64_t own = 0, own_least = 0, total;
-#pragma unroll
-                for (int k = 0; k < kThreadList; ++k) {
-                    const uint64_t m = r.listed_mass(threadIdx.x * kThreadList + k, kept);
-                    own += m;
-                    if ((double)m >= least_mass(f)) own_least += m;
-                }
-                sum_ahead(s, own, 0, &total);
-                sum = before + total;
-                if (ask == 0) {
-                    sum_ahead(s, own_least, 1, &total);
-                    if (threadIdx.x == 0) s.least = total;
-                    all_listed = true;
+                // the sum of the list's first ones, and of those of them that reach min_p; a list without one: no sum
+                if (threadIdx.x == 0) s.sum = 0;
+                __syncthreads();
+                const int kept = rest < n ? (int)rest : n;
+                for (int i = threadIdx.x; i < n; i += kThreads) {
+                    if (s.rank[i] == kept) s.sum = s.run[i];
+                    if (ask == 0 && by_min_p && s.rank[i] <= kept && r.listed_mass(i) >= least_mass(f))
+                        atomicMax((unsigned long long*)&s.least, (unsigned long long)s.run[i]);
                 }
                 __syncthreads();
+                sum = before + s.sum;
+                all_listed = ask == 0;
             } else {
-                r.search(all_listed ? kept : n, before, target, ask & 1);
+                r.search(n, before, target);
                 sum = s.sum;
                 in_list = true;
-                __syncthreads();
             }
+            __syncthreads();
         } else if (ask > 0) {
             binned = in_list = false;
             r.by_digits(ask == 1 ? f.top_k : 0, target);
@@ -533,7 +560,8 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleLaunch L, int64_t fir
         all_low = fminf(all_low, __builtin_bit_cast(float, s.wave_low[w]));
         none |= s.wave_nan[w] != 0;
     }
-    all_high += 0.0f;
+    all_high = fminf(all_high, kMost) + 0.0f;
+    all_low = fminf(all_low, kMost);
     none |= all_high == -kInf;
     int64_t token = -1;
     if (!none && f.temperature == 0.0) {
@@ -544,7 +572,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleLaunch L, int64_t fir
         r.each([&](f8 x, int at) {
 #pragma unroll
             for (int e = kRowRun - 1; e >= 0; --e)
-                if (x[e] == all_high && (uint32_t)(at + e) < first) first = (uint32_t)(at + e);
+                if (fminf(x[e], kMost) == all_high && (uint32_t)(at + e) < first) first = (uint32_t)(at + e);
         });
         if (first != ~0u) atomicMin(&s.first, first);
         __syncthreads();
@@ -553,17 +581,17 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleLaunch L, int64_t fir
         const double log2e = 0x1.71547652b82fep+0;
         r.mass = {all_high, log2e / f.temperature};
         // bins down to where masses vanish, 29 temperatures below the largest, or to the smallest logit; any scale is right
-        const float range = fminf(29.0f * (float)f.temperature, all_high < kInf ? all_high - all_low : 1.0f);
+        const float range = fminf(29.0f * (float)f.temperature, all_high - all_low);
         const float scale = (float)(kBins - 1) / range;
         r.bin = {all_high, scale < 1e30f ? scale : 1e30f};
-        const bool by_k = f.top_k > 0 && f.top_k <= kThreads, by_min_p = !by_k && f.top_k == 0 && !(f.top_p < 1.0) && f.min_p > 0.0;
+        const bool by_k = f.top_k > 0 && f.top_k <= kMostTopK, by_min_p = !by_k && f.top_k == 0 && !(f.top_p < 1.0) && f.min_p > 0.0;
         int last = -1;
         if (by_k) {
             for (int i = threadIdx.x; i < kBins; i += kThreads) { s.mass[i] = 0; s.count[i] = 0; }
             __syncthreads();
-            atomicAdd(&s.count[r.bin(high)], 1u);
+            atomicAdd(&s.count[r.bin(fminf(high, kMost))], 1u);
             __syncthreads();
-            r.search_bins(f.top_k, {}, 0);
+            r.search_bins(true, target_count(f.top_k), 0);
             last = (int)s.place;
         } else if (by_min_p) {
             // where masses reach min_p, which they may by being rounded up, and a bin more for the roundings of both sides

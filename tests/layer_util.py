@@ -97,13 +97,13 @@ def sample(logits, u, temperature, top_k, top_p, min_p):
     temperature, top_p, min_p = f32(temperature), f32(top_p), f32(min_p)
     if np.isnan(x).any() or not (0 <= temperature < np.inf) or x.max() == -np.inf:
         return -1
+    x = np.minimum(x, np.finfo(np.float32).max)
     order = np.argsort(-x, kind="stable")
     if temperature == 0:
         return int(order[0])
     y = x[order].astype(np.float64)
-    with np.errstate(invalid="ignore"):
-        mass = np.where(y == y[0], 2.0 ** 40, np.rint(np.exp((y - y[0]) / temperature) * 2.0 ** 40))
-    mass = mass.astype(np.uint64)
+    with np.errstate(over="ignore"):
+        mass = np.rint(np.exp((y - y[0]) / temperature) * 2.0 ** 40).astype(np.uint64)
     if 0 < top_k < mass.size:
         mass = mass[:top_k]
     run = np.cumsum(mass)
