@@ -150,36 +150,16 @@ __device__ __forceinline__ i4 load_weights(const int8_t* row, int k, int inputs)
     return {(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
 }
 
-typedef float f4u __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ float output_scale(const ProductLaunch& L, int64_t n) { return L.weight_scales ? global(L.weight_scales)[n] : L.code_scale; }
+__device__ __forceinline__ float output_bias(const ProductLaunch& L, int64_t n) { return L.bias ? load_one(L.bias, L.bias_type, n) : 0.0f; }
 
-// Scales and biases of four outputs; those behind the last one repeat it
-struct Columns {
-    f4 scale, bias;
-    __device__ __forceinline__ Columns(const ProductLaunch& L, int64_t n)
-    {
-        if (n + 4 <= L.outputs) {
-            scale = L.weight_scales ? *(const QADAM_GLOBAL f4u*)(L.weight_scales + n) : (f4)L.code_scale;
-            if (!L.bias) bias = 0.0f;
-            else if (L.bias_type == QADAM_F32) bias = *(const QADAM_GLOBAL f4u*)(static_cast<const float*>(L.bias) + n);
-            else if (L.bias_type == QADAM_BF16) bias = to_float<QADAM_BF16, 4>(load_raw<QADAM_BF16, 4, false>(static_cast<const __bf16*>(L.bias) + n));
-            else bias = to_float<QADAM_F16, 4>(load_raw<QADAM_F16, 4, false>(static_cast<const _Float16*>(L.bias) + n));
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t m = n + i < L.outputs ? n + i : L.outputs - 1;
-            scale[i] = L.weight_scales ? global(L.weight_scales)[m] : L.code_scale;
-            bias[i] = L.bias ? load_one(L.bias, L.bias_type, m) : 0.0f;
-        }
-    }
-    // one rounding per operation
-    __device__ __forceinline__ f4 operator()(const ProductLaunch& L, i4 sum, float token) const
-    {
-        f4 y = __builtin_convertvector(sum, f4) * token * scale;
-        if (L.bias) y += bias;
-        return y;
-    }
-};
+// Four outputs of a token, one rounding per operation
+__device__ __forceinline__ f4 results(const ProductLaunch& L, i4 sum, float token, f4 scale, f4 bias)
+{
+    f4 y = __builtin_convertvector(sum, f4) * token * scale;
+    if (L.bias) y += bias;          // -0 without one stays
+    return y;
+}
 
 template <int OT, int N>
 __device__ __forceinline__ void store_some(typename Element<OT>::T* p, typename Run<OT, N>::F y, int64_t n)
@@ -302,12 +282,18 @@ __global__ void __launch_bounds__(64 * kRowWaves) k_product_rows(ProductLaunch L
     for (int i = 0; i < ROWS; ++i) {
         const int64_t n = n0 + i * 16 + lane / 16 * 4;
         if (n >= L.outputs) continue;
-        const Columns columns(L, n);
+        f4 scale, bias;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t m = n + e < L.outputs ? n + e : L.outputs - 1;
+            scale[e] = output_scale(L, m);
+            bias[e] = output_bias(L, m);
+        }
 #pragma unroll
         for (int j = 0; j < COLS; ++j) {
             const int64_t t = t0 + j * 16 + lane % 16;
             if (t >= L.tokens) continue;
-            const f4 y = columns(L, acc[i][j], MADE ? made_scales[t] : global(L.token_scales)[t]);
+            const f4 y = results(L, acc[i][j], MADE ? made_scales[t] : global(L.token_scales)[t], scale, bias);
             const int64_t at = t * L.out_stride + n;
             if (L.out_type == QADAM_F32) store_some<QADAM_F32, 4>(static_cast<float*>(L.out) + at, y, L.outputs - n);
             else if (L.out_type == QADAM_BF16) store_some<QADAM_BF16, 4>(static_cast<__bf16*>(L.out) + at, y, L.outputs - n);
@@ -335,7 +321,9 @@ struct Tiles {
     static constexpr int a_bytes = BM * kStep, stage = (BM + BN) * kStep;
     static constexpr int a_loads = BM * 8 / threads, b_loads = BN * 8 / threads;
     static constexpr int pitch(int size) { return BN / WN * size + 16; }        // of a row of results in LDS
-    static constexpr int lds = 2 * stage > WM * WN * 32 * pitch(4) ? 2 * stage : WM * WN * 32 * pitch(4);
+    // of the results: rows of each wavefront, then scale and bias of the tile's outputs
+    static constexpr int columns(int size) { return WM * WN * 32 * pitch(size); }
+    static constexpr int lds = 2 * stage > columns(4) + 8 * BN ? 2 * stage : columns(4) + 8 * BN;
 };
 
 template <int BM, int BN, int WM, int WN, bool DIRECT, int OT>
@@ -354,18 +342,19 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product_tiles(ProductLaunch L,
     const int8_t* a_base = L.codes + t0 * L.codes_stride;
     const int8_t* b_base = L.weight + n0 * L.weight_stride;
     const int a_rows = (int)(L.tokens - t0 < BM ? L.tokens - t0 : BM), b_rows = (int)(L.outputs - n0 < BN ? L.outputs - n0 : BN);
-    int a_at[S::a_loads], b_at[S::b_loads], b_run[S::b_loads];
+    uint32_t a_at[S::a_loads], b_at[S::b_loads];
+    int b_run[S::b_loads];
 #pragma unroll
     for (int i = 0; i < S::a_loads; ++i) {
         const int c = i * S::threads + threadIdx.x, row = c / 8, run = (c % 8 ^ (row & 7)) * 16;
-        a_at[i] = (row < a_rows ? row : a_rows - 1) * (int)L.codes_stride + run;
+        a_at[i] = (uint32_t)(row < a_rows ? row : a_rows - 1) * (uint32_t)L.codes_stride + (uint32_t)run;
     }
     const int8_t* b_row[S::b_loads];
 #pragma unroll
     for (int i = 0; i < S::b_loads; ++i) {
         const int c = i * S::threads + threadIdx.x, row = c / 8;
         b_run[i] = (c % 8 ^ (row & 7)) * 16;
-        if constexpr (DIRECT) b_at[i] = (row < b_rows ? row : b_rows - 1) * (int)L.weight_stride;
+        if constexpr (DIRECT) b_at[i] = (uint32_t)(row < b_rows ? row : b_rows - 1) * (uint32_t)L.weight_stride;
         else b_row[i] = b_base + (int64_t)(row < b_rows ? row : b_rows - 1) * L.weight_stride;
     }
     i4 b_held[DIRECT ? 1 : S::b_loads];
@@ -373,11 +362,11 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product_tiles(ProductLaunch L,
     auto load = [&](int step, int buffer, int i) {
         int8_t* to = lds + buffer * S::stage;
         if (i < S::a_loads) {
-            __builtin_amdgcn_global_load_lds((const QADAM_GLOBAL void*)(a_base + step * kStep + a_at[i]),
+            __builtin_amdgcn_global_load_lds((const QADAM_GLOBAL void*)(a_base + (a_at[i] + (uint32_t)(step * kStep))),
                                              (__attribute__((address_space(3))) void*)(to + (i * S::threads + wave * 64) * 16), 16, 0, 0);
         } else if constexpr (DIRECT) {
             const int b = i - S::a_loads, k = step * kStep + b_run[b];
-            __builtin_amdgcn_global_load_lds((const QADAM_GLOBAL void*)(b_base + b_at[b] + (k < L.inputs ? k : 0)),
+            __builtin_amdgcn_global_load_lds((const QADAM_GLOBAL void*)(b_base + (b_at[b] + (uint32_t)(k < L.inputs ? k : 0))),
                                              (__attribute__((address_space(3))) void*)(to + S::a_bytes + (b * S::threads + wave * 64) * 16), 16, 0, 0);
         } else {
             const int b = i - S::a_loads;
@@ -463,6 +452,13 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product_tiles(ProductLaunch L,
     typedef typename Element<OT>::T O;
     constexpr int kPitch = S::pitch(sizeof(O)), kRun = 16 / sizeof(O), kRuns = BN / WN / kRun;
     int8_t* own = lds + wave * 32 * kPitch;
+    float* columns = (float*)(lds + S::columns(sizeof(O)));
+    for (int i = threadIdx.x; i < BN; i += S::threads) {
+        const int64_t n = n0 + i < L.outputs ? n0 + i : L.outputs - 1;
+        columns[i] = output_scale(L, n);
+        columns[BN + i] = output_bias(L, n);
+    }
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < S::mt; ++i) {
         const int64_t t = t0 + m0 + i * 32;
@@ -472,10 +468,10 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product_tiles(ProductLaunch L,
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int at = j * 32 + 8 * q + lane / 32 * 4;
-                const Columns columns(L, n0 + c0 + at);
+                const f4 scale = *(const f4*)(columns + c0 + at), bias = *(const f4*)(columns + BN + c0 + at);
                 const i4 sum = {acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
                 typedef O o4 __attribute__((ext_vector_type(4)));
-                *(o4*)(own + lane % 32 * kPitch + at * sizeof(O)) = __builtin_convertvector(columns(L, sum, token), o4);
+                *(o4*)(own + lane % 32 * kPitch + at * sizeof(O)) = __builtin_convertvector(results(L, sum, token, scale, bias), o4);
             }
 #pragma unroll
         for (int q = 0; q < 32 * kRuns / 64; ++q) {
