@@ -22,30 +22,38 @@ constexpr int norm_partials(int dim)
 constexpr int linear8_padded(int inputs) { return (inputs + 127) / 128 * 128; }     // of a token's integers in scratch
 constexpr int kMadeInputs = 8192;       // tokens * padded inputs up to which every workgroup makes the integers itself
 
-// Which kernel takes a product, by its sizes.
+constexpr int row_waves(int rows) { return rows == 1 ? 4 : 8; }     // of a workgroup of the rows' kernels, by tiles of 16 rows of a wavefront
+
+// Which kernel takes a product, by its sizes.  us per call on both sides of each line (2048 inputs, 8192 outputs, where nothing else is
+// said): rows / tiles of 64: 17 tokens 10.3 / 13.3, 32 tokens 10.8 / 13.2; 48 tokens in two tiles of 32 12.8 / 13.4, 64 tokens of 768 to 2304
+// 12.4 / 9.1.  Tiles of 64 / 128: 384 tokens 15.2 / 18.1, 512 tokens 17.1 / 18.4, 768 tokens 25.8 / 20.6; 1024 tokens of 768 to 2304
+// 10.5 / 12.4, 2048 16.5 / 15.4.  Tiles of 256 run one to a CU and take 1.7 times what two tiles of 128 do: 128 / 256: 1024 tokens
+// 23.4 / 28.7, 2048 tokens 43.5 / 38.4, 4096 83.7 / 72.7, 16384 337 / 280; 8192 tokens of 768 to 2304 36.4 / 40.1.
 struct Linear8Plan {
-    enum Kind { kRows16, kRows32, kRows64, kTiles128, kTiles256 } kind;
+    enum Kind { kRows16, kRows32, kTiles64, kTiles128, kTiles256 } kind;
     bool made;              // the product's workgroups make the tokens' integers
     int split;              // of the rows' kernels: wavefronts that share the inputs
 
     constexpr Linear8Plan(int64_t tokens, int64_t outputs, int inputs, bool floats) : kind(kTiles128), made(false), split(1)
     {
         const int64_t tiles128 = (tokens + 127) / 128 * ((outputs + 127) / 128), tiles256 = (tokens + 255) / 256 * ((outputs + 255) / 256);
-        if (tokens <= 64 || (tokens <= 512 && tiles128 < 192)) {
-            kind = tokens <= 16 ? kRows16 : tokens <= 32 ? kRows32 : kRows64;
+        if (tokens <= 32) {
+            kind = tokens <= 16 ? kRows16 : kRows32;
             made = floats && tokens <= 16 && tokens * linear8_padded(inputs) <= kMadeInputs;
-            const int rows = kind == kRows16 ? 16 : 32, cols = kind == kRows16 ? 16 : kind == kRows32 ? 32 : 64;
-            const int64_t waves = (outputs + rows - 1) / rows * ((tokens + cols - 1) / cols);
-            while (split < 4 && waves * split < 2048 && inputs > 256 * split) split *= 2;
-        } else if (tiles256 >= 384) {
+            const int rows = kind == kRows16 ? 1 : 2;
+            const int64_t waves = (outputs + 16 * rows - 1) / (16 * rows);
+            while (split < row_waves(rows) && waves * split < 2048 && inputs > 256 * split) split *= 2;
+        } else if (tiles128 <= 256) {
+            kind = kTiles64;
+        } else if ((tiles256 + 255) / 256 * 17 < (tiles128 + 511) / 512 * 10) {
             kind = kTiles256;
         }
     }
 };
 
-// Place of a workgroup's tile.  Workgroups go to the 8 XCDs in turn: each XCD gets a run of tiles, columns of 8 tiles of tokens one after
+// Place of a workgroup's tile.  Workgroups go to the 8 XCDs in turn: each XCD gets a run of tiles, columns of 4 tiles of tokens one after
 // the other, so that the tiles that it works on together share rows of both operands in its L2.
-constexpr int kTileColumn = 8;
+constexpr int kTileColumn = 4;
 constexpr void tile_place(int block, int across, int down, int* tm, int* tn)
 {
     const int total = across * down, each = total / 8, more = total % 8, xcd = block % 8;

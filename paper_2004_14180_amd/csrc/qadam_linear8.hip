@@ -173,43 +173,44 @@ __device__ __forceinline__ void store_some(typename Element<OT>::T* p, typename 
 // ---- few tokens -----------------------------------------------------------------------------------
 // A wavefront takes ROWS tiles of 16 rows of the weights and COLS tiles of 16 tokens, and a part of the inputs; `split` of a workgroup's
 // wavefronts share the rows and add their sums in LDS.  A lane's 16 integers of a matrix instruction are 16 bytes of one row, so the
-// weights come from memory into their places, at any address.
-// MADE: the workgroup makes the tokens' integers itself, in LDS, which saves the launch that would.
-constexpr int kRowWaves = 4;
-
-template <int ROWS, int COLS, bool MADE>
-__global__ void __launch_bounds__(64 * kRowWaves) k_product_rows(ProductLaunch L, TokensLaunch X, int split, int64_t first)
+// weights come from memory into their places, at any address.  AHEAD chunks of 64 inputs are loaded together, of weights and tokens, while
+// the ones before are multiplied.
+// MADE: the workgroup makes the tokens' integers itself, in LDS, which saves the launch that would, while its first weights are on the way.
+// a barrier for what lies in LDS: loads from memory stay under way
+__device__ __forceinline__ void lds_barrier()
 {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+template <int ROWS, int COLS, int AHEAD, bool MADE>
+__global__ void __launch_bounds__(64 * row_waves(ROWS)) k_product_rows(ProductLaunch L, TokensLaunch X, int split, int64_t first)
+{
+    constexpr int kRowWaves = row_waves(ROWS);
     extern __shared__ __attribute__((aligned(16))) int8_t lds[];
-    __shared__ uint32_t most[kRowWaves];
-    __shared__ float made_scales[16];
+    __shared__ uint32_t most[16];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int padded = X.padded;
     const int64_t per = (L.outputs + 16 * ROWS * (kRowWaves / split) - 1) / (16 * ROWS * (kRowWaves / split));
     const int64_t group = blockIdx.x % per, t0 = first + blockIdx.x / per * (16 * COLS);
-    if constexpr (MADE) {
-        for (int t = 0; t < (int)L.tokens; ++t) {
-            uint32_t m = 0;
-            for (int at = threadIdx.x * kRowRun; at < L.inputs; at += 64 * kRowWaves * kRowRun)
-                m = larger(m, largest_of(load_part(X.x, X.x_type, t * X.x_stride + at, L.inputs - at)));
-            m = wave_largest(m);
-            __syncthreads();
-            if (lane == 0) most[wave] = m;
-            __syncthreads();
-            for (int w = 0; w < kRowWaves; ++w) m = larger(m, most[w]);
-            const TokenScale s(m);
-            if (threadIdx.x == 0) made_scales[t] = s.scale;
-            for (int at = threadIdx.x * kRowRun; at < padded; at += 64 * kRowWaves * kRowRun) {
-                f8 x = 0.0f;
-                if (at < L.inputs) x = load_part(X.x, X.x_type, t * X.x_stride + at, L.inputs - at);
-                *(uint64_t*)(lds + t * padded + at) = codes_of(s, x);
-            }
-        }
-        __syncthreads();
-    }
     const int part = wave % split, chunks = (L.inputs + 63) / 64, each = (chunks + split - 1) / split;
     const int begin = part * each, end = begin + each < chunks ? begin + each : chunks;
     const int64_t n0 = (group * (kRowWaves / split) + wave / split) * (16 * ROWS);
+    const int k0 = lane / 16 * 16;
+
+    // tokens that become integers here: runs of 8, a few per thread
+    constexpr int kHeld = MADE ? kMadeInputs / (64 * kRowWaves * kRowRun) : 1;
+    const int runs = padded / kRowRun;
+    f8 held[kHeld];
+    if constexpr (MADE) {
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h) {
+            const int q = h * 64 * kRowWaves + threadIdx.x, t = q / runs, at = q % runs * kRowRun;
+            held[h] = 0.0f;
+            if (t < (int)L.tokens && at < L.inputs) held[h] = load_part(X.x, X.x_type, t * X.x_stride + at, L.inputs - at);
+        }
+    }
     const int8_t* row[ROWS];
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
@@ -224,42 +225,69 @@ __global__ void __launch_bounds__(64 * kRowWaves) k_product_rows(ProductLaunch L
         there[j] = t < L.tokens;
         token[j] = MADE ? lds + (there[j] ? t : 0) * padded : L.codes + (there[j] ? t : 0) * L.codes_stride;
     }
-    const int k0 = lane / 16 * 16;
+    i4 w[ROWS][AHEAD], x[COLS][AHEAD];
+    auto load_rows = [&](int c) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) w[i][u] = c + u < end ? load_weights(row[i], (c + u) * 64 + k0, L.inputs) : (i4)0;
+    };
+    auto load_tokens = [&](int c) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int j = 0; j < COLS; ++j) {
+                x[j][u] = 0;
+                if (c + u < end && there[j]) {
+                    if constexpr (MADE) x[j][u] = *(const i4*)(token[j] + (c + u) * 64 + k0);
+                    else x[j][u] = *(const QADAM_GLOBAL i4*)(token[j] + (c + u) * 64 + k0);
+                }
+            }
+    };
+    load_rows(begin);
+    if constexpr (MADE) {
+        if (threadIdx.x < 16) most[threadIdx.x] = 0;
+        lds_barrier();
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h) {
+            const int t = (h * 64 * kRowWaves + (int)threadIdx.x) / runs;
+            if (t < (int)L.tokens) atomicMax(&most[t], largest_of(held[h]));
+        }
+        lds_barrier();
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h) {
+            const int q = h * 64 * kRowWaves + threadIdx.x, t = q / runs;
+            if (t < (int)L.tokens) *(uint64_t*)(lds + q * kRowRun) = codes_of(TokenScale(most[t]), held[h]);
+        }
+        lds_barrier();
+    }
+    load_tokens(begin);
     i4 acc[ROWS][COLS];
 #pragma unroll
     for (int i = 0; i < ROWS; ++i)
 #pragma unroll
         for (int j = 0; j < COLS; ++j) acc[i][j] = 0;
-    constexpr int kAhead = ROWS == 1 ? 8 : 4;       // chunks of the weights under way together
-    i4 w[ROWS][kAhead];
-    auto load = [&](int c) {
+#pragma unroll 1
+    for (int c = begin; c < end; c += AHEAD) {
+        i4 w_now[ROWS][AHEAD], x_now[COLS][AHEAD];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
+        for (int u = 0; u < AHEAD; ++u) {
 #pragma unroll
-            for (int i = 0; i < ROWS; ++i) w[i][u] = c + u < end ? load_weights(row[i], (c + u) * 64 + k0, L.inputs) : (i4)0;
-    };
-    load(begin);
-    for (int c = begin; c < end; c += kAhead) {
-        i4 now[ROWS][kAhead];
+            for (int i = 0; i < ROWS; ++i) w_now[i][u] = w[i][u];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-#pragma unroll
-            for (int i = 0; i < ROWS; ++i) now[i][u] = w[i][u];
-        if (c + kAhead < end) load(c + kAhead);
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (c + u >= end) break;
-#pragma unroll
-            for (int j = 0; j < COLS; ++j) {
-                i4 x = 0;
-                if (there[j]) {
-                    if constexpr (MADE) x = *(const i4*)(token[j] + (c + u) * 64 + k0);
-                    else x = *(const QADAM_GLOBAL i4*)(token[j] + (c + u) * 64 + k0);
-                }
-#pragma unroll
-                for (int i = 0; i < ROWS; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now[i][u], x, acc[i][j], 0, 0, 0);
-            }
+            for (int j = 0; j < COLS; ++j) x_now[j][u] = x[j][u];
         }
+        if (c + AHEAD < end) {
+            load_rows(c + AHEAD);
+            load_tokens(c + AHEAD);
+        }
+        // chunks behind the end are zeros
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int j = 0; j < COLS; ++j)
+#pragma unroll
+                for (int i = 0; i < ROWS; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w_now[i][u], x_now[j][u], acc[i][j], 0, 0, 0);
     }
     if (split > 1) {
         __syncthreads();
@@ -293,7 +321,7 @@ __global__ void __launch_bounds__(64 * kRowWaves) k_product_rows(ProductLaunch L
         for (int j = 0; j < COLS; ++j) {
             const int64_t t = t0 + j * 16 + lane % 16;
             if (t >= L.tokens) continue;
-            const f4 y = results(L, acc[i][j], MADE ? made_scales[t] : global(L.token_scales)[t], scale, bias);
+            const f4 y = results(L, acc[i][j], MADE ? TokenScale(most[t]).scale : global(L.token_scales)[t], scale, bias);
             const int64_t at = t * L.out_stride + n;
             if (L.out_type == QADAM_F32) store_some<QADAM_F32, 4>(static_cast<float*>(L.out) + at, y, L.outputs - n);
             else if (L.out_type == QADAM_BF16) store_some<QADAM_BF16, 4>(static_cast<__bf16*>(L.out) + at, y, L.outputs - n);
@@ -518,15 +546,16 @@ hipError_t tiles(const ProductLaunch& L)
     return hipSuccess;
 }
 
-template <int ROWS, int COLS, bool MADE>
+template <int ROWS, int COLS, int AHEAD, bool MADE>
 hipError_t rows(const ProductLaunch& L, const TokensLaunch& X, int split)
 {
-    const int64_t across = (L.outputs + 16 * ROWS * (kRowWaves / split) - 1) / (16 * ROWS * (kRowWaves / split)), most = ((int64_t)1 << 23) / across;
+    constexpr int kRowWaves = row_waves(ROWS);
+    const int64_t across = (L.outputs + 16 * ROWS * (kRowWaves / split) - 1) / (16 * ROWS * (kRowWaves / split)), most = ((int64_t)1 << 22) / across;
     int lds = split > 1 ? kRowWaves * ROWS * COLS * 64 * 16 : 0;
     if (MADE && lds < (int)L.tokens * X.padded) lds = (int)L.tokens * X.padded;
     for (int64_t t = 0; t < L.tokens; t += most * 16 * COLS) {
         const int64_t rest = (L.tokens - t + 16 * COLS - 1) / (16 * COLS);
-        k_product_rows<ROWS, COLS, MADE><<<dim3((int)(across * (rest < most ? rest : most))), dim3(64 * kRowWaves), lds, L.stream>>>(L, X, split, t);
+        k_product_rows<ROWS, COLS, AHEAD, MADE><<<dim3((int)(across * (rest < most ? rest : most))), dim3(64 * kRowWaves), lds, L.stream>>>(L, X, split, t);
     }
     return hipGetLastError();
 }
@@ -550,13 +579,13 @@ hipError_t launch_product(const ProductLaunch& L, const TokensLaunch& X)
             if (e != hipSuccess) return e;
         }
     } else {
-        return rows<1, 1, true>(L, X, p.split);
+        return rows<1, 1, 4, true>(L, X, p.split);
     }
     const bool direct = reinterpret_cast<uintptr_t>(L.weight) % 16 == 0 && L.weight_stride % 16 == 0 && L.inputs % 16 == 0 && L.weight_stride <= 1 << 22;
     switch (p.kind) {
-    case Linear8Plan::kRows16: return rows<1, 1, false>(L, X, p.split);
-    case Linear8Plan::kRows32: return rows<2, 2, false>(L, X, p.split);
-    case Linear8Plan::kRows64: return rows<2, 4, false>(L, X, p.split);
+    case Linear8Plan::kRows16: return rows<1, 1, 4, false>(L, X, p.split);
+    case Linear8Plan::kRows32: return rows<2, 2, 4, false>(L, X, p.split);
+    case Linear8Plan::kTiles64: return direct ? tiles<64, 64, 2, 2, true>(L) : tiles<64, 64, 2, 2, false>(L);
     case Linear8Plan::kTiles256:
         if (direct) return tiles<256, 256, 4, 2, true>(L);
         [[fallthrough]];
