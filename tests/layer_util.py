@@ -13,7 +13,7 @@ def depth(dim):
 
 def rows_depth(rows, dim):
     """... in a sum over rows: those of one wavefront, four wavefronts; the workgroups' sums are added in fp64."""
-    partials = min(512, max(8, (1 << 21) // dim))
+    partials = min(512 if dim <= 2048 else 256, max(8, (1 << 21) // dim))
     return -(-rows // partials) + 4
 
 
