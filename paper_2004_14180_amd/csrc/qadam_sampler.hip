@@ -51,19 +51,18 @@ struct Mass {
         constexpr double kRound = 0x1.8p52;
         const double y = fmax(((double)x - (double)largest) * per_unit, -100.0);
         const double rounded = y + kRound, r = y - (rounded - kRound);
-        double e = 0x1.b6571dbf753eep-24;
-        e = __builtin_fma(e, r, 0x1.63ef969af1055p-20);
-        e = __builtin_fma(e, r, 0x1.ffcb7678c7b33p-17);
-        e = __builtin_fma(e, r, 0x1.43088e257ed10p-13);
-        e = __builtin_fma(e, r, 0x1.5d87fe908f74fp-10);
-        e = __builtin_fma(e, r, 0x1.3b2ab72b175efp-7);
-        e = __builtin_fma(e, r, 0x1.c6b08d704411ap-5);
-        e = __builtin_fma(e, r, 0x1.ebfbdff8149f2p-3);
-        e = __builtin_fma(e, r, 0x1.62e42fefa39f7p-1);
-        e = __builtin_fma(e, r, 0x1.000000000003dp+0);
-        // e is above 2^-1 and below 2^1, n + 40 from -60 to 40: an addition to the exponent
-        const uint64_t bits = __builtin_bit_cast(uint64_t, e) + ((uint64_t)(uint32_t)((int)(uint32_t)__builtin_bit_cast(uint64_t, rounded) + 40) << 52);
-        const double m = __builtin_bit_cast(double, bits) + 0x1p52;
+        const double r2 = r * r, r4 = r2 * r2;
+        // by pairs, which do not wait for each other; 2^40 is in the coefficients
+        const double e01 = __builtin_fma(0x1.62e42fefa39f7p+39, r, 0x1.000000000003dp+40);
+        const double e23 = __builtin_fma(0x1.c6b08d704411ap+35, r, 0x1.ebfbdff8149f2p+37);
+        const double e45 = __builtin_fma(0x1.5d87fe908f74fp+30, r, 0x1.3b2ab72b175efp+33);
+        const double e67 = __builtin_fma(0x1.ffcb7678c7b33p+23, r, 0x1.43088e257ed10p+27);
+        const double e89 = __builtin_fma(0x1.b6571dbf753eep+16, r, 0x1.63ef969af1055p+20);
+        const double e = __builtin_fma(__builtin_fma(__builtin_fma(e89, r2, e67), r2, e45), r4, __builtin_fma(e23, r2, e01));
+        // e is above 2^39 and below 2^41, n from -100 to 0: 2^n is an addition to the exponent, in the upper half
+        const uint64_t bits = __builtin_bit_cast(uint64_t, e);
+        const uint32_t high = (uint32_t)(bits >> 32) + ((uint32_t)__builtin_bit_cast(uint64_t, rounded) << 20);
+        const double m = __builtin_bit_cast(double, (uint64_t)high << 32 | (uint32_t)bits) + 0x1p52;
         return __builtin_bit_cast(uint64_t, m) & 0xfffffffffffffull;
     }
 };
@@ -105,6 +104,7 @@ struct Shared {
     uint32_t wave_key[kWaves], wave_low[kWaves], wave_nan[kWaves], wave_equal[kWaves];
     uint64_t least;             // sum of the masses that reach min_p
     uint32_t listed, first;
+    int      min_p_bin;
     // what a search leaves
     int64_t  place;
     uint64_t before, sum;
@@ -153,6 +153,7 @@ struct Row {
     int vocab;
     Mass mass;
     Bin bin;
+    bool infinite;          // the largest logit is
 
     __device__ __forceinline__ float logit(int i) const { return fminf((float)global(logits)[i], kMost); }
 
@@ -185,8 +186,12 @@ struct Row {
         typename Run<LT, kRowRun>::V next = load(at, &next_start);
 #pragma unroll 1
         while (true) {
-            const f8 x = to_float<LT, kRowRun>(next);
+            f8 x = to_float<LT, kRowRun>(next);
             const int start = next_start;
+            if (infinite) {
+#pragma unroll
+                for (int e = 0; e < kRowRun; ++e) x[e] = fminf(x[e], kMost);
+            }
             at += kAcross;
             if (at < vocab) next = load(at, &next_start);
             body(x, start);
@@ -201,13 +206,14 @@ struct Row {
         __syncthreads();
         if (threadIdx.x == 0) s.listed = 0;
         __syncthreads();
+        // where these bins lie, and a little more; what is within is looked at closer
+        const float width = 1.0f / bin.per_unit, slack = 0x1p-19f * (fabsf(bin.largest) + (float)(hi + 1) * width);
+        const float most = bin.largest - (float)lo * width + slack;
+        const float least = hi < kBins - 1 ? fmaxf(bin.largest - (float)(hi + 1) * width - slack, -kMost) : -kMost;
         each([&](f8 x, int at) {
             uint32_t take = 0;
 #pragma unroll
-            for (int e = 0; e < kRowRun; ++e) {
-                x[e] = fminf(x[e], kMost);
-                take |= ((uint32_t)(bin(x[e]) - lo) <= (uint32_t)(hi - lo) && x[e] > -kInf ? 1u : 0u) << e;
-            }
+            for (int e = 0; e < kRowRun; ++e) take |= (x[e] >= least && x[e] <= most ? 1u : 0u) << e;
             // few are taken: one place in the list after the other
             while (take) {
                 const int e = __builtin_ctz(take);
@@ -215,6 +221,8 @@ struct Row {
                 float v = x[0];
 #pragma unroll
                 for (int k = 1; k < kRowRun; ++k) v = e == k ? x[k] : v;
+                const int b = bin(v);
+                if (b < lo || b > hi) continue;
                 const uint32_t to = atomicAdd(&s.listed, 1u);
                 if (to < kList) s.list[to] = (uint64_t)key_of(v) << 32 | (uint32_t)(at + e);
             }
@@ -397,9 +405,16 @@ __device__ __forceinline__ Target target_p(const RowFilters& f, uint64_t sum)
 }
 __device__ __forceinline__ Target target_u(const RowFilters& f, uint64_t sum) { return {(double)f.u * (double)sum, true}; }
 
+// The bin of the logits whose masses round to what min_p asks for, to one on either side; kBins - 1 beyond the bins.
+__device__ __forceinline__ int min_p_bin(const Bin& bin, const RowFilters& f)
+{
+    const float below = (float)(-log(((double)least_mass(f) - 0.5) * 0x1p-40) * f.temperature);
+    return (int)fminf(fmaxf(below, 0.0f) * bin.per_unit, (float)(kBins - 1));
+}
+
 // The token of a row whose largest logit is known.  `last` >= 0: all tokens that can be drawn lie in the bins 0 to last.
-// Three sums are asked for one after the other, each only where its filter is: that of the first top_k, that of those that top_p leaves, and
-// the token's.
+// Sums are asked for one after the other, each only where its filter is: 1 that of the first top_k, 2 that of those that top_p leaves, 3 that
+// of those that reach min_p, 4 the token's.
 template <int LT, bool SHORT>
 __device__ __forceinline__ int64_t draw(const Row<LT, SHORT>& r, const RowFilters& f, int last)
 {
@@ -411,7 +426,7 @@ __device__ __forceinline__ int64_t draw(const Row<LT, SHORT>& r, const RowFilter
     int n = 0;
     uint64_t sum = 0;
 #pragma unroll 1
-    for (int ask = last >= 0 ? 0 : 1; ask <= 3; ++ask) {
+    for (int ask = last >= 0 ? 0 : 1; ask <= 4; ++ask) {
         int lo = 0, hi = last;
         uint64_t before = 0;
         int64_t rest = counts ? f.top_k : kList;        // tokens of the list whose sum is asked for
@@ -424,20 +439,18 @@ __device__ __forceinline__ int64_t draw(const Row<LT, SHORT>& r, const RowFilter
         if (ask == 1) {
             for (int i = threadIdx.x; i < kBins; i += kThreads) { s.mass[i] = 0; s.count[i] = 0; }
             __syncthreads();
-            const uint64_t least = by_min_p ? least_mass(f) : 0;
-            uint64_t own_least = 0;
             r.each([&](f8 x, int) {
 #pragma unroll
                 for (int e = 0; e < kRowRun; ++e) {
-                    const float v = fminf(x[e], kMost);
-                    const int b = r.bin(v);
-                    const uint64_t m = r.mass(v);
-                    if (counts) atomicAdd(&s.count[b], 1u);
-                    if (by_min_p) own_least += m >= least ? m : 0;
-                    if (m > 0) atomicAdd((unsigned long long*)&s.mass[b], (unsigned long long)m);
+                    const uint64_t m = r.mass(x[e]);
+                    if (m > 0) atomicAdd((unsigned long long*)&s.mass[r.bin(x[e])], (unsigned long long)m);
                 }
             });
-            if (by_min_p) atomicAdd((unsigned long long*)&s.least, (unsigned long long)own_least);
+            if (counts)
+                r.each([&](f8 x, int) {
+#pragma unroll
+                    for (int e = 0; e < kRowRun; ++e) atomicAdd(&s.count[r.bin(x[e])], 1u);
+                });
             __syncthreads();
             // all of them: no bin is asked for
             sum = r.search_bins(false, {__builtin_inf(), false}, 0);
@@ -447,17 +460,29 @@ __device__ __forceinline__ int64_t draw(const Row<LT, SHORT>& r, const RowFilter
             if (!(f.top_p < 1.0)) continue;
             target = target_p(f, sum);
         } else if (ask == 3) {
+            if (!by_min_p) continue;
             __syncthreads();
-            if (by_min_p && s.least < sum) sum = s.least;
+            if (all_listed) {
+                if (s.least < sum) sum = s.least;
+                continue;
+            }
+        } else if (ask == 4) {
             target = target_u(f, sum);
         }
         if (ask > 0 && binned && !all_listed) {
-            r.search_bins(ask == 1, target, 1);
-            lo = hi = (int)s.place;
-            before = s.before;
-            if (ask == 1) {
-                // the masses in front of the bin
-                rest = f.top_k - (int64_t)before;
+            if (ask == 3) {
+                // the bin in which masses reach min_p, and one more on either side
+                const int at = s.min_p_bin;
+                lo = at > 0 ? at - 1 : 0;
+                hi = at + 1 < kBins ? at + 1 : kBins - 1;
+            } else {
+                r.search_bins(ask == 1, target, 1);
+                lo = hi = (int)s.place;
+                before = s.before;
+            }
+            if (ask == 1 || ask == 3) {
+                // the masses in front of the bins
+                rest = ask == 1 ? f.top_k - (int64_t)before : kList;
                 uint64_t own = 0;
 #pragma unroll
                 for (int k = 0; k < kThreadBins; ++k) own += (int)threadIdx.x * kThreadBins + k < lo ? s.mass[threadIdx.x * kThreadBins + k] : 0;
@@ -466,24 +491,36 @@ __device__ __forceinline__ int64_t draw(const Row<LT, SHORT>& r, const RowFilter
         }
         if (binned && !all_listed) n = r.collect(lo, hi);
         if (binned && n <= kList) {
-            if (ask < 2) {
+            if (ask < 2 || ask == 3) {
                 // the sum of the list's first ones, and of those of them that reach min_p; a list without one: no sum
                 if (threadIdx.x == 0) s.sum = 0;
                 __syncthreads();
                 const int kept = rest < n ? (int)rest : n;
                 for (int i = threadIdx.x; i < n; i += kThreads) {
                     if (s.rank[i] == kept) s.sum = s.run[i];
-                    if (ask == 0 && by_min_p && s.rank[i] <= kept && r.listed_mass(i) >= least_mass(f))
+                    if (ask != 1 && by_min_p && s.rank[i] <= kept && r.listed_mass(i) >= least_mass(f))
                         atomicMax((unsigned long long*)&s.least, (unsigned long long)s.run[i]);
                 }
                 __syncthreads();
-                sum = before + s.sum;
+                if (ask == 3) sum = before + s.least < sum ? before + s.least : sum;
+                else sum = before + s.sum;
                 all_listed = ask == 0;
             } else {
                 r.search(n, before, target);
                 sum = s.sum;
                 in_list = true;
             }
+            __syncthreads();
+        } else if (ask == 3) {
+            const uint64_t least = least_mass(f);
+            uint64_t own = 0;
+            for (int i = threadIdx.x; i < r.vocab; i += kThreads) {
+                const uint64_t m = r.mass(r.logit(i));
+                own += m >= least ? m : 0;
+            }
+            atomicAdd((unsigned long long*)&s.least, (unsigned long long)own);
+            __syncthreads();
+            if (s.least < sum) sum = s.least;
             __syncthreads();
         } else if (ask > 0) {
             binned = in_list = false;
@@ -536,7 +573,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleLaunch L, int64_t fir
         if (!(own.top_k > 0 && own.top_k < L.vocab)) own.top_k = 0;
         s.filters = own;
     }
-    Row<LT, SHORT> r{s, static_cast<const typename Element<LT>::T*>(L.logits) + row * L.logits_stride, (int)L.vocab, {}, {}};
+    Row<LT, SHORT> r{s, static_cast<const typename Element<LT>::T*>(L.logits) + row * L.logits_stride, (int)L.vocab, {}, {}, false};
 
     // largest, smallest that is no minus infinity, NaN
     float high = -kInf, low = kInf;
@@ -560,6 +597,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleLaunch L, int64_t fir
         all_low = fminf(all_low, __builtin_bit_cast(float, s.wave_low[w]));
         none |= s.wave_nan[w] != 0;
     }
+    r.infinite = all_high == kInf;
     all_high = fminf(all_high, kMost) + 0.0f;
     all_low = fminf(all_low, kMost);
     none |= all_high == -kInf;
@@ -572,7 +610,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleLaunch L, int64_t fir
         r.each([&](f8 x, int at) {
 #pragma unroll
             for (int e = kRowRun - 1; e >= 0; --e)
-                if (fminf(x[e], kMost) == all_high && (uint32_t)(at + e) < first) first = (uint32_t)(at + e);
+                if (x[e] == all_high && (uint32_t)(at + e) < first) first = (uint32_t)(at + e);
         });
         if (first != ~0u) atomicMin(&s.first, first);
         __syncthreads();
@@ -585,6 +623,8 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleLaunch L, int64_t fir
         const float scale = (float)(kBins - 1) / range;
         r.bin = {all_high, scale < 1e30f ? scale : 1e30f};
         const bool by_k = f.top_k > 0 && f.top_k <= kMostTopK, by_min_p = !by_k && f.top_k == 0 && !(f.top_p < 1.0) && f.min_p > 0.0;
+        if (f.min_p > 0.0 && threadIdx.x == 0) s.min_p_bin = min_p_bin(r.bin, f);
+        __syncthreads();
         int last = -1;
         if (by_k) {
             for (int i = threadIdx.x; i < kBins; i += kThreads) { s.mass[i] = 0; s.count[i] = 0; }
@@ -594,10 +634,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleLaunch L, int64_t fir
             r.search_bins(true, target_count(f.top_k), 0);
             last = (int)s.place;
         } else if (by_min_p) {
-            // where masses reach min_p, which they may by being rounded up, and a bin more for the roundings of both sides
-            const double least = (f.min_p < 1.0 ? f.min_p : 1.0) - 0x1p-40;
-            const float below = least > 0.0 ? (float)(-log(least) * f.temperature) * 1.0001f : kInf;
-            last = (int)fminf(below * r.bin.per_unit, (float)(kBins - 1)) + 1;
+            last = s.min_p_bin + 1;
         }
         token = draw(r, f, last);
     }

@@ -52,6 +52,17 @@ def test_filters(temperature, top_k):
             _check(x, u, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
 
 
+@pytest.mark.parametrize("min_p", [1e-30, 2.0 ** -41, 2.0 ** -40, 1.5 * 2.0 ** -40, 3e-12, 1e-9, 1e-4, 0.3, 0.9999999])
+@pytest.mark.parametrize("top_k", [0, 30, 700])
+def test_min_p_beside_the_others(min_p, top_k):
+    """From half a unit of the masses on: the tokens that reach it are found in the bins, or in the list of the first ones."""
+    for dtype, std, temperature in ((F32, 4.0, 1.0), (BF16, 4.0, 0.6), (F32, 30.0, 1.0), (F32, 0.01, 1.0)):
+        x, u = _logits(6, 20011, dtype, seed=top_k, std=std)
+        u[0] = 1.0 - 2.0 ** -24
+        for top_p in (1.0, 0.999, 0.7):
+            _check(x, u, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
+
+
 @pytest.mark.parametrize("vocab", [100, 5000, 60000])
 @pytest.mark.parametrize("levels", [1, 2, 5])
 def test_equal_logits(vocab, levels):
