@@ -133,14 +133,19 @@ __device__ __forceinline__ uint64_t sum_ahead(Shared& s, uint64_t x, int turn, u
     run = moved_sum<0x143, 0xc>(run);
     if (lane == 63) s.wave_sum[turn][wave] = run;
     __syncthreads();
-    uint64_t before = 0, all = 0;
-#pragma unroll 4
-    for (int w = 0; w < kWaves; ++w) {
-        const uint64_t v = s.wave_sum[turn][w];
-        before += w < wave ? v : 0;
-        all += v;
-    }
-    *total = all;
+    // every row of 16 lanes adds the wavefronts' sums
+    static_assert(kWaves == 16, "a row of lanes");
+    uint64_t all = s.wave_sum[turn][lane % 16];
+    all = moved_sum<0x111>(all);
+    all = moved_sum<0x112>(all);
+    all = moved_sum<0x114>(all);
+    all = moved_sum<0x118>(all);
+    auto of_lane = [&](int from) {
+        return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(all >> 32), from) << 32 |
+               (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)all, from);
+    };
+    *total = of_lane(15);
+    const uint64_t before = wave > 0 ? of_lane(__builtin_amdgcn_readfirstlane(wave - 1)) : 0;
     return before + run - x;
 }
 
@@ -208,12 +213,19 @@ struct Row {
         __syncthreads();
         // where these bins lie, and a little more; what is within is looked at closer
         const float width = 1.0f / bin.per_unit, slack = 0x1p-19f * (fabsf(bin.largest) + (float)(hi + 1) * width);
-        const float most = bin.largest - (float)lo * width + slack;
         const float least = hi < kBins - 1 ? fmaxf(bin.largest - (float)(hi + 1) * width - slack, -kMost) : -kMost;
+        // differences that are not negative are in the order of their bits, in front of all that are negative
+        const uint32_t within = __builtin_bit_cast(uint32_t, fmaxf(bin.largest - (float)lo * width + slack - least, 0.0f));
         each([&](f8 x, int at) {
+            typedef uint32_t u8 __attribute__((ext_vector_type(kRowRun)));
+            const u8 above = __builtin_bit_cast(u8, x - least);
+            uint32_t nearest = above[0];
+#pragma unroll
+            for (int e = 1; e < kRowRun; ++e) nearest = above[e] < nearest ? above[e] : nearest;
+            if (nearest > within) return;
             uint32_t take = 0;
 #pragma unroll
-            for (int e = 0; e < kRowRun; ++e) take |= (x[e] >= least && x[e] <= most ? 1u : 0u) << e;
+            for (int e = 0; e < kRowRun; ++e) take |= (above[e] <= within ? 1u : 0u) << e;
             // few are taken: one place in the list after the other
             while (take) {
                 const int e = __builtin_ctz(take);
@@ -575,15 +587,19 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleLaunch L, int64_t fir
     }
     Row<LT, SHORT> r{s, static_cast<const typename Element<LT>::T*>(L.logits) + row * L.logits_stride, (int)L.vocab, {}, {}, false};
 
-    // largest, smallest that is no minus infinity, NaN
+    // Largest, NaN; the smallest that is no minus infinity where bins could be much wider than they need be.
     float high = -kInf, low = kInf;
     bool nan = false;
+    const bool wide = L.filters.temperatures || L.filters.temperature > 1.0f;
     r.each([&](f8 x, int) {
 #pragma unroll
-        for (int e = 0; e < kRowRun; ++e) {
-            nan |= x[e] != x[e];
-            high = fmaxf(high, x[e]);
-            low = fminf(low, x[e] == -kInf ? kInf : x[e]);
+        for (int e = 0; e < kRowRun; e += 2) {
+            nan |= __builtin_isunordered(x[e], x[e + 1]);
+            high = fmaxf(fmaxf(high, x[e]), x[e + 1]);
+        }
+        if (wide) {
+#pragma unroll
+            for (int e = 0; e < kRowRun; ++e) low = fminf(low, x[e] == -kInf ? kInf : x[e]);
         }
     });
     float all_high = wave_extreme<true>(high), all_low = wave_extreme<false>(low);
@@ -599,7 +615,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleLaunch L, int64_t fir
     }
     r.infinite = all_high == kInf;
     all_high = fminf(all_high, kMost) + 0.0f;
-    all_low = fminf(all_low, kMost);
+    all_low = wide ? fminf(all_low, kMost) : -kInf;
     none |= all_high == -kInf;
     int64_t token = -1;
     if (!none && f.temperature == 0.0) {
@@ -619,7 +635,7 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleLaunch L, int64_t fir
         const double log2e = 0x1.71547652b82fep+0;
         r.mass = {all_high, log2e / f.temperature};
         // bins down to where masses vanish, 29 temperatures below the largest, or to the smallest logit; any scale is right
-        const float range = fminf(29.0f * (float)f.temperature, all_high - all_low);
+        const float range = fminf(fminf(29.0f * (float)f.temperature, all_high - all_low), kMost);
         const float scale = (float)(kBins - 1) / range;
         r.bin = {all_high, scale < 1e30f ? scale : 1e30f};
         const bool by_k = f.top_k > 0 && f.top_k <= kMostTopK, by_min_p = !by_k && f.top_k == 0 && !(f.top_p < 1.0) && f.min_p > 0.0;
