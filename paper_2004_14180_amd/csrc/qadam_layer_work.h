@@ -28,10 +28,11 @@ constexpr int row_waves(int rows) { return rows == 1 ? 4 : 8; }     // of a work
 // Which kernel takes a product, by its sizes.  us per call on both sides of each line (2048 inputs, 8192 outputs, where nothing else is
 // said): rows / tiles of 64: 17 tokens 10.3 / 13.3, 32 tokens 10.8 / 13.2; 48 tokens in two tiles of 32 12.8 / 13.4, 64 tokens of 768 to 2304
 // 12.4 / 9.1.  Tiles of 64 / 128: 384 tokens 15.2 / 18.1, 512 tokens 17.1 / 18.4, 768 tokens 25.8 / 20.6; 1024 tokens of 768 to 2304
-// 10.5 / 12.4, 2048 16.5 / 15.4.  Tiles of 256 run one to a CU and take 1.7 times what two tiles of 128 do: 128 / 256: 1024 tokens
+// 10.5 / 12.4, 2048 16.5 / 15.4.  Up to two tiles of 64 on a CU wait for their loads: steps of two / three of them in LDS: 64 tokens
+// 14.0 / 11.2, 256 tokens 14.6 / 13.8, 512 tokens (four on a CU) 18.5 / 21.5.  Tiles of 256 run one to a CU and take 1.7 times what two tiles of 128 do: 128 / 256: 1024 tokens
 // 23.4 / 28.7, 2048 tokens 43.5 / 38.4, 4096 83.7 / 72.7, 16384 337 / 280; 8192 tokens of 768 to 2304 36.4 / 40.1.
 struct Linear8Plan {
-    enum Kind { kRows16, kRows32, kTiles64, kTiles128, kTiles256 } kind;
+    enum Kind { kRows16, kRows32, kTiles64Deep, kTiles64, kTiles128, kTiles256 } kind;
     bool made;              // the product's workgroups make the tokens' integers
     int split;              // of the rows' kernels: wavefronts that share the inputs
 
@@ -45,7 +46,8 @@ struct Linear8Plan {
             const int64_t waves = (outputs + 16 * rows - 1) / (16 * rows);
             while (split < row_waves(rows) && waves * split < 2048 && inputs > 256 * split) split *= 2;
         } else if (tiles128 <= 256) {
-            kind = kTiles64;
+            const int64_t tiles64 = (tokens + 63) / 64 * ((outputs + 63) / 64);
+            kind = tiles64 <= 512 ? kTiles64Deep : kTiles64;
         } else if ((tiles256 + 255) / 256 * 17 < (tiles128 + 511) / 512 * 10) {
             kind = kTiles256;
         }

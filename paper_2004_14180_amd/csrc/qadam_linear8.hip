@@ -5,6 +5,8 @@
 //   * few tokens: bound by reading the weights.  They go from memory straight into the matrix instructions' registers, once, by as many
 //     wavefronts as keep enough loads under way (k_product_rows);
 //   * many tokens: bound by the matrix instructions and by what feeds them.  Tiles of both operands pass through LDS (k_product_tiles).
+#include <type_traits>
+
 #include "qadam_layers.h"
 #include "qadam_row.h"
 
@@ -332,7 +334,7 @@ __global__ void __launch_bounds__(64 * row_waves(ROWS)) k_product_rows(ProductLa
 
 // ---- many tokens ----------------------------------------------------------------------------------
 // A workgroup makes a tile of BM tokens and BN outputs, its wavefronts WM by WN parts of it, in steps of 128 inputs.  Both operands of a
-// step pass through LDS, two steps' worth of it: while one is multiplied, the next is loaded straight from memory into the other.  A row
+// step pass through LDS, STAGES steps' worth of it: while one is multiplied, the next ones are loaded straight from memory into the others.  A row
 // of 128 integers takes its 8 runs of 16 bytes in an order of its own, run ^ (row % 8), so that the 8 lanes that LDS serves together
 // find theirs in different banks although rows are 128 bytes apart.
 //
@@ -343,7 +345,7 @@ __global__ void __launch_bounds__(64 * row_waves(ROWS)) k_product_rows(ProductLa
 // DIRECT: rows of the weights lie at addresses of 16 bytes and are loaded into LDS directly; else they pass through registers.
 constexpr int kStep = 128;
 
-template <int BM, int BN, int WM, int WN>
+template <int BM, int BN, int WM, int WN, int STAGES>
 struct Tiles {
     static constexpr int threads = 64 * WM * WN, mt = BM / WM / 32, nt = BN / WN / 32;
     static constexpr int a_bytes = BM * kStep, stage = (BM + BN) * kStep;
@@ -351,13 +353,13 @@ struct Tiles {
     static constexpr int pitch(int size) { return BN / WN * size + 16; }        // of a row of results in LDS
     // of the results: rows of each wavefront, then scale and bias of the tile's outputs
     static constexpr int columns(int size) { return WM * WN * 32 * pitch(size); }
-    static constexpr int lds = 2 * stage > columns(4) + 8 * BN ? 2 * stage : columns(4) + 8 * BN;
+    static constexpr int lds = STAGES * stage > columns(4) + 8 * BN ? STAGES * stage : columns(4) + 8 * BN;
 };
 
-template <int BM, int BN, int WM, int WN, bool DIRECT, int OT>
+template <int BM, int BN, int WM, int WN, int STAGES, bool DIRECT, int OT>
 __global__ void __launch_bounds__(64 * WM * WN) k_product_tiles(ProductLaunch L, int64_t first, int across, int down)
 {
-    typedef Tiles<BM, BN, WM, WN> S;
+    typedef Tiles<BM, BN, WM, WN, STAGES> S;
     extern __shared__ __attribute__((aligned(16))) int8_t lds[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     int tm, tn;
@@ -408,13 +410,14 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product_tiles(ProductLaunch L,
             for (int b = 0; b < S::b_loads; ++b) *(i4*)(lds + buffer * S::stage + S::a_bytes + (b * S::threads + threadIdx.x) * 16) = b_held[b];
         }
     };
-    // all of this wavefront's loads into LDS have arrived, and all wavefronts are here: the instructions that load into LDS are not
-    // waited for by a barrier alone
-    auto meet = [] {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    // This wavefront's loads into LDS have arrived but for the last `under_way`, and all wavefronts are here: the instructions that load
+    // into LDS are not waited for by a barrier alone.
+    auto meet = [](auto under_way) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(under_way.value) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
+    constexpr std::integral_constant<int, (STAGES - 2) * kLoads> kAhead;        // the loads of the steps behind the next one
 
     i16 acc[S::mt][S::nt];
 #pragma unroll
@@ -449,34 +452,40 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product_tiles(ProductLaunch L,
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    static_assert(DIRECT || S::a_loads == S::b_loads, "the second half of the loads are the weights', which are placed before the next step's");
+    static_assert(DIRECT || (S::a_loads == S::b_loads && STAGES == 2), "the second half of the loads are the weights', which are placed before the next step's");
     constexpr int kFirst = kLoads / 2;          // of a step's loads: the ones in front of the block in which the others are issued
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) load(0, 0, i);
-    place(0);
-    meet();
     const int last = steps - 1;
+    // steps behind the last one are the last one once more, unused
+    auto step_of = [&](int s) { return s < last ? s : last; };
 #pragma unroll
-    for (int i = 0; i < kFirst; ++i) load(last > 0 ? 1 : 0, 1, i);
+    for (int s = 0; s < STAGES - 1; ++s)
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) load(step_of(s), s, i);
+    place(0);
+    meet(kAhead);
+#pragma unroll
+    for (int i = 0; i < kFirst; ++i) load(step_of(STAGES - 1), STAGES - 1, i);
 #pragma unroll
     for (int q = 0; q < kOperands; ++q) read(0, 0, 0, q);
+    int buffer = 0;                             // of step s
     for (int s = 0; s < last; ++s) {
-        const int buffer = s & 1;
-        block(0, true, buffer, 1, true, s + 1, buffer ^ 1, kFirst, kLoads - kFirst);
+        const int next = buffer + 1 < STAGES ? buffer + 1 : 0, before = buffer > 0 ? buffer - 1 : STAGES - 1;
+        block(0, true, buffer, 1, true, step_of(s + STAGES - 1), before, kFirst, kLoads - kFirst);
         block(1, true, buffer, 2, false, 0, 0, 0, 0);
         block(0, true, buffer, 3, false, 0, 0, 0, 0);
-        place(buffer ^ 1);
-        meet();
-        block(1, true, buffer ^ 1, 0, true, s + 2 < last ? s + 2 : last, buffer, 0, kFirst);     // at the end the last step once more, unused
+        place(next);
+        meet(kAhead);
+        block(1, true, next, 0, true, step_of(s + STAGES), buffer, 0, kFirst);
+        buffer = next;
     }
-    block(0, true, last & 1, 1, false, 0, 0, 0, 0);
-    block(1, true, last & 1, 2, false, 0, 0, 0, 0);
-    block(0, true, last & 1, 3, false, 0, 0, 0, 0);
+    block(0, true, buffer, 1, false, 0, 0, 0, 0);
+    block(1, true, buffer, 2, false, 0, 0, 0, 0);
+    block(0, true, buffer, 3, false, 0, 0, 0, 0);
     block(1, false, 0, 0, false, 0, 0, 0, 0);
 
     // Results through LDS, 32 tokens of a wavefront at a time, so that whole lines are stored: a lane holds 4 outputs of a token, and
     // 8 bytes each in 32 rows cost a quarter of the call.
-    meet();
+    meet(std::integral_constant<int, 0>());
     typedef typename Element<OT>::T O;
     constexpr int kPitch = S::pitch(sizeof(O)), kRun = 16 / sizeof(O), kRuns = BN / WN / kRun;
     int8_t* own = lds + wave * 32 * kPitch;
@@ -521,10 +530,10 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product_tiles(ProductLaunch L,
     }
 }
 
-template <int BM, int BN, int WM, int WN, bool DIRECT>
+template <int BM, int BN, int WM, int WN, int STAGES, bool DIRECT>
 hipError_t tiles(const ProductLaunch& L)
 {
-    typedef Tiles<BM, BN, WM, WN> S;
+    typedef Tiles<BM, BN, WM, WN, STAGES> S;
     // a launch takes as many rows of tiles as keep it below 2^22 workgroups
     const int across = (int)((L.outputs + BN - 1) / BN), most = (1 << 22) / across;
     for (int64_t t = 0; t < L.tokens; t += (int64_t)most * BM) {
@@ -538,9 +547,9 @@ hipError_t tiles(const ProductLaunch& L)
             kernel<<<dim3(across * down), dim3(S::threads), S::lds, L.stream>>>(L, t, across, down);
             return hipGetLastError();
         };
-        const hipError_t e = L.out_type == QADAM_F32    ? run(k_product_tiles<BM, BN, WM, WN, DIRECT, QADAM_F32>)
-                             : L.out_type == QADAM_BF16 ? run(k_product_tiles<BM, BN, WM, WN, DIRECT, QADAM_BF16>)
-                                                        : run(k_product_tiles<BM, BN, WM, WN, DIRECT, QADAM_F16>);
+        const hipError_t e = L.out_type == QADAM_F32    ? run(k_product_tiles<BM, BN, WM, WN, STAGES, DIRECT, QADAM_F32>)
+                             : L.out_type == QADAM_BF16 ? run(k_product_tiles<BM, BN, WM, WN, STAGES, DIRECT, QADAM_BF16>)
+                                                        : run(k_product_tiles<BM, BN, WM, WN, STAGES, DIRECT, QADAM_F16>);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -585,11 +594,14 @@ hipError_t launch_product(const ProductLaunch& L, const TokensLaunch& X)
     switch (p.kind) {
     case Linear8Plan::kRows16: return rows<1, 1, 4, false>(L, X, p.split);
     case Linear8Plan::kRows32: return rows<2, 2, 4, false>(L, X, p.split);
-    case Linear8Plan::kTiles64: return direct ? tiles<64, 64, 2, 2, true>(L) : tiles<64, 64, 2, 2, false>(L);
-    case Linear8Plan::kTiles256:
-        if (direct) return tiles<256, 256, 4, 2, true>(L);
+    case Linear8Plan::kTiles64Deep:
+        if (direct) return tiles<64, 64, 2, 2, 3, true>(L);
         [[fallthrough]];
-    default: return direct ? tiles<128, 128, 2, 2, true>(L) : tiles<128, 128, 2, 2, false>(L);
+    case Linear8Plan::kTiles64: return direct ? tiles<64, 64, 2, 2, 2, true>(L) : tiles<64, 64, 2, 2, 2, false>(L);
+    case Linear8Plan::kTiles256:
+        if (direct) return tiles<256, 256, 4, 2, 2, true>(L);
+        [[fallthrough]];
+    default: return direct ? tiles<128, 128, 2, 2, 2, true>(L) : tiles<128, 128, 2, 2, 2, false>(L);
     }
 }
 

@@ -41,7 +41,7 @@ def test_the_products_plan(tmp_path):
                 CHECK(!q.made && p.kind == q.kind, "kind");
                 CHECK(!p.made || (p.kind == Linear8Plan::kRows16 && tokens * linear8_padded(inputs) <= kMadeInputs), "%lld %d", tokens, inputs);
                 CHECK(tokens > 16 || p.kind == Linear8Plan::kRows16, "few tokens");
-                CHECK(tokens <= 32 || p.kind >= Linear8Plan::kTiles64, "many tokens");
+                CHECK(tokens <= 32 || p.kind >= Linear8Plan::kTiles64Deep, "many tokens");
                 const int waves = row_waves(p.kind == Linear8Plan::kRows16 ? 1 : 2);
                 CHECK(p.split >= 1 && p.split <= waves && waves % p.split == 0, "split %d", p.split);
             }
