@@ -499,7 +499,7 @@ int qadam_linear8_forward(qadam_linear8_t h, int64_t num_tokens, const void* x, 
                           const int8_t* weight, int64_t weight_stride, const float* weight_scales, int32_t k_x, const void* bias,
                           int32_t bias_type, void* out, int32_t out_type, int64_t out_stride, void* stream);
 
-/* Sampling of one token per row of `vocab` (1 to 2^24) logits from given random numbers.  Tokens are taken in descending order of their logits,
+/* Sampling of one token per row of `vocab` (1 to 2^22) logits from given random numbers.  Tokens are taken in descending order of their logits,
  * the lower index first among equals, and every filter keeps the first ones of that order:
  *     mass_i = round(2^40 exp((logit_i - largest) / temperature)) in fp64, an integer, so that sums are exact;
  *     top_k > 0      the first top_k;

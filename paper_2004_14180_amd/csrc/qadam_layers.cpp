@@ -192,7 +192,7 @@ int qadam_linear8_forward(qadam_linear8_t h, int64_t num_tokens, const void* x, 
     const TokensLaunch X{num_tokens, x, x_stride, there ? nullptr : h->codes.get(), padded, h->scales.get(), K, padded, x_type, s};
     QADAM_HIP(launch_product({num_tokens, h->outputs, there ? static_cast<const int8_t*>(x) : h->codes.get(), there ? x_stride : padded,
                               x_scales ? x_scales : h->scales.get(), weight, weight_stride, weight_scales, bias, out, out_stride,
-                              std::ldexp(1.0f, -(k_x + 1)), K, bias_type, out_type, s}, X));
+                              weight_scales ? 1.0f : std::ldexp(1.0f, -(k_x + 1)), K, bias_type, out_type, s}, X));
     return QADAM_OK;
 }
 
@@ -201,7 +201,8 @@ int qadam_sampler_init(qadam_sampler_t* out, int64_t vocab, int64_t max_rows)
     if (!out) return fail(QADAM_EINVAL, "null argument");
     *out = nullptr;
     if (vocab < 1 || max_rows < 0) return fail(QADAM_EINVAL, "vocab < 1 or max_rows < 0");
-    if (vocab > 1 << 24 || max_rows > 1 << 24) return fail(QADAM_ERANGE, "more than 2^24 tokens of the vocabulary, or more than 2^24 rows");
+    if (vocab > 1 << 22) return fail(QADAM_ERANGE, "a vocabulary of more than 2^22: its masses' sum may not fit 64 bits");
+    if (max_rows > 1 << 24) return fail(QADAM_ERANGE, "more than 2^24 rows");
     return guarded([&]() -> int {
         std::unique_ptr<qadam_sampler_ctx> h(new qadam_sampler_ctx);
         h->vocab = vocab; h->max_rows = max_rows;

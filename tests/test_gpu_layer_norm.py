@@ -8,7 +8,7 @@ from paper_2004_14180_amd import LayerNorm, QAdamError
 
 pytestmark = pytest.mark.gpu
 
-DIMS = [1, 2, 7, 8, 9, 64, 129, 256, 511, 512, 513, 768, 1001, 1024, 1025, 2040, 2048, 2049, 4096, 4097, 5003, 8192, 8193, 20001]
+DIMS = [1, 2, 7, 8, 9, 64, 127, 128, 129, 256, 511, 512, 513, 768, 1001, 1024, 1025, 2040, 2048, 2049, 4096, 4097, 5003, 8192, 8193, 20001]
 
 
 def _gen(seed):
@@ -226,6 +226,25 @@ def test_another_stream():
     q.forward(x, w, None, out, stream=side)
     side.synchronize()
     assert torch.equal(out, want)
+
+
+def test_the_widest_row_and_more_than_2_to_31_elements():
+    gen = _gen(5)
+    x = torch.randn(2, 1 << 20, generator=gen, device="cuda")
+    _, mean, rstd = _check_forward(x, None, None, F32)
+    _check_grad(x.flip(0), x, None, mean, rstd, F32, F32)
+    # 2^21 + 5 rows of 1024 in the same memory as their results
+    rows, dim = (1 << 21) + 5, 1024
+    x = torch.empty(rows, dim, dtype=BF16, device="cuda").normal_(generator=gen)
+    last, first = x[-7:].clone(), x[:7].clone()
+    mean, rstd = torch.zeros(rows, device="cuda"), torch.zeros(rows, device="cuda")
+    q = LayerNorm(dim)
+    q.forward(x, None, None, x, mean, rstd)
+    for got, was, m, r in ((x[-7:], last, mean[-7:], rstd[-7:]), (x[:7], first, mean[:7], rstd[:7])):
+        y, m64, r64, ty, tm, tr = layer_norm64(was, None, None, 1e-5)
+        close(m, m64, tm, "mean")
+        close(r, r64, tr, "rstd")
+        close(got, y, rounded(ty, y, BF16), "out")
 
 
 def test_refusals():

@@ -148,9 +148,8 @@ def test_layouts_and_no_tokens():
     q.forward(torch.zeros(0, 40, device="cuda"), w, torch.zeros(0, 24, device="cuda"), k_x=6)
 
 
-@pytest.mark.parametrize("tokens", [1, 40, 300])
-def test_recorded_calls(tokens):
-    inputs, outputs = 768, 3000
+@pytest.mark.parametrize("tokens,inputs,outputs", [(1, 768, 3000), (20, 768, 3000), (40, 768, 3000), (300, 768, 3000), (2500, 128, 3000), (5000, 128, 5120)])
+def test_recorded_calls(tokens, inputs, outputs):
     gen = _gen(5)
     x, w = torch.randn(tokens, inputs, generator=gen, device="cuda"), _weights(gen, outputs, inputs)
     q = Linear8(outputs, inputs, tokens)
@@ -168,6 +167,42 @@ def test_recorded_calls(tokens):
         torch.cuda.synchronize()
         q.forward(x, w, want, k_x=6)
         assert torch.equal(got, want), k
+
+
+@pytest.mark.parametrize("tokens", [1, 30, 5000])
+def test_another_stream(tokens):
+    gen = _gen(8)
+    x, w = torch.randn(tokens, 144, generator=gen, device="cuda"), _weights(gen, 5120, 144)
+    q, side = Linear8(5120, 144, tokens), torch.cuda.Stream()
+    out, want = torch.zeros(tokens, 5120, device="cuda"), torch.zeros(tokens, 5120, device="cuda")
+    q.forward(x, w, want, k_x=6)
+    torch.cuda.synchronize()
+    q.forward(x, w, out, k_x=6, stream=side)
+    side.synchronize()
+    assert torch.equal(out, want)
+
+
+def test_more_than_2_to_31_elements():
+    """Results and weights beyond 32-bit offsets."""
+    gen = _gen(9)
+    tokens, inputs, outputs = 70_000, 16, 33_000
+    x, w = torch.randn(tokens, inputs, generator=gen, device="cuda"), _weights(gen, outputs, inputs)
+    out = torch.empty(tokens, outputs, dtype=BF16, device="cuda")
+    assert out.numel() > 1 << 31
+    Linear8(outputs, inputs, tokens).forward(x, w, out, k_x=6)
+    for rows in (slice(0, 3), slice(65_070, 65_080), slice(tokens - 3, tokens)):
+        codes, s = token_codes(x[rows])
+        _same(out[rows], linear8(codes, s, w, 2.0 ** -7, None, BF16))
+    del out
+    outputs, stride = 40, 60_000_001                    # rows of the weights far apart
+    whole = torch.zeros(outputs * stride, dtype=torch.int8, device="cuda")
+    w = whole.view(outputs, stride)[:, 1:1 + inputs]
+    w.copy_(_weights(gen, outputs, inputs))
+    for n in (1, 33, 400):
+        codes, s = token_codes(x[:n])
+        out = torch.zeros(n, outputs, device="cuda")
+        Linear8(outputs, inputs, n).forward(x[:n], w, out, k_x=6)
+        _same(out, linear8(codes, s, w, 2.0 ** -7, None, F32))
 
 
 def test_refusals():

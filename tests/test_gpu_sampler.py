@@ -34,7 +34,7 @@ def _logits(rows, vocab, dtype, seed=0, std=3.0, gap=0):
     return x, torch.rand(rows, generator=gen, device="cuda")
 
 
-@pytest.mark.parametrize("vocab", [1, 2, 3, 63, 64, 65, 1000, 1023, 1024, 1025, 4097, 32003, 50257, 70001])
+@pytest.mark.parametrize("vocab", [1, 2, 3, 7, 8, 9, 17, 63, 64, 65, 1000, 1023, 1024, 1025, 4097, 32003, 50257, 70001])
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 def test_sizes_and_types(vocab, dtype):
     x, u = _logits(12, vocab, dtype, gap=3)
@@ -134,6 +134,25 @@ def test_many_rows_and_one_row_for_all():
     _check(x[:1].expand(500, 600), u[:500], top_p=0.8)
 
 
+def test_the_largest_vocabulary():
+    """All masses equal and as large as they can be: their sum is 2^62."""
+    x = torch.zeros(1, 1 << 22, device="cuda").half()
+    for u in (0.0, 0.3, 1.0 - 2.0 ** -24):
+        for kw in (dict(), dict(top_p=0.5), dict(top_k=(1 << 22) - 1), dict(min_p=1.0)):
+            _check(x, torch.tensor([u], device="cuda"), **kw)
+
+
+def test_another_stream():
+    x, u = _logits(64, 9000, F32)
+    q, side = Sampler(9000, 64), torch.cuda.Stream()
+    out, want = torch.zeros(64, dtype=torch.int64, device="cuda"), torch.zeros(64, dtype=torch.int64, device="cuda")
+    q.sample(x, u, want, top_p=0.9)
+    torch.cuda.synchronize()
+    q.sample(x, u, out, top_p=0.9, stream=side)
+    side.synchronize()
+    assert torch.equal(out, want)
+
+
 def test_a_large_vocabulary():
     x, u = _logits(3, 1 << 20, BF16)
     _check(x, u)
@@ -183,6 +202,6 @@ def test_no_rows_and_refusals():
                dict(logits=None), dict(u=None), dict(out=None), dict(logits=z(4, 16).cpu()), dict(top_p=z(4).cpu())):
         with pytest.raises((ValueError, QAdamError)):
             q.sample(**{**good, **kw})
-    for bad in [(0, 1), (1, -1), ((1 << 24) + 1, 1), (1, (1 << 24) + 1)]:
+    for bad in [(0, 1), (1, -1), ((1 << 22) + 1, 1), (1, (1 << 24) + 1)]:
         with pytest.raises(QAdamError):
             Sampler(*bad)
