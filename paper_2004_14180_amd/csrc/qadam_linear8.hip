@@ -84,17 +84,27 @@ __device__ __forceinline__ void store_codes(int8_t* p, uint64_t v, int n)
         if (i < n) global(p)[i] = (int8_t)(v >> 8 * i);
 }
 
-// One workgroup per token; up to HELD * 2048 inputs stay in registers between the maximum and the integers, beyond that the row is read
-// again.  Integers up to `padded` are written, zeros from `inputs` on.
+// A workgroup per token, and its next one under way; up to HELD * 2048 inputs stay in registers between the maximum and the integers, beyond
+// that the row is read again.  Integers up to `padded` are written, zeros from `inputs` on.
 template <int HELD>
 __global__ void __launch_bounds__(kThreads) k_tokens(TokensLaunch L)
 {
     __shared__ uint32_t most[2][kThreads / 64];
     constexpr int kAcross = kThreads * kRowRun;
+    const int first = threadIdx.x * kRowRun;
+    f8 next[HELD];
+    auto load = [&](int64_t t) {
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) {
+            next[k] = 0.0f;
+            const int at = first + k * kAcross;
+            if (at < L.inputs) next[k] = load_part(L.x, L.x_type, t * L.x_stride + at, L.inputs - at);
+        }
+    };
+    if (L.x_type != QADAM_CODES8) load(blockIdx.x);
     int turn = 0;
     for (int64_t t = blockIdx.x; t < L.tokens; t += gridDim.x, turn ^= 1) {
         int8_t* to = L.codes + t * L.codes_stride;
-        const int first = threadIdx.x * kRowRun;
         if (L.x_type == QADAM_CODES8) {
             const int8_t* from = static_cast<const int8_t*>(L.x) + t * L.x_stride;
             for (int at = first; at < L.padded; at += kAcross) {
@@ -110,12 +120,10 @@ __global__ void __launch_bounds__(kThreads) k_tokens(TokensLaunch L)
         uint32_t m = 0;
 #pragma unroll
         for (int k = 0; k < HELD; ++k) {
-            x[k] = 0.0f;
-            const int at = first + k * kAcross;
-            if (at < L.inputs) x[k] = load_part(L.x, L.x_type, t * L.x_stride + at, L.inputs - at);
+            x[k] = next[k];
+            m = larger(m, largest_of(x[k]));
         }
-#pragma unroll
-        for (int k = 0; k < HELD; ++k) m = larger(m, largest_of(x[k]));
+        if (t + gridDim.x < L.tokens) load(t + gridDim.x);
         for (int at = first + HELD * kAcross; at < L.inputs; at += kAcross)
             m = larger(m, largest_of(load_part(L.x, L.x_type, t * L.x_stride + at, L.inputs - at)));
         m = wave_largest(m);
@@ -175,8 +183,7 @@ __device__ __forceinline__ void store_some(typename Element<OT>::T* p, typename 
 // ---- few tokens -----------------------------------------------------------------------------------
 // A wavefront takes ROWS tiles of 16 rows of the weights and COLS tiles of 16 tokens, and a part of the inputs; `split` of a workgroup's
 // wavefronts share the rows and add their sums in LDS.  A lane's 16 integers of a matrix instruction are 16 bytes of one row, so the
-// weights come from memory into their places, at any address.  AHEAD chunks of 64 inputs are loaded together, of weights and tokens, while
-// the ones before are multiplied.
+// weights come from memory into their places, at any address.  AHEAD chunks of 64 inputs are under way at a time.
 // MADE: the workgroup makes the tokens' integers itself, in LDS, which saves the launch that would, while its first weights are on the way.
 // a barrier for what lies in LDS: loads from memory stay under way
 __device__ __forceinline__ void lds_barrier()
@@ -227,26 +234,27 @@ __global__ void __launch_bounds__(64 * row_waves(ROWS)) k_product_rows(ProductLa
         there[j] = t < L.tokens;
         token[j] = MADE ? lds + (there[j] ? t : 0) * padded : L.codes + (there[j] ? t : 0) * L.codes_stride;
     }
+    // chunks under way: chunk c of this wavefront's in place (c - begin) % AHEAD; zeros behind the last one
     i4 w[ROWS][AHEAD], x[COLS][AHEAD];
-    auto load_rows = [&](int c) {
+    auto load_rows = [&](int c, int u) {
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
-#pragma unroll
-            for (int i = 0; i < ROWS; ++i) w[i][u] = c + u < end ? load_weights(row[i], (c + u) * 64 + k0, L.inputs) : (i4)0;
+        for (int i = 0; i < ROWS; ++i) w[i][u] = c < end ? load_weights(row[i], c * 64 + k0, L.inputs) : (i4)0;
     };
-    auto load_tokens = [&](int c) {
+    auto load_tokens = [&](int c, int u) {
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
-#pragma unroll
-            for (int j = 0; j < COLS; ++j) {
-                x[j][u] = 0;
-                if (c + u < end && there[j]) {
-                    if constexpr (MADE) x[j][u] = *(const i4*)(token[j] + (c + u) * 64 + k0);
-                    else x[j][u] = *(const QADAM_GLOBAL i4*)(token[j] + (c + u) * 64 + k0);
-                }
+        for (int j = 0; j < COLS; ++j) {
+            x[j][u] = 0;
+            if (c < end && there[j]) {
+                if constexpr (MADE) x[j][u] = *(const i4*)(token[j] + c * 64 + k0);
+                else x[j][u] = *(const QADAM_GLOBAL i4*)(token[j] + c * 64 + k0);
             }
+        }
     };
-    load_rows(begin);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+        load_rows(begin + u, u);
+        if constexpr (!MADE) load_tokens(begin + u, u);
+    }
     if constexpr (MADE) {
         if (threadIdx.x < 16) most[threadIdx.x] = 0;
         lds_barrier();
@@ -263,34 +271,24 @@ __global__ void __launch_bounds__(64 * row_waves(ROWS)) k_product_rows(ProductLa
         }
         lds_barrier();
     }
-    load_tokens(begin);
     i4 acc[ROWS][COLS];
 #pragma unroll
     for (int i = 0; i < ROWS; ++i)
 #pragma unroll
         for (int j = 0; j < COLS; ++j) acc[i][j] = 0;
 #pragma unroll 1
-    for (int c = begin; c < end; c += AHEAD) {
-        i4 w_now[ROWS][AHEAD], x_now[COLS][AHEAD];
+    for (int c = begin; c < end; c += AHEAD)
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-#pragma unroll
-            for (int i = 0; i < ROWS; ++i) w_now[i][u] = w[i][u];
-#pragma unroll
-            for (int j = 0; j < COLS; ++j) x_now[j][u] = x[j][u];
-        }
-        if (c + AHEAD < end) {
-            load_rows(c + AHEAD);
-            load_tokens(c + AHEAD);
-        }
-        // chunks behind the end are zeros
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
+            if (c + u >= end) break;
+            if constexpr (MADE) load_tokens(c + u, u);
 #pragma unroll
             for (int j = 0; j < COLS; ++j)
 #pragma unroll
-                for (int i = 0; i < ROWS; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w_now[i][u], x_now[j][u], acc[i][j], 0, 0, 0);
-    }
+                for (int i = 0; i < ROWS; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i][u], x[j][u], acc[i][j], 0, 0, 0);
+            load_rows(c + AHEAD + u, u);
+            if constexpr (!MADE) load_tokens(c + AHEAD + u, u);
+        }
     if (split > 1) {
         __syncthreads();
         i4* sums = (i4*)lds;
