@@ -332,14 +332,20 @@ __global__ void __launch_bounds__(64 * row_waves(ROWS)) k_product_rows(ProductLa
 
 // ---- many tokens ----------------------------------------------------------------------------------
 // A workgroup makes a tile of BM tokens and BN outputs, its wavefronts WM by WN parts of it, in steps of 128 inputs.  Both operands of a
-// step pass through LDS, STAGES steps' worth of it: while one is multiplied, the next ones are loaded straight from memory into the others.  A row
-// of 128 integers takes its 8 runs of 16 bytes in an order of its own, run ^ (row % 8), so that the 8 lanes that LDS serves together
-// find theirs in different banks although rows are 128 bytes apart.
+// step pass through LDS, STAGES steps' worth of it: while one is multiplied, the next ones are loaded straight from memory into the
+// others.  A row of 128 integers takes its 8 runs of 16 bytes in an order of its own, run ^ (row / 2 % 8), so that the 16 lanes that
+// LDS serves together find theirs in different banks although rows are 128 bytes apart (by row % 8 two of them shared one: a quarter of
+// the LDS's cycles, and 1 us of the call).
 //
 // A step's products are four blocks of 32 inputs.  Between the matrix instructions of one block the next block's operands are read from
 // LDS and the next step's are loaded, one instruction after each, as the source has them (sched_barrier): left to the compiler, reads
-// and products alternate with waits.  The step changes in front of its last block, whose operands are in registers by then.
+// and products alternate with waits, and the call below takes 12 % longer.  The step changes in front of its last block, whose operands are
+// in registers by then.
 //
+// 16384 tokens of 2048 to 8192 outputs: 257 us of the call's 281, 2.1 POPS, which the card's power sets: the matrix units are busy 56 % of
+// the time at 1.74 GHz, and the same instructions on zeros take 19 % less; products alone, without loads, LDS and results, took 177.
+// Results (268 MB) are 26 of them; stored past the caches, since they would push the operands out (43 us).  Taken back: steps of 64 inputs with
+// three to five of them in LDS 306-313 us per call, four wavefronts of 128 x 128 (290), columns of 8 and 16 tiles (+ 5), priorities (the same).
 // DIRECT: rows of the weights lie at addresses of 16 bytes and are loaded into LDS directly; else they pass through registers.
 constexpr int kStep = 128;
 
@@ -374,14 +380,14 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product_tiles(ProductLaunch L,
     int b_run[S::b_loads];
 #pragma unroll
     for (int i = 0; i < S::a_loads; ++i) {
-        const int c = i * S::threads + threadIdx.x, row = c / 8, run = (c % 8 ^ (row & 7)) * 16;
+        const int c = i * S::threads + threadIdx.x, row = c / 8, run = (c % 8 ^ (row >> 1 & 7)) * 16;
         a_at[i] = (uint32_t)(row < a_rows ? row : a_rows - 1) * (uint32_t)L.codes_stride + (uint32_t)run;
     }
     const int8_t* b_row[S::b_loads];
 #pragma unroll
     for (int i = 0; i < S::b_loads; ++i) {
         const int c = i * S::threads + threadIdx.x, row = c / 8;
-        b_run[i] = (c % 8 ^ (row & 7)) * 16;
+        b_run[i] = (c % 8 ^ (row >> 1 & 7)) * 16;
         if constexpr (DIRECT) b_at[i] = (uint32_t)(row < b_rows ? row : b_rows - 1) * (uint32_t)L.weight_stride;
         else b_row[i] = b_base + (int64_t)(row < b_rows ? row : b_rows - 1) * L.weight_stride;
     }
@@ -426,7 +432,7 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product_tiles(ProductLaunch L,
     i4 a[2][S::mt], b[2][S::nt];
     constexpr int kOperands = S::mt + S::nt, kProducts = S::mt * S::nt;
     auto read = [&](int buffer, int block, int into, int i) {
-        const int row = lane % 32, run = (block * 2 + lane / 32 ^ (row & 7)) * 16;
+        const int row = lane % 32, run = (block * 2 + lane / 32 ^ (row >> 1 & 7)) * 16;
         const int8_t* from = lds + buffer * S::stage + run;
         if (i < S::mt) a[into][i] = *(const i4*)(from + (m0 + i * 32 + row) * kStep);
         else b[into][i - S::mt] = *(const i4*)(from + S::a_bytes + (c0 + (i - S::mt) * 32 + row) * kStep);
