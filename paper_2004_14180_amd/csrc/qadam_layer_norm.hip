@@ -1,4 +1,9 @@
 // gfx950 kernels of layer norm and its gradient.
+//
+// Both are bound by memory: a row is read once and stays in registers over its sums, the next one is on the way meanwhile, and results
+// stream past the caches.  16384 rows of 2048 bf16: forward 24 us (134 MB, 5.6 TB/s), backward 36 (201 MB, 5.6 TB/s) and 5 for the sums over
+// rows; 8191 rows of 1001 f16 at odd addresses 14.7 and 3.8; 1024 rows of 768 fp32 4.9 and 4.3, which are two chains of loads.
+// The variance is taken of differences from the mean, in a second pass over registers: sums of squares would cancel where rows lie far from 0.
 #include <type_traits>
 
 #include "qadam_layers.h"
@@ -296,7 +301,8 @@ __global__ void __launch_bounds__(64 * kLongWaves) k_layer_norm_grad_long(NormBa
     }
 }
 
-// dweight and dbias: a workgroup per kSumColumns columns, whose threads take a slice of the workgroups' sums each, in fp64.
+// dweight and dbias: a workgroup per kSumColumns columns, whose threads take a slice of the workgroups' sums each, in fp64.  512 sums of 2048
+// columns, 8 MB: 4.8 us; with 64 columns and 16 slices in a workgroup, so on a quarter of the CUs, 9.7.
 constexpr int kSumThreads = 1024, kSumColumns = 16, kSumSlices = kSumThreads / kSumColumns;
 
 __device__ __forceinline__ void store_one(void* p, int type, int64_t i, float x)

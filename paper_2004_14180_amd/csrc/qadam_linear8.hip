@@ -185,6 +185,10 @@ __device__ __forceinline__ void store_some(typename Element<OT>::T* p, typename 
 // wavefronts share the rows and add their sums in LDS.  A lane's 16 integers of a matrix instruction are 16 bytes of one row, so the
 // weights come from memory into their places, at any address.  AHEAD chunks of 64 inputs are under way at a time.
 // MADE: the workgroup makes the tokens' integers itself, in LDS, which saves the launch that would, while its first weights are on the way.
+//
+// One token of 768 to 50257 outputs, 38.6 MB of weights: 10.1 us per call, the kernel 9.6, of which 2.5 pass until the first product; the rest
+// is 5.4 TB/s.  AHEAD 2, 6, 8, 12: 9.6, 10.2, 10.1, 11.4; with a launch for the integers in front 12.  Four wavefronts in a workgroup, where
+// eight took 13.1: they hold the registers of a SIMD in larger lots.
 // a barrier for what lies in LDS: loads from memory stay under way
 __device__ __forceinline__ void lds_barrier()
 {
@@ -338,14 +342,15 @@ __global__ void __launch_bounds__(64 * row_waves(ROWS)) k_product_rows(ProductLa
 // the LDS's cycles, and 1 us of the call).
 //
 // A step's products are four blocks of 32 inputs.  Between the matrix instructions of one block the next block's operands are read from
-// LDS and the next step's are loaded, one instruction after each, as the source has them (sched_barrier): left to the compiler, reads
-// and products alternate with waits, and the call below takes 12 % longer.  The step changes in front of its last block, whose operands are
-// in registers by then.
+// LDS and the next step's are loaded, one instruction after each, as the source has them (sched_barrier): in the compiler's order reads
+// and products alternate with waits (the bare product of the sizes below, plain stores: 312 us, so 300).  The step changes in front of its
+// last block, whose operands are in registers by then.
 //
-// 16384 tokens of 2048 to 8192 outputs: 257 us of the call's 281, 2.1 POPS, which the card's power sets: the matrix units are busy 56 % of
-// the time at 1.74 GHz, and the same instructions on zeros take 19 % less; products alone, without loads, LDS and results, took 177.
-// Results (268 MB) are 26 of them; stored past the caches, since they would push the operands out (43 us).  Taken back: steps of 64 inputs with
-// three to five of them in LDS 306-313 us per call, four wavefronts of 128 x 128 (290), columns of 8 and 16 tiles (+ 5), priorities (the same).
+// 16384 tokens of 2048 to 8192 outputs: about 256 of the call's 280 us, 2.1 POPS, which the card's power sets: the matrix units are busy 56 %
+// of the time at 1.74 GHz, and the bare product without results takes 268 us of usual integers and 217 of zeros; its matrix instructions
+// alone, without loads and LDS, take 177.  Results (268 MB) are stored past the caches, since they would push the operands out: 333 us per
+// call with ordinary stores, 291 so.  Taken back: steps of 64 inputs with three to five of them in LDS (306-313, 287), four wavefronts of
+// 128 x 128 (bare 268, 256), columns of 8 and 16 tiles (291, 286), a higher priority of the products (the same).
 // DIRECT: rows of the weights lie at addresses of 16 bytes and are loaded into LDS directly; else they pass through registers.
 constexpr int kStep = 128;
 

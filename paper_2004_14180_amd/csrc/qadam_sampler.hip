@@ -4,12 +4,17 @@
 // masses, and the token is where the sum in that order passes u times the smallest of them.  Masses are integers, whose sums are the
 // same in any order: workgroups add them in LDS with atomics and the result is the same on every run.  The logits are sorted into
 // kBins bins of equal width, from the largest on down to where masses vanish.  Bins are in the order of the logits, so that a sum is
-// found by looking through the bins and then through one bin's tokens, which are few and are sorted:
-//   * top_k up to kMostTopK: the largest logit of each thread gives a bin that at least top_k tokens lie in or in front of; those (a few more than
-//     top_k) are sorted, and no mass of another token is taken.  The same where min_p is the only filter: it names the bin;
-//   * else the masses of all tokens are added by bins (about 20 operations in fp64 each, which is most of the time), and each of
-//     the sums that are asked for takes one more pass, which collects a bin's tokens;
+// found by looking through the bins and then through one bin's tokens, which are few:
+//   * top_k up to kMostTopK: the largest logit of each thread gives a bin that at least top_k tokens lie in or in front of; those (a few
+//     more than top_k) are listed, and no mass of another token is taken.  The same where min_p is the only filter: it names the bin;
+//   * else the masses of all tokens are added by bins, and each of the sums that are asked for takes one more pass, which lists a
+//     bin's tokens;
 //   * tokens of a bin that are more than kList (2048, that is many equal logits): by digits of the logits, a pass for each.
+//
+// Bound by the instructions of one CU per row.  One row of 50257 fp32, top_k 50: 14.4 us, of which the largest logit takes 2.6, the
+// threads' bins 2.5, the list 5.4 and its sums 2.  top_p alone, fp32: 34.5; of bf16's 92 thousand cycles the masses take 38 (31 operations per
+// token, most of them in fp64) and the two lists 12 to 21 each; 256 such rows 44.  33 rows of 32003 fp16 28.5;
+// by digits throughout they took 300.  kBins of 4096 and 8192: 256 rows of 50257 41.7 and 45.1, 1000 rows of 5000 57.0, 59.7 and 74.0.
 #include "qadam_layers.h"
 #include "qadam_row.h"
 
