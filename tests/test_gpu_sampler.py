@@ -142,6 +142,21 @@ def test_the_largest_vocabulary():
             _check(x, torch.tensor([u], device="cuda"), **kw)
 
 
+def test_more_rows_than_a_launch():
+    rows = (1 << 21) + 3
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    x, u = torch.randn(rows, 9, generator=gen, device="cuda").half(), torch.rand(rows, generator=gen, device="cuda")
+    out = torch.full((rows,), -7, dtype=torch.int32, device="cuda")
+    q = Sampler(9, rows)
+    q.sample(x, u, out, temperature=0.0)
+    top, first = x.max(1, keepdim=True).values, torch.arange(9, device="cuda")
+    assert torch.equal(out.long(), torch.where(x == top, first, 9).min(1).values)
+    q.sample(x, u, out, top_p=0.7)
+    for r in (0, 1, (1 << 21) - 1, 1 << 21, rows - 1):
+        assert out[r].item() == layer_util.sample(x[r], u[r].item(), 1.0, 0, 0.7, 0.0)
+    assert q.get_status() == 0
+
+
 def test_another_stream():
     x, u = _logits(64, 9000, F32)
     q, side = Sampler(9000, 64), torch.cuda.Stream()
