@@ -58,6 +58,15 @@ __device__ __forceinline__ void row_sums(float& x, float& y, float* at)
     }
 }
 
+// a b + c, rounded once: the library is built without contraction
+__device__ __forceinline__ f8 fused(f8 a, f8 b, f8 c)
+{
+    f8 y;
+#pragma unroll
+    for (int i = 0; i < kRowRun; ++i) y[i] = __builtin_fmaf(a[i], b[i], c[i]);
+    return y;
+}
+
 // What a lane holds of a row: RUNS runs of kRowRun elements, LANES lanes apart.
 template <int LANES, int RUNS>
 struct Lane {
@@ -125,13 +134,17 @@ __global__ void __launch_bounds__(group_threads(LANES)) k_layer_norm(NormForward
 #pragma unroll
         for (int k = 0; k < RUNS; ++k) {
             x[k] -= mean;
+            if (l.left(k) < kRowRun) {
 #pragma unroll
-            for (int i = 0; i < kRowRun; ++i) squares += i < l.left(k) ? x[k][i] * x[k][i] : 0.0f;
+                for (int i = 0; i < kRowRun; ++i) x[k][i] = i < l.left(k) ? x[k][i] : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < kRowRun; ++i) squares = __builtin_fmaf(x[k][i], x[k][i], squares);
         }
         const float rstd = 1.0f / sqrtf(row_sum<LANES>(squares, sums[turn][1]) * inv + L.eps);
 #pragma unroll
         for (int k = 0; k < RUNS; ++k)
-            if (l.left(k) > 0) store_part(L.out, L.out_type, row * L.out_stride + l.at(k), x[k] * rstd * w[k] + b[k], l.left(k));
+            if (l.left(k) > 0) store_part(L.out, L.out_type, row * L.out_stride + l.at(k), fused(x[k] * rstd, w[k], b[k]), l.left(k));
         if (l.lane == 0) {
             if (L.mean) global(L.mean)[row] = mean;
             if (L.rstd) global(L.rstd)[row] = rstd;
@@ -210,20 +223,20 @@ __global__ void __launch_bounds__(group_threads(LANES)) k_layer_norm_grad(NormBa
             xh[k] = (to_float<XT, kRowRun>(raw_x[k]) - mean) * r;
             // no dout behind the row's end: nothing there enters a sum
             db[k] += dy;
-            dw[k] += dy * xh[k];
+            dw[k] = fused(dy, xh[k], dw[k]);
             g[k] = dy * w[k];
 #pragma unroll
             for (int i = 0; i < kRowRun; ++i) {
                 sum += g[k][i];
-                along += g[k][i] * xh[k][i];
+                along = __builtin_fmaf(g[k][i], xh[k][i], along);
             }
         }
         if (row + step < L.rows) load(row + step);
         row_sums<LANES>(sum, along, sums[turn]);
-        const float c1 = sum * inv, c2 = along * inv;
+        const float c1 = sum * inv, c2 = -(along * inv);
 #pragma unroll
         for (int k = 0; k < RUNS; ++k)
-            if (l.left(k) > 0) store_part(L.dx, L.dx_type, row * L.dx_stride + l.at(k), (g[k] - c1 - xh[k] * c2) * r, l.left(k));
+            if (l.left(k) > 0) store_part(L.dx, L.dx_type, row * L.dx_stride + l.at(k), fused(xh[k], (f8)c2, g[k] - c1) * r, l.left(k));
     }
     if (!L.dweight && !L.dbias) return;
     float* out = L.partial + (int64_t)blockIdx.x * 2 * L.dim;
