@@ -167,26 +167,20 @@ struct Row {
 
     __device__ __forceinline__ float logit(int i) const { return fminf((float)global(logits)[i], kMost); }
 
-    // kRowRun logits from `start` on; minus infinity in front of `from`, where another thread has them, and behind the row's end
+    // kRowRun logits from `start` on, which is in front of `from` where the row ends before a whole run
     __device__ __forceinline__ typename Run<LT, kRowRun>::V load(int from, int* start) const
     {
         *start = SHORT || from + kRowRun <= vocab ? from : vocab - kRowRun;
-        typename Run<LT, kRowRun>::V raw;
-        if constexpr (!SHORT) {
-            raw = load_raw<LT, kRowRun, false>(logits + *start);
-        } else {
-            raw = (T)-kInf;
+        if constexpr (!SHORT) return load_raw<LT, kRowRun, false>(logits + *start);
+        typename Run<LT, kRowRun>::V raw = (T)-kInf;
 #pragma unroll
-            for (int e = 0; e < kRowRun - 1; ++e)
-                if (e < vocab) raw[e] = global(logits)[e];
-        }
-#pragma unroll
-        for (int e = 0; e < kRowRun; ++e)
-            if (!SHORT && *start + e < from) raw[e] = (T)-kInf;
+        for (int e = 0; e < kRowRun - 1; ++e)
+            if (e < vocab) raw[e] = global(logits)[e];
         return raw;
     }
 
-    // body(run of logits, index of the first): all of the row, a thread's next run under way meanwhile
+    // body(run of logits, index of the first): all of the row, minus infinity where another run has a logit too; a thread's next run is under
+    // way meanwhile, so what was loaded is not looked at before its turn
     template <typename F>
     __device__ __forceinline__ void each(F&& body) const
     {
@@ -198,6 +192,10 @@ struct Row {
         while (true) {
             f8 x = to_float<LT, kRowRun>(next);
             const int start = next_start;
+            if (start < at) {
+#pragma unroll
+                for (int e = 0; e < kRowRun; ++e) x[e] = start + e < at ? -kInf : x[e];
+            }
             if (infinite) {
 #pragma unroll
                 for (int e = 0; e < kRowRun; ++e) x[e] = fminf(x[e], kMost);
