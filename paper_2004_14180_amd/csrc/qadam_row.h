@@ -21,6 +21,20 @@ __device__ __forceinline__ typename Run<TYPE, kRowRun>::V load_part(const void* 
     return v;
 }
 
+// Of a run that lies `behind` elements behind its place, where a row ended, the elements from there on; zeros behind them.  Loads of whole
+// runs are not waited for until they are used, which those of single elements under conditions are.
+template <int TYPE>
+__device__ __forceinline__ typename Run<TYPE, kRowRun>::V moved_up(typename Run<TYPE, kRowRun>::V v, int behind)
+{
+#pragma unroll
+    for (int b = kRowRun / 2; b > 0; b /= 2)
+        if (behind & b) {
+#pragma unroll
+            for (int k = 0; k < kRowRun; ++k) v[k] = k + b < kRowRun ? v[k + b < kRowRun ? k + b : 0] : (typename Element<TYPE>::T)0;
+        }
+    return v;
+}
+
 template <int TYPE, bool ONCE = true>
 __device__ __forceinline__ void store_part(void* p, f8 x, int n)
 {
