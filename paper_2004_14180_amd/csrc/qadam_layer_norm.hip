@@ -74,8 +74,6 @@ struct Lane {
     __device__ __forceinline__ Lane(int d) : lane(threadIdx.x % LANES), dim(d) {}
     __device__ __forceinline__ int at(int k) const { return (k * LANES + lane) * kRowRun; }
     __device__ __forceinline__ int left(int k) const { return dim - at(k); }
-    // how far in front of its place the row's last run is loaded, so that it is a whole one
-    __device__ __forceinline__ int behind(int k) const { return left(k) < kRowRun && dim >= kRowRun ? kRowRun - left(k) : 0; }
     // of a workgroup's rows the one that this lane has a part of
     __device__ __forceinline__ int row() const
     {
@@ -92,18 +90,8 @@ __device__ __forceinline__ void load_row(const Lane<LANES, RUNS>& l, const void*
 #pragma unroll
     for (int k = 0; k < RUNS; ++k) {
         out[k] = 0;
-        if (l.left(k) <= 0) continue;
-        if (l.dim >= kRowRun) out[k] = load_raw<TYPE, kRowRun, false>(p + l.at(k) - l.behind(k));
-        else out[k] = load_part<TYPE, false>(p, l.dim);
+        if (l.left(k) > 0) out[k] = load_ahead<TYPE>(p, l.at(k), l.dim);
     }
-}
-
-// ... and what it holds once it is there
-template <int LANES, int RUNS, int TYPE>
-__device__ __forceinline__ f8 loaded(const Lane<LANES, RUNS>& l, int k, typename Run<TYPE, kRowRun>::V raw)
-{
-    if (l.left(k) > 0 && l.behind(k) > 0) raw = moved_up<TYPE>(raw, l.behind(k));
-    return to_float<TYPE, kRowRun>(raw);
 }
 
 template <int LANES, int RUNS>
@@ -137,7 +125,7 @@ __global__ void __launch_bounds__(group_threads(LANES)) k_layer_norm(NormForward
         float sum = 0.0f, squares = 0.0f;
 #pragma unroll
         for (int k = 0; k < RUNS; ++k) {
-            x[k] = loaded<LANES, RUNS, XT>(l, k, raw[k]);
+            x[k] = loaded<XT>(raw[k], l.at(k), l.dim);
 #pragma unroll
             for (int i = 0; i < kRowRun; ++i) sum += x[k][i];
         }
@@ -231,8 +219,8 @@ __global__ void __launch_bounds__(group_threads(LANES)) k_layer_norm_grad(NormBa
         const float r = rstd;
 #pragma unroll
         for (int k = 0; k < RUNS; ++k) {
-            const f8 dy = loaded<LANES, RUNS, DT>(l, k, raw_dy[k]);
-            xh[k] = (loaded<LANES, RUNS, XT>(l, k, raw_x[k]) - mean) * r;
+            const f8 dy = loaded<DT>(raw_dy[k], l.at(k), l.dim);
+            xh[k] = (loaded<XT>(raw_x[k], l.at(k), l.dim) - mean) * r;
             // no dout behind the row's end: nothing there enters a sum
             db[k] += dy;
             dw[k] = fused(dy, xh[k], dw[k]);

@@ -86,46 +86,37 @@ __device__ __forceinline__ void store_codes(int8_t* p, uint64_t v, int n)
 
 // A workgroup per token, and its next one under way; up to HELD * 2048 inputs stay in registers between the maximum and the integers, beyond
 // that the row is read again.  Integers up to `padded` are written, zeros from `inputs` on.
-template <int HELD>
+template <int XT, int HELD>
 __global__ void __launch_bounds__(kThreads) k_tokens(TokensLaunch L)
 {
     __shared__ uint32_t most[2][kThreads / 64];
     constexpr int kAcross = kThreads * kRowRun;
     const int first = threadIdx.x * kRowRun;
-    f8 next[HELD];
+    const auto* x = static_cast<const typename Element<XT>::T*>(L.x);
+    typename Run<XT, kRowRun>::V next[HELD];
     auto load = [&](int64_t t) {
 #pragma unroll
         for (int k = 0; k < HELD; ++k) {
-            next[k] = 0.0f;
+            next[k] = 0;
             const int at = first + k * kAcross;
-            if (at < L.inputs) next[k] = load_part(L.x, L.x_type, t * L.x_stride + at, L.inputs - at);
+            if (at < L.inputs) next[k] = load_ahead<XT>(x + t * L.x_stride, at, L.inputs);
         }
     };
-    if (L.x_type != QADAM_CODES8) load(blockIdx.x);
+    load(blockIdx.x);
     int turn = 0;
     for (int64_t t = blockIdx.x; t < L.tokens; t += gridDim.x, turn ^= 1) {
         int8_t* to = L.codes + t * L.codes_stride;
-        if (L.x_type == QADAM_CODES8) {
-            const int8_t* from = static_cast<const int8_t*>(L.x) + t * L.x_stride;
-            for (int at = first; at < L.padded; at += kAcross) {
-                uint64_t v = 0;
-                if (L.inputs - at >= kRowRun) v = __builtin_bit_cast(uint64_t, load_raw<QADAM_CODES8, kRowRun>(from + at));
-                else
-                    for (int i = 0; i < L.inputs - at; ++i) v |= (uint64_t)(uint8_t)global(from)[at + i] << 8 * i;
-                store_codes(to + at, v, L.padded - at);
-            }
-            continue;
-        }
-        f8 x[HELD];
+        const auto* from = x + t * L.x_stride;
+        f8 held[HELD];
         uint32_t m = 0;
 #pragma unroll
         for (int k = 0; k < HELD; ++k) {
-            x[k] = next[k];
-            m = larger(m, largest_of(x[k]));
+            held[k] = loaded<XT>(next[k], first + k * kAcross, L.inputs);
+            m = larger(m, largest_of(held[k]));
         }
         if (t + gridDim.x < L.tokens) load(t + gridDim.x);
         for (int at = first + HELD * kAcross; at < L.inputs; at += kAcross)
-            m = larger(m, largest_of(load_part(L.x, L.x_type, t * L.x_stride + at, L.inputs - at)));
+            m = larger(m, largest_of(loaded<XT>(load_ahead<XT>(from, at, L.inputs), at, L.inputs)));
         m = wave_largest(m);
         if (threadIdx.x % 64 == 0) most[turn][threadIdx.x / 64] = m;
         __syncthreads();
@@ -134,15 +125,37 @@ __global__ void __launch_bounds__(kThreads) k_tokens(TokensLaunch L)
 #pragma unroll
         for (int k = 0; k < HELD; ++k) {
             const int at = first + k * kAcross;
-            if (at < L.padded) store_codes(to + at, codes_of(s, x[k]), L.padded - at);
+            if (at < L.padded) store_codes(to + at, codes_of(s, held[k]), L.padded - at);
         }
         for (int at = first + HELD * kAcross; at < L.padded; at += kAcross) {
             f8 y = 0.0f;
-            if (at < L.inputs) y = load_part(L.x, L.x_type, t * L.x_stride + at, L.inputs - at);
+            if (at < L.inputs) y = loaded<XT>(load_ahead<XT>(from, at, L.inputs), at, L.inputs);
             store_codes(to + at, codes_of(s, y), L.padded - at);
         }
         if (threadIdx.x == 0) global(L.scales)[t] = s.scale;
     }
+}
+
+// Tokens that are integers already, in rows of `padded`
+__global__ void __launch_bounds__(kThreads) k_token_codes(TokensLaunch L)
+{
+    for (int64_t t = blockIdx.x; t < L.tokens; t += gridDim.x) {
+        const int8_t* from = static_cast<const int8_t*>(L.x) + t * L.x_stride;
+        for (int at = threadIdx.x * kRowRun; at < L.padded; at += kThreads * kRowRun) {
+            uint64_t v = 0;
+            if (L.inputs - at >= kRowRun) v = __builtin_bit_cast(uint64_t, load_raw<QADAM_CODES8, kRowRun>(from + at));
+            else
+                for (int i = 0; i < L.inputs - at; ++i) v |= (uint64_t)(uint8_t)global(from)[at + i] << 8 * i;
+            store_codes(L.codes + t * L.codes_stride + at, v, L.padded - at);
+        }
+    }
+}
+
+template <int XT>
+void launch_tokens_of(const TokensLaunch& L, dim3 grid)
+{
+    if (L.inputs <= 2048) k_tokens<XT, 1><<<grid, dim3(kThreads), 0, L.stream>>>(L);
+    else k_tokens<XT, 4><<<grid, dim3(kThreads), 0, L.stream>>>(L);
 }
 
 // ---- what both products share ---------------------------------------------------------------------
@@ -583,8 +596,10 @@ hipError_t rows(const ProductLaunch& L, const TokensLaunch& X, int split)
 hipError_t launch_tokens(const TokensLaunch& L)
 {
     const dim3 grid((int)(L.tokens < 8192 ? L.tokens : 8192));
-    if (L.inputs <= 2048) k_tokens<1><<<grid, dim3(kThreads), 0, L.stream>>>(L);
-    else k_tokens<4><<<grid, dim3(kThreads), 0, L.stream>>>(L);
+    if (L.x_type == QADAM_CODES8) k_token_codes<<<grid, dim3(kThreads), 0, L.stream>>>(L);
+    else if (L.x_type == QADAM_F32) launch_tokens_of<QADAM_F32>(L, grid);
+    else if (L.x_type == QADAM_BF16) launch_tokens_of<QADAM_BF16>(L, grid);
+    else launch_tokens_of<QADAM_F16>(L, grid);
     return hipGetLastError();
 }
 

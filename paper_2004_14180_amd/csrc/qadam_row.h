@@ -21,18 +21,29 @@ __device__ __forceinline__ typename Run<TYPE, kRowRun>::V load_part(const void* 
     return v;
 }
 
-// Of a run that lies `behind` elements behind its place, where a row ended, the elements from there on; zeros behind them.  Loads of whole
-// runs are not waited for until they are used, which those of single elements under conditions are.
+// The run at `at` < dim of a row of `dim` elements, not yet put in its place: where the row ends within it, its last kRowRun elements, in one
+// load that nothing waits for before the run is used, as a wave does for loads of single elements under conditions.
 template <int TYPE>
-__device__ __forceinline__ typename Run<TYPE, kRowRun>::V moved_up(typename Run<TYPE, kRowRun>::V v, int behind)
+__device__ __forceinline__ typename Run<TYPE, kRowRun>::V load_ahead(const typename Element<TYPE>::T* row, int at, int dim)
 {
+    if (dim < kRowRun) return load_part<TYPE, false>(row, dim);
+    return load_raw<TYPE, kRowRun, false>(row + (at + kRowRun <= dim ? at : dim - kRowRun));
+}
+
+// ... and its elements in their place, zeros behind them
+template <int TYPE>
+__device__ __forceinline__ f8 loaded(typename Run<TYPE, kRowRun>::V v, int at, int dim)
+{
+    if (at < dim && at + kRowRun > dim && dim >= kRowRun) {
+        const int by = at + kRowRun - dim;
 #pragma unroll
-    for (int b = kRowRun / 2; b > 0; b /= 2)
-        if (behind & b) {
+        for (int b = kRowRun / 2; b > 0; b /= 2)
+            if (by & b) {
 #pragma unroll
-            for (int k = 0; k < kRowRun; ++k) v[k] = k + b < kRowRun ? v[k + b < kRowRun ? k + b : 0] : (typename Element<TYPE>::T)0;
-        }
-    return v;
+                for (int k = 0; k < kRowRun; ++k) v[k] = k + b < kRowRun ? v[k + b < kRowRun ? k + b : 0] : (typename Element<TYPE>::T)0;
+            }
+    }
+    return to_float<TYPE, kRowRun>(v);
 }
 
 template <int TYPE, bool ONCE = true>
