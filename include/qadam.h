@@ -479,7 +479,8 @@ int qadam_layer_norm_grad(qadam_layer_norm_t h, int64_t rows, const void* dout, 
  *     a = max |x_j|;  q_j = round(x_j (127 (1 / a))), ties to even;  s = a (1/127)
  * (a < 2^-116: q = 0, s = 0; a not finite: q = 0, s = NaN).  The sum over j of q_j w_nj is exact, in 32-bit integers; then, in fp32,
  *     out[t][n] = ((float) sum * s_t) * r_n + bias_n,    r_n = weight_scales[n], or 2^-(k_x+1) for weight codes.
- * max_tokens (up to 2^24, and max_tokens * inputs up to 2^36) bounds num_tokens of one call; the handle's scratch holds their integers. */
+ * max_tokens (up to 2^24, and max_tokens * inputs up to 2^36) bounds num_tokens of one call; the handle's scratch holds their integers, and 4 MiB of
+ * sums where few outputs have many inputs. */
 typedef struct qadam_linear8_ctx* qadam_linear8_t;
 
 int qadam_linear8_init(qadam_linear8_t* out, int64_t outputs, int32_t inputs, int64_t max_tokens);

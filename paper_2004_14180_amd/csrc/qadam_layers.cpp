@@ -44,6 +44,8 @@ struct qadam_linear8_ctx {
     int64_t outputs, max_tokens;
     DeviceArray<int8_t> codes;
     DeviceArray<float> scales;
+    DeviceArray<int32_t> sums;          // of workgroups that share a tile's inputs, and how many of them have left theirs
+    DeviceArray<uint32_t> arrived;
 };
 
 struct qadam_sampler_ctx {
@@ -139,6 +141,10 @@ int qadam_linear8_init(qadam_linear8_t* out, int64_t outputs, int32_t inputs, in
         QADAM_HIP(hipGetDevice(&h->device));
         QADAM_CHECK(allocate(h->codes, (size_t)max_tokens * (size_t)linear8_padded(inputs)));
         QADAM_CHECK(allocate(h->scales, (size_t)max_tokens));
+        if (linear8_may_share(outputs, inputs, max_tokens)) {
+            QADAM_CHECK(allocate(h->sums, (size_t)kPartTiles * kPartSum));
+            QADAM_CHECK(allocate(h->arrived, kPartTiles));
+        }
         *out = h.release();
         return QADAM_OK;
     });
@@ -189,10 +195,11 @@ int qadam_linear8_forward(qadam_linear8_t h, int64_t num_tokens, const void* x, 
     const hipStream_t s = static_cast<hipStream_t>(stream);
     // integers that lie as the kernels want them are taken where they are
     const bool there = x_type == QADAM_CODES8 && K == padded && x_stride % 16 == 0 && x_stride <= 1 << 22 && reinterpret_cast<uintptr_t>(x) % 16 == 0;
-    const TokensLaunch X{num_tokens, x, x_stride, there ? nullptr : h->codes.get(), padded, h->scales.get(), K, padded, x_type, s};
+    const TokensLaunch X{num_tokens, x, x_stride, there ? nullptr : h->codes.get(), padded, h->scales.get(), K, padded, x_type, s,
+                         h->arrived.get()};
     QADAM_HIP(launch_product({num_tokens, h->outputs, there ? static_cast<const int8_t*>(x) : h->codes.get(), there ? x_stride : padded,
                               x_scales ? x_scales : h->scales.get(), weight, weight_stride, weight_scales, bias, out, out_stride,
-                              weight_scales ? 1.0f : std::ldexp(1.0f, -(k_x + 1)), K, bias_type, out_type, s}, X));
+                              weight_scales ? 1.0f : std::ldexp(1.0f, -(k_x + 1)), K, bias_type, out_type, s, there ? nullptr : h->sums.get()}, X));
     return QADAM_OK;
 }
 

@@ -51,6 +51,7 @@ struct TokensLaunch {
     float*  scales;         // not written for a copy
     int32_t inputs, padded, x_type;
     hipStream_t stream;
+    uint32_t* arrived = nullptr;        // kPartTiles counters that become zeros, or null
 };
 hipError_t launch_tokens(const TokensLaunch& L);
 
@@ -68,6 +69,7 @@ struct ProductLaunch {
     float   code_scale;     // where there are no weight_scales
     int32_t inputs, bias_type, out_type;
     hipStream_t stream;
+    int32_t* sums;          // kPartTiles * kPartSum, of workgroups that share a tile; null: none do
 };
 // X: how the tokens become L.codes, its own `codes` null where they need not.
 hipError_t launch_product(const ProductLaunch& L, const TokensLaunch& X);

@@ -2,7 +2,7 @@
 //
 // Sums of products of 8-bit integers are exact in 32 bits in whatever order they are taken, so that the work may be split over wavefronts
 // in any way and the result stays the same bits.  Two ways, by sizes alone (Linear8Plan):
-//   * few tokens: bound by reading the weights.  They go from memory straight into the matrix instructions' registers, once, by as many
+//   * few tokens (16 at most): bound by reading the weights.  They go from memory straight into the matrix instructions' registers, once, by as many
 //     wavefronts as keep enough loads under way (k_product_rows);
 //   * many tokens: bound by the matrix instructions and by what feeds them.  Tiles of both operands pass through LDS (k_product_tiles).
 #include <type_traits>
@@ -84,6 +84,12 @@ __device__ __forceinline__ void store_codes(int8_t* p, uint64_t v, int n)
         if (i < n) global(p)[i] = (int8_t)(v >> 8 * i);
 }
 
+__device__ __forceinline__ void clear_arrived(const TokensLaunch& L)
+{
+    static_assert(kPartTiles == kThreads, "a counter per thread");
+    if (L.arrived && blockIdx.x == 0) global(L.arrived)[threadIdx.x] = 0;
+}
+
 // A workgroup per token, and its next one under way; up to HELD * 2048 inputs stay in registers between the maximum and the integers, beyond
 // that the row is read again.  Integers up to `padded` are written, zeros from `inputs` on.
 template <int XT, int HELD>
@@ -103,6 +109,7 @@ __global__ void __launch_bounds__(kThreads) k_tokens(TokensLaunch L)
         }
     };
     load(blockIdx.x);
+    clear_arrived(L);
     int turn = 0;
     for (int64_t t = blockIdx.x; t < L.tokens; t += gridDim.x, turn ^= 1) {
         int8_t* to = L.codes + t * L.codes_stride;
@@ -139,6 +146,7 @@ __global__ void __launch_bounds__(kThreads) k_tokens(TokensLaunch L)
 // Tokens that are integers already, in rows of `padded`
 __global__ void __launch_bounds__(kThreads) k_token_codes(TokensLaunch L)
 {
+    clear_arrived(L);
     for (int64_t t = blockIdx.x; t < L.tokens; t += gridDim.x) {
         const int8_t* from = static_cast<const int8_t*>(L.x) + t * L.x_stride;
         for (int at = threadIdx.x * kRowRun; at < L.padded; at += kThreads * kRowRun) {
@@ -194,9 +202,9 @@ __device__ __forceinline__ void store_some(typename Element<OT>::T* p, typename 
 }
 
 // ---- few tokens -----------------------------------------------------------------------------------
-// A wavefront takes ROWS tiles of 16 rows of the weights and COLS tiles of 16 tokens, and a part of the inputs; `split` of a workgroup's
-// wavefronts share the rows and add their sums in LDS.  A lane's 16 integers of a matrix instruction are 16 bytes of one row, so the
-// weights come from memory into their places, at any address.  AHEAD chunks of 64 inputs are under way at a time.
+// A wavefront takes 16 rows of the weights, all tokens (16 at most) and a part of the inputs; `split` of a workgroup's wavefronts share the
+// rows and add their sums in LDS.  A lane's 16 integers of a matrix instruction are 16 bytes of one row, so the weights come from memory
+// into their places, at any address.  AHEAD chunks of 64 inputs are under way at a time.
 // MADE: the workgroup makes the tokens' integers itself, in LDS, which saves the launch that would, while its first weights are on the way.
 //
 // One token of 768 to 50257 outputs, 38.6 MB of weights: 10.1 us per call, the kernel 9.6, of which 2.5 pass until the first product; the rest
@@ -210,20 +218,17 @@ __device__ __forceinline__ void lds_barrier()
     asm volatile("" ::: "memory");
 }
 
-template <int ROWS, int COLS, int AHEAD, bool MADE>
-__global__ void __launch_bounds__(64 * row_waves(ROWS)) k_product_rows(ProductLaunch L, TokensLaunch X, int split, int64_t first)
+template <int AHEAD, bool MADE>
+__global__ void __launch_bounds__(64 * kRowWaves) k_product_rows(ProductLaunch L, TokensLaunch X, int split)
 {
-    constexpr int kRowWaves = row_waves(ROWS);
     extern __shared__ __attribute__((aligned(16))) int8_t lds[];
-    __shared__ uint32_t most[16];
+    __shared__ uint32_t most[kRowsTokens];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int padded = X.padded;
-    const int64_t per = (L.outputs + 16 * ROWS * (kRowWaves / split) - 1) / (16 * ROWS * (kRowWaves / split));
-    const int64_t group = blockIdx.x % per, t0 = first + blockIdx.x / per * (16 * COLS);
     const int part = wave % split, chunks = (L.inputs + 63) / 64, each = (chunks + split - 1) / split;
     const int begin = part * each, end = begin + each < chunks ? begin + each : chunks;
-    const int64_t n0 = (group * (kRowWaves / split) + wave / split) * (16 * ROWS);
-    const int k0 = lane / 16 * 16;
+    const int64_t n0 = ((int64_t)blockIdx.x * (kRowWaves / split) + wave / split) * 16;
+    const int k0 = lane / 16 * 16, t = lane % 16;
 
     // tokens that become integers here: runs of 8, a few per thread
     constexpr int kHeld = MADE ? kMadeInputs / (64 * kRowWaves * kRowRun) : 1;
@@ -232,119 +237,78 @@ __global__ void __launch_bounds__(64 * row_waves(ROWS)) k_product_rows(ProductLa
     if constexpr (MADE) {
 #pragma unroll
         for (int h = 0; h < kHeld; ++h) {
-            const int q = h * 64 * kRowWaves + threadIdx.x, t = q / runs, at = q % runs * kRowRun;
+            const int q = h * 64 * kRowWaves + threadIdx.x, m = q / runs, at = q % runs * kRowRun;
             held[h] = 0.0f;
-            if (t < (int)L.tokens && at < L.inputs) held[h] = load_part(X.x, X.x_type, t * X.x_stride + at, L.inputs - at);
+            if (m < (int)L.tokens && at < L.inputs) held[h] = load_part(X.x, X.x_type, m * X.x_stride + at, L.inputs - at);
         }
     }
-    const int8_t* row[ROWS];
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        const int64_t n = n0 + i * 16 + lane % 16;
-        row[i] = L.weight + (n < L.outputs ? n : L.outputs - 1) * L.weight_stride;
-    }
-    const int8_t* token[COLS];
-    bool there[COLS];
-#pragma unroll
-    for (int j = 0; j < COLS; ++j) {
-        const int64_t t = t0 + j * 16 + lane % 16;
-        there[j] = t < L.tokens;
-        token[j] = MADE ? lds + (there[j] ? t : 0) * padded : L.codes + (there[j] ? t : 0) * L.codes_stride;
-    }
+    const int8_t* row = L.weight + (n0 + t < L.outputs ? n0 + t : L.outputs - 1) * L.weight_stride;
+    const bool there = t < L.tokens;
+    const int8_t* token = MADE ? lds + (there ? t : 0) * padded : L.codes + (there ? t : 0) * L.codes_stride;
     // chunks under way: chunk c of this wavefront's in place (c - begin) % AHEAD; zeros behind the last one
-    i4 w[ROWS][AHEAD], x[COLS][AHEAD];
-    auto load_rows = [&](int c, int u) {
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) w[i][u] = c < end ? load_weights(row[i], c * 64 + k0, L.inputs) : (i4)0;
-    };
-    auto load_tokens = [&](int c, int u) {
-#pragma unroll
-        for (int j = 0; j < COLS; ++j) {
-            x[j][u] = 0;
-            if (c < end && there[j]) {
-                if constexpr (MADE) x[j][u] = *(const i4*)(token[j] + c * 64 + k0);
-                else x[j][u] = *(const QADAM_GLOBAL i4*)(token[j] + c * 64 + k0);
-            }
+    i4 w[AHEAD], x[AHEAD];
+    auto load_row = [&](int c, int u) { w[u] = c < end ? load_weights(row, c * 64 + k0, L.inputs) : (i4)0; };
+    auto load_token = [&](int c, int u) {
+        x[u] = 0;
+        if (c < end && there) {
+            if constexpr (MADE) x[u] = *(const i4*)(token + c * 64 + k0);
+            else x[u] = *(const QADAM_GLOBAL i4*)(token + c * 64 + k0);
         }
     };
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
-        load_rows(begin + u, u);
-        if constexpr (!MADE) load_tokens(begin + u, u);
+        load_row(begin + u, u);
+        if constexpr (!MADE) load_token(begin + u, u);
     }
     if constexpr (MADE) {
-        if (threadIdx.x < 16) most[threadIdx.x] = 0;
+        if (threadIdx.x < kRowsTokens) most[threadIdx.x] = 0;
         lds_barrier();
 #pragma unroll
         for (int h = 0; h < kHeld; ++h) {
-            const int t = (h * 64 * kRowWaves + (int)threadIdx.x) / runs;
-            if (t < (int)L.tokens) atomicMax(&most[t], largest_of(held[h]));
+            const int m = (h * 64 * kRowWaves + (int)threadIdx.x) / runs;
+            if (m < (int)L.tokens) atomicMax(&most[m], largest_of(held[h]));
         }
         lds_barrier();
 #pragma unroll
         for (int h = 0; h < kHeld; ++h) {
-            const int q = h * 64 * kRowWaves + threadIdx.x, t = q / runs;
-            if (t < (int)L.tokens) *(uint64_t*)(lds + q * kRowRun) = codes_of(TokenScale(most[t]), held[h]);
+            const int q = h * 64 * kRowWaves + threadIdx.x, m = q / runs;
+            if (m < (int)L.tokens) *(uint64_t*)(lds + q * kRowRun) = codes_of(TokenScale(most[m]), held[h]);
         }
         lds_barrier();
     }
-    i4 acc[ROWS][COLS];
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i)
-#pragma unroll
-        for (int j = 0; j < COLS; ++j) acc[i][j] = 0;
+    i4 acc = 0;
 #pragma unroll 1
     for (int c = begin; c < end; c += AHEAD)
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             if (c + u >= end) break;
-            if constexpr (MADE) load_tokens(c + u, u);
-#pragma unroll
-            for (int j = 0; j < COLS; ++j)
-#pragma unroll
-                for (int i = 0; i < ROWS; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i][u], x[j][u], acc[i][j], 0, 0, 0);
-            load_rows(c + AHEAD + u, u);
-            if constexpr (!MADE) load_tokens(c + AHEAD + u, u);
+            if constexpr (MADE) load_token(c + u, u);
+            acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u], x[u], acc, 0, 0, 0);
+            load_row(c + AHEAD + u, u);
+            if constexpr (!MADE) load_token(c + AHEAD + u, u);
         }
     if (split > 1) {
         __syncthreads();
         i4* sums = (i4*)lds;
-        if (part > 0) {
-#pragma unroll
-            for (int i = 0; i < ROWS; ++i)
-#pragma unroll
-                for (int j = 0; j < COLS; ++j) sums[((wave * ROWS + i) * COLS + j) * 64 + lane] = acc[i][j];
-        }
+        if (part > 0) sums[wave * 64 + lane] = acc;
         __syncthreads();
         if (part > 0) return;
-        for (int p = 1; p < split; ++p)
-#pragma unroll
-            for (int i = 0; i < ROWS; ++i)
-#pragma unroll
-                for (int j = 0; j < COLS; ++j) acc[i][j] += sums[(((wave + p) * ROWS + i) * COLS + j) * 64 + lane];
+        for (int p = 1; p < split; ++p) acc += sums[(wave + p) * 64 + lane];
     }
+    const int64_t n = n0 + lane / 16 * 4;
+    if (n >= L.outputs || !there) return;
+    f4 scale, bias;
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        const int64_t n = n0 + i * 16 + lane / 16 * 4;
-        if (n >= L.outputs) continue;
-        f4 scale, bias;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int64_t m = n + e < L.outputs ? n + e : L.outputs - 1;
-            scale[e] = output_scale(L, m);
-            bias[e] = output_bias(L, m);
-        }
-#pragma unroll
-        for (int j = 0; j < COLS; ++j) {
-            const int64_t t = t0 + j * 16 + lane % 16;
-            if (t >= L.tokens) continue;
-            const f4 y = results(L, acc[i][j], MADE ? TokenScale(most[t]).scale : global(L.token_scales)[t], scale, bias);
-            const int64_t at = t * L.out_stride + n;
-            if (L.out_type == QADAM_F32) store_some<QADAM_F32, 4>(static_cast<float*>(L.out) + at, y, L.outputs - n);
-            else if (L.out_type == QADAM_BF16) store_some<QADAM_BF16, 4>(static_cast<__bf16*>(L.out) + at, y, L.outputs - n);
-            else store_some<QADAM_F16, 4>(static_cast<_Float16*>(L.out) + at, y, L.outputs - n);
-        }
+    for (int e = 0; e < 4; ++e) {
+        const int64_t m = n + e < L.outputs ? n + e : L.outputs - 1;
+        scale[e] = output_scale(L, m);
+        bias[e] = output_bias(L, m);
     }
+    const f4 y = results(L, acc, MADE ? TokenScale(most[t]).scale : global(L.token_scales)[t], scale, bias);
+    const int64_t at = t * L.out_stride + n;
+    if (L.out_type == QADAM_F32) store_some<QADAM_F32, 4>(static_cast<float*>(L.out) + at, y, L.outputs - n);
+    else if (L.out_type == QADAM_BF16) store_some<QADAM_BF16, 4>(static_cast<__bf16*>(L.out) + at, y, L.outputs - n);
+    else store_some<QADAM_F16, 4>(static_cast<_Float16*>(L.out) + at, y, L.outputs - n);
 }
 
 // ---- many tokens ----------------------------------------------------------------------------------
@@ -365,6 +329,7 @@ __global__ void __launch_bounds__(64 * row_waves(ROWS)) k_product_rows(ProductLa
 // call with ordinary stores, 291 so.  Taken back: steps of 64 inputs with three to five of them in LDS (306-313, 287), four wavefronts of
 // 128 x 128 (bare 268, 256), columns of 8 and 16 tiles (291, 286), a higher priority of the products (the same).
 // DIRECT: rows of the weights lie at addresses of 16 bytes and are loaded into LDS directly; else they pass through registers.
+// parts: workgroups that share a tile of 64 by 64, each with a part of the steps.
 constexpr int kStep = 128;
 
 template <int BM, int BN, int WM, int WN, int STAGES>
@@ -379,15 +344,18 @@ struct Tiles {
 };
 
 template <int BM, int BN, int WM, int WN, int STAGES, bool DIRECT, int OT>
-__global__ void __launch_bounds__(64 * WM * WN) k_product_tiles(ProductLaunch L, int64_t first, int across, int down)
+__global__ void __launch_bounds__(64 * WM * WN) k_product_tiles(ProductLaunch L, int64_t first, int across, int down, int parts, uint32_t* arrived)
 {
     typedef Tiles<BM, BN, WM, WN, STAGES> S;
     extern __shared__ __attribute__((aligned(16))) int8_t lds[];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    constexpr bool kParts = BM * BN == kPartSum;
+    const int tile = kParts ? blockIdx.x % (across * down) : blockIdx.x, part = kParts ? blockIdx.x / (across * down) : 0;
     int tm, tn;
-    tile_place(blockIdx.x, across, down, &tm, &tn);
+    tile_place(tile, across, down, &tm, &tn);
     const int64_t t0 = first + (int64_t)tm * BM, n0 = (int64_t)tn * BN;
     const int steps = (L.inputs + kStep - 1) / kStep;
+    const int begin = kParts ? steps * part / parts : 0, last = (kParts ? steps * (part + 1) / parts : steps) - begin - 1;
 
     // where this thread's runs of a step come from: rows behind the last one repeat it, inputs behind the last one repeat the row's first
     // ones (the tokens' integers are zeros there)
@@ -476,9 +444,8 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product_tiles(ProductLaunch L,
     };
     static_assert(DIRECT || (S::a_loads == S::b_loads && STAGES == 2), "the second half of the loads are the weights', which are placed before the next step's");
     constexpr int kFirst = kLoads / 2;          // of a step's loads: the ones in front of the block in which the others are issued
-    const int last = steps - 1;
     // steps behind the last one are the last one once more, unused
-    auto step_of = [&](int s) { return s < last ? s : last; };
+    auto step_of = [&](int s) { return begin + (s < last ? s : last); };
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s)
 #pragma unroll
@@ -504,6 +471,30 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product_tiles(ProductLaunch L,
     block(1, true, buffer, 2, false, 0, 0, 0, 0);
     block(0, true, buffer, 3, false, 0, 0, 0, 0);
     block(1, false, 0, 0, false, 0, 0, 0, 0);
+
+    if constexpr (kParts)
+        if (parts > 1) {
+            // The workgroup that comes last adds the others' sums to its own.  Sums are stored and loaded past the caches that each XCD has of
+            // its own (atomic at the scope of the GPU), so that it is enough to wait for the stores before the count: fences in their
+            // place, which write back all of an L2, took 20 us.  Loads of four parts at a time save nothing.
+            typedef uint64_t u8 __attribute__((ext_vector_type(8)));
+            uint64_t* sums = (uint64_t*)L.sums + (int64_t)tile * parts * (kPartSum / 2) + threadIdx.x;
+            const u8 own = __builtin_bit_cast(u8, acc[0][0]);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) __hip_atomic_store(sums + part * (kPartSum / 2) + q * S::threads, own[q], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            meet(std::integral_constant<int, 0>());
+            uint32_t* count = (uint32_t*)lds;
+            if (threadIdx.x == 0) *count = atomicAdd(arrived + tile, 1u);
+            __syncthreads();
+            if (*count != (uint32_t)parts - 1) return;
+            for (int p = 0; p < parts; ++p) {
+                if (p == part) continue;
+                u8 other;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) other[q] = __hip_atomic_load(sums + p * (kPartSum / 2) + q * S::threads, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                acc[0][0] += __builtin_bit_cast(i16, other);
+            }
+        }
 
     // Results through LDS, 32 tokens of a wavefront at a time, so that whole lines are stored: a lane holds 4 outputs of a token, and
     // 8 bytes each in 32 rows cost a quarter of the call.
@@ -553,7 +544,7 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product_tiles(ProductLaunch L,
 }
 
 template <int BM, int BN, int WM, int WN, int STAGES, bool DIRECT>
-hipError_t tiles(const ProductLaunch& L)
+hipError_t tiles(const ProductLaunch& L, int parts = 1, uint32_t* arrived = nullptr)
 {
     typedef Tiles<BM, BN, WM, WN, STAGES> S;
     // a launch takes as many rows of tiles as keep it below 2^22 workgroups
@@ -566,7 +557,7 @@ hipError_t tiles(const ProductLaunch& L)
                 const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::lds);
                 if (e != hipSuccess) return e;
             }
-            kernel<<<dim3(across * down), dim3(S::threads), S::lds, L.stream>>>(L, t, across, down);
+            kernel<<<dim3(across * down * parts), dim3(S::threads), S::lds, L.stream>>>(L, t, across, down, parts, arrived);
             return hipGetLastError();
         };
         const hipError_t e = L.out_type == QADAM_F32    ? run(k_product_tiles<BM, BN, WM, WN, STAGES, DIRECT, QADAM_F32>)
@@ -577,17 +568,13 @@ hipError_t tiles(const ProductLaunch& L)
     return hipSuccess;
 }
 
-template <int ROWS, int COLS, int AHEAD, bool MADE>
+template <int AHEAD, bool MADE>
 hipError_t rows(const ProductLaunch& L, const TokensLaunch& X, int split)
 {
-    constexpr int kRowWaves = row_waves(ROWS);
-    const int64_t across = (L.outputs + 16 * ROWS * (kRowWaves / split) - 1) / (16 * ROWS * (kRowWaves / split)), most = ((int64_t)1 << 22) / across;
-    int lds = split > 1 ? kRowWaves * ROWS * COLS * 64 * 16 : 0;
+    const int of_a_group = 16 * (kRowWaves / split);
+    int lds = split > 1 ? kRowWaves * 64 * 16 : 0;
     if (MADE && lds < (int)L.tokens * X.padded) lds = (int)L.tokens * X.padded;
-    for (int64_t t = 0; t < L.tokens; t += most * 16 * COLS) {
-        const int64_t rest = (L.tokens - t + 16 * COLS - 1) / (16 * COLS);
-        k_product_rows<ROWS, COLS, AHEAD, MADE><<<dim3((int)(across * (rest < most ? rest : most))), dim3(64 * kRowWaves), lds, L.stream>>>(L, X, split, t);
-    }
+    k_product_rows<AHEAD, MADE><<<dim3((int)((L.outputs + of_a_group - 1) / of_a_group)), dim3(64 * kRowWaves), lds, L.stream>>>(L, X, split);
     return hipGetLastError();
 }
 
@@ -605,23 +592,25 @@ hipError_t launch_tokens(const TokensLaunch& L)
 
 hipError_t launch_product(const ProductLaunch& L, const TokensLaunch& X)
 {
-    const Linear8Plan p(L.tokens, L.outputs, L.inputs, X.x_type != QADAM_CODES8);
+    // rows of the weights that can be loaded into LDS directly
+    const bool direct = reinterpret_cast<uintptr_t>(L.weight) % 16 == 0 && L.weight_stride % 16 == 0 && L.inputs % 16 == 0 && L.weight_stride <= 1 << 22;
+    const Linear8Plan p(L.tokens, L.outputs, L.inputs, X.x_type != QADAM_CODES8, direct);
     if (!p.made) {
         if (X.codes) {
             const hipError_t e = launch_tokens(X);
             if (e != hipSuccess) return e;
         }
     } else {
-        return rows<1, 1, 4, true>(L, X, p.split);
+        return rows<4, true>(L, X, p.split);
     }
-    const bool direct = reinterpret_cast<uintptr_t>(L.weight) % 16 == 0 && L.weight_stride % 16 == 0 && L.inputs % 16 == 0 && L.weight_stride <= 1 << 22;
+    const int parts = L.sums ? p.parts : 1;
     switch (p.kind) {
-    case Linear8Plan::kRows16: return rows<1, 1, 4, false>(L, X, p.split);
-    case Linear8Plan::kRows32: return rows<2, 2, 4, false>(L, X, p.split);
+    case Linear8Plan::kRows: return rows<4, false>(L, X, p.split);
     case Linear8Plan::kTiles64Deep:
-        if (direct) return tiles<64, 64, 2, 2, 3, true>(L);
+        if (direct) return tiles<64, 64, 2, 2, 3, true>(L, parts, X.arrived);
         [[fallthrough]];
-    case Linear8Plan::kTiles64: return direct ? tiles<64, 64, 2, 2, 2, true>(L) : tiles<64, 64, 2, 2, 2, false>(L);
+    case Linear8Plan::kTiles64:
+        return direct ? tiles<64, 64, 2, 2, 2, true>(L, parts, X.arrived) : tiles<64, 64, 2, 2, 2, false>(L, parts, X.arrived);
     case Linear8Plan::kTiles256:
         if (direct) return tiles<256, 256, 4, 2, 2, true>(L);
         [[fallthrough]];

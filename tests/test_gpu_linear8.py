@@ -81,6 +81,36 @@ def test_many_tiles(tokens, inputs, outputs, gap, offset):
     _check(tokens, inputs, outputs, BF16, F32, scales=False, gap=gap, offset=offset)
 
 
+# inputs of a token that several workgroups take: 2 to 16 parts of them, of equal and of different lengths, weights at any address
+@pytest.mark.parametrize("tokens,outputs", [(17, 1), (32, 64), (33, 300), (64, 2048), (65, 1000), (130, 1027), (500, 700)])
+@pytest.mark.parametrize("inputs,gap,offset", [(1024, 0, 1), (1023, 0, 0), (4096, 0, 0), (4224, 16, 0), (8192, 0, 0), (8191, 2, 7), (33_000, 8, 0)])
+def test_inputs_shared_by_workgroups(tokens, outputs, inputs, gap, offset):
+    _check(tokens, inputs, outputs, BF16, F32, bias=F16, gap=gap, offset=offset, out_gap=2)
+
+
+def test_inputs_shared_in_turn():
+    """Calls of one handle in which tiles have many, few and no parts, one behind the other without a wait."""
+    gen = _gen(11)
+    inputs, outputs, most = 8192, 200, 300
+    x, w = torch.randn(most, inputs, generator=gen, device="cuda"), _weights(gen, outputs, inputs)
+    unaligned = torch.empty(outputs * inputs + 1, dtype=torch.int8, device="cuda")[1:].view(outputs, inputs).copy_(w)
+    codes, s = token_codes(x)
+    want = linear8(codes, s, w, 2.0 ** -7, None, F32).cuda()
+    q, same = Linear8(outputs, inputs, most), Linear8(outputs, inputs, most)
+    codes, s = codes.cuda(), s.cuda()
+    outs = []
+    for repeat in range(20):
+        for n in (300, 17, 64, 1, 129, 65):
+            out, second, third = (torch.full((n, outputs), 9.0, device="cuda") for _ in range(3))
+            q.forward(x[:n], w, out, k_x=6)
+            same.forward(x[:n], unaligned, second, k_x=6)
+            q.forward(codes[:n], w, third, k_x=6, x_scales=s[:n])
+            outs.append((n, out, second, third))
+    for n, *got in outs:
+        for out in got:
+            assert torch.equal(out, want[:n]), n
+
+
 def test_the_largest_sums():
     """Sums of -128 * -128 over the most inputs: just below 2^31."""
     inputs = (1 << 17) - 1
@@ -148,7 +178,7 @@ def test_layouts_and_no_tokens():
     q.forward(torch.zeros(0, 40, device="cuda"), w, torch.zeros(0, 24, device="cuda"), k_x=6)
 
 
-@pytest.mark.parametrize("tokens,inputs,outputs", [(1, 768, 3000), (20, 768, 3000), (40, 768, 3000), (300, 768, 3000), (2500, 128, 3000), (5000, 128, 5120)])
+@pytest.mark.parametrize("tokens,inputs,outputs", [(1, 768, 3000), (20, 768, 3000), (40, 768, 3000), (300, 768, 3000), (40, 8192, 192), (20, 2047, 500), (2500, 128, 3000), (5000, 128, 5120)])
 def test_recorded_calls(tokens, inputs, outputs):
     gen = _gen(5)
     x, w = torch.randn(tokens, inputs, generator=gen, device="cuda"), _weights(gen, outputs, inputs)

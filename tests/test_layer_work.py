@@ -39,11 +39,16 @@ def test_the_products_plan(tmp_path):
             for (int inputs = 1; inputs < 1 << 17; inputs = inputs * 3 / 2 + 1) {
                 const Linear8Plan p(tokens, outputs, inputs, true), q(tokens, outputs, inputs, false);
                 CHECK(!q.made && p.kind == q.kind, "kind");
-                CHECK(!p.made || (p.kind == Linear8Plan::kRows16 && tokens * linear8_padded(inputs) <= kMadeInputs), "%lld %d", tokens, inputs);
-                CHECK(tokens > 16 || p.kind == Linear8Plan::kRows16, "few tokens");
-                CHECK(tokens <= 32 || p.kind >= Linear8Plan::kTiles64Deep, "many tokens");
-                const int waves = row_waves(p.kind == Linear8Plan::kRows16 ? 1 : 2);
-                CHECK(p.split >= 1 && p.split <= waves && waves % p.split == 0, "split %d", p.split);
+                CHECK(!p.made || tokens * linear8_padded(inputs) <= kMadeInputs, "%lld %d", tokens, inputs);
+                CHECK((tokens <= kRowsTokens) == (p.kind == Linear8Plan::kRows), "few tokens");
+                CHECK(p.split >= 1 && p.split <= kRowWaves && kRowWaves % p.split == 0, "split %d", p.split);
+                for (bool direct : {false, true}) {
+                    const Linear8Plan s(tokens, outputs, inputs, true, direct);
+                    const long long tiles = (tokens + 63) / 64 * ((outputs + 63) / 64);
+                    CHECK(s.kind == p.kind && s.parts >= 1 && s.parts <= (inputs + 127) / 128, "parts %d", s.parts);
+                    CHECK(s.parts == 1 || (tiles * s.parts <= kPartTiles && (s.kind == Linear8Plan::kTiles64Deep || s.kind == Linear8Plan::kTiles64)), "parts %d", s.parts);
+                    CHECK(s.parts == 1 || linear8_may_share(outputs, inputs, tokens), "scratch");
+                }
             }
     CHECK(linear8_padded(1) == 128 && linear8_padded(128) == 128 && linear8_padded(129) == 256 && linear8_padded((1 << 17) - 1) == 1 << 17, "padded");""")
 
