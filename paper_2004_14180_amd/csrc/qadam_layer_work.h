@@ -30,7 +30,7 @@ constexpr int kRowWaves = 4;            // of a workgroup of that kernel
 // them are in LDS, 0.5 where weights pass through registers.  Adding the parts' sums takes 2 to 3 us, hence steps that a part has at least.
 // us per call, one part / parts: 64 tokens of 8192 to 2048 22.5 / 14.4, of 4096 to 1024 14.3 / 12.6 (parts of 8 steps 15.2 and 12.0), of 65536 to
 // 64 148 / 41 (8 parts at most 45.7); of 2048 to 8192 10.6 / 11.2, not taken.  Through registers: 64 tokens of 2047 to 2048 17.7 / 13.2 (parts of
-// 8 steps 14.4), of 1023 12.9 / 12.1.
+// 8 steps 14.4), of 1023 12.9 / 12.1, all before two steps of weights were under way; since then 10.9 and 9.4.
 constexpr int kPartTiles = 256;         // workgroups that may have a part
 constexpr int kPartSum = 64 * 64;       // sums of a tile
 constexpr int kMostParts = 16;
@@ -40,9 +40,10 @@ constexpr int part_steps(bool direct) { return direct ? 16 : 4; }
 // said): rows / tiles of 64: 9 tokens 9.1 / 9.9, 16 tokens 9.7 / 10.4, of 1023 to 2048 9.4 / 12.5; beyond 16, with rows in pairs of tiles, 17 tokens
 // 10.3 / 10.2, 32 tokens 10.9 / 10.2, of 768 to 50257 18.9 / 13.6, of 768 to 2304 10.2 / 8.4.  Tiles of 64 / 128: 384 tokens 15.2 / 18.1, 512 tokens
 // 17.1 / 18.4, 768 tokens 25.8 / 20.6; 1024 tokens of 768 to 2304 10.5 / 12.4, 2048 16.5 / 15.4.  Up to two tiles of 64 on a CU wait for their
-// loads: steps of two / three of them in LDS: 64 tokens 14.0 / 11.2, 256 tokens 14.6 / 13.8, 512 tokens (four on a CU) 18.5 / 21.5.  Tiles of 256
-// run one to a CU and take 1.7 times what two tiles of 128 do: 128 / 256: 1024 tokens 23.4 / 28.7, 2048 tokens 43.5 / 38.4, 4096 83.7 / 72.7,
-// 16384 337 / 280; 8192 tokens of 768 to 2304 36.4 / 40.1.
+// loads: steps of two / three of them in LDS: 64 tokens 14.0 / 11.2, 256 tokens 14.6 / 13.8, 512 tokens (four on a CU) 18.5 / 21.5; through
+// registers, of 2047 to 2048, 512 tokens (one on a CU) 16.3 / 14.8, 1024 18.6 / 20.0.  Tiles of 256 run one to a CU and take 1.7 times what two
+// tiles of 128 do: 128 / 256: 1024 tokens 23.4 / 28.7, 2048 tokens 43.5 / 38.4, 4096 83.7 / 72.7, 16384 337 / 280; 8192 tokens of 768 to
+// 2304 36.4 / 40.1.
 struct Linear8Plan {
     enum Kind { kRows, kTiles64Deep, kTiles64, kTiles128, kTiles256 } kind;
     bool made;              // the product's workgroups make the tokens' integers
@@ -59,7 +60,7 @@ struct Linear8Plan {
             while (split < kRowWaves && waves * split < 2048 && inputs > 256 * split) split *= 2;
         } else if (tiles128 <= 256) {
             const int64_t tiles64 = (tokens + 63) / 64 * ((outputs + 63) / 64);
-            kind = tiles64 <= 512 ? kTiles64Deep : kTiles64;
+            kind = tiles64 <= (direct ? 512 : 256) ? kTiles64Deep : kTiles64;
             while (parts < kMostParts && tiles64 * parts * 2 <= kPartTiles && linear8_padded(inputs) / 128 >= parts * 2 * part_steps(direct)) parts *= 2;
         } else if ((tiles256 + 255) / 256 * 17 < (tiles128 + 511) / 512 * 10) {
             kind = kTiles256;

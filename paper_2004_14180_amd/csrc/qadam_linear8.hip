@@ -201,6 +201,29 @@ __device__ __forceinline__ void store_some(typename Element<OT>::T* p, typename 
         if (i < n) global(p)[i] = (typename Element<OT>::T)y[i];
 }
 
+// ... where a row has 16 of them: the 16 that end with the row's last one, loaded without a condition, if those from k on would pass it, which
+// `in_place` moves to where they belong.  What it leaves behind the last one is any of the row's: tokens have zeros there.
+__device__ __forceinline__ i4 load_window(const int8_t* row, int k, int inputs)
+{
+    return *(const QADAM_GLOBAL i4u*)(row + (k < inputs - 16 ? k : inputs - 16));
+}
+
+__device__ __forceinline__ i4 in_place(i4 v, int k, int inputs)
+{
+    const int by = k + 16 - inputs;
+    if (inputs < 16 || by <= 0 || by >= 16) return v;       // shorter rows are not loaded like this
+#pragma unroll
+    for (int q = 2; q > 0; q /= 2)
+        if (by & 4 * q) {
+#pragma unroll
+            for (int e = 0; e + q < 4; ++e) v[e] = v[e + q];
+        }
+    i4 w = v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = (int)__builtin_amdgcn_alignbyte((uint32_t)v[e < 3 ? e + 1 : 3], (uint32_t)v[e], (uint32_t)(by & 3));
+    return w;
+}
+
 // ---- few tokens -----------------------------------------------------------------------------------
 // A wavefront takes 16 rows of the weights, all tokens (16 at most) and a part of the inputs; `split` of a workgroup's wavefronts share the
 // rows and add their sums in LDS.  A lane's 16 integers of a matrix instruction are 16 bytes of one row, so the weights come from memory
@@ -328,7 +351,8 @@ __global__ void __launch_bounds__(64 * kRowWaves) k_product_rows(ProductLaunch L
 // alone, without loads and LDS, take 177.  Results (268 MB) are stored past the caches, since they would push the operands out: 333 us per
 // call with ordinary stores, 291 so.  Taken back: steps of 64 inputs with three to five of them in LDS (306-313, 287), four wavefronts of
 // 128 x 128 (bare 268, 256), columns of 8 and 16 tiles (291, 286), a higher priority of the products (the same).
-// DIRECT: rows of the weights lie at addresses of 16 bytes and are loaded into LDS directly; else they pass through registers.
+// DIRECT: rows of the weights lie at addresses of 16 bytes and are loaded into LDS directly; else they pass through registers, STAGES - 1 steps
+// of them on the way, all by loads of 16 bytes without a condition: 64 tokens of 2047 to 2048 10.9 us, 13.2 with conditions and a step less.
 // parts: workgroups that share a tile of 64 by 64, each with a part of the steps.
 constexpr int kStep = 128;
 
@@ -377,9 +401,9 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product_tiles(ProductLaunch L,
         if constexpr (DIRECT) b_at[i] = (uint32_t)(row < b_rows ? row : b_rows - 1) * (uint32_t)L.weight_stride;
         else b_row[i] = b_base + (int64_t)(row < b_rows ? row : b_rows - 1) * L.weight_stride;
     }
-    i4 b_held[DIRECT ? 1 : S::b_loads];
+    i4 b_held[DIRECT ? 1 : STAGES - 1][DIRECT ? 1 : S::b_loads];        // of step s in s % (STAGES - 1)
     constexpr int kLoads = S::a_loads + S::b_loads;
-    auto load = [&](int step, int buffer, int i) {
+    auto load = [&](int step, int buffer, int i, auto set) {
         int8_t* to = lds + buffer * S::stage;
         if (i < S::a_loads) {
             __builtin_amdgcn_global_load_lds((const QADAM_GLOBAL void*)(a_base + (a_at[i] + (uint32_t)(step * kStep))),
@@ -390,14 +414,17 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product_tiles(ProductLaunch L,
                                              (__attribute__((address_space(3))) void*)(to + S::a_bytes + (b * S::threads + wave * 64) * 16), 16, 0, 0);
         } else {
             const int b = i - S::a_loads;
-            b_held[b] = load_weights(b_row[b], step * kStep + b_run[b], L.inputs);
+            const int k = step * kStep + b_run[b];
+            b_held[set.value][b] = L.inputs >= 16 ? load_window(b_row[b], k, L.inputs) : load_weights(b_row[b], k, L.inputs);
         }
     };
     // what was loaded into registers goes to LDS
-    auto place = [&](int buffer) {
+    auto place = [&](int step, int buffer, auto set) {
         if constexpr (!DIRECT) {
 #pragma unroll
-            for (int b = 0; b < S::b_loads; ++b) *(i4*)(lds + buffer * S::stage + S::a_bytes + (b * S::threads + threadIdx.x) * 16) = b_held[b];
+            for (int b = 0; b < S::b_loads; ++b)
+                *(i4*)(lds + buffer * S::stage + S::a_bytes + (b * S::threads + threadIdx.x) * 16) =
+                    in_place(b_held[set.value][b], step * kStep + b_run[b], L.inputs);
         }
     };
     // This wavefront's loads into LDS have arrived but for the last `under_way`, and all wavefronts are here: the instructions that load
@@ -424,7 +451,7 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product_tiles(ProductLaunch L,
         else b[into][i - S::mt] = *(const i4*)(from + S::a_bytes + (c0 + (i - S::mt) * 32 + row) * kStep);
     };
     // the products of the operands in a[from], b[from]; between them the reads of the next block's and the loads [begin, begin + count)
-    auto block = [&](int from, bool reads, int buffer, int next, bool loads, int step, int into, int begin, int count) {
+    auto block = [&](int from, bool reads, int buffer, int next, bool loads, int step, int into, int begin, int count, auto set) {
 #pragma unroll
         for (int m = 0; m < kProducts; ++m) {
             const int i = m / S::nt, j = m % S::nt;
@@ -437,40 +464,54 @@ __global__ void __launch_bounds__(64 * WM * WN) k_product_tiles(ProductLaunch L,
             if (loads) {
 #pragma unroll
                 for (int q = 0; q < kLoads; ++q)
-                    if (q < count && q * kProducts / count == m) load(step, into, begin + q);
+                    if (q < count && q * kProducts / count == m) load(step, into, begin + q, set);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    static_assert(DIRECT || (S::a_loads == S::b_loads && STAGES == 2), "the second half of the loads are the weights', which are placed before the next step's");
+    static_assert(DIRECT || S::a_loads == S::b_loads, "the second half of the loads are the weights', which are placed before others take their registers");
     constexpr int kFirst = kLoads / 2;          // of a step's loads: the ones in front of the block in which the others are issued
     // steps behind the last one are the last one once more, unused
     auto step_of = [&](int s) { return begin + (s < last ? s : last); };
+    constexpr int kSets = DIRECT ? 1 : STAGES - 1;
+    constexpr std::integral_constant<int, 0> kSet0;
+    constexpr std::integral_constant<int, kSets - 1> kSet1;
+    static_assert(kSets <= 2, "sets of registers are named");
 #pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s)
+    for (int s = 0; s < STAGES - 1; ++s) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) load(step_of(s), s, i);
-    place(0);
+        for (int i = 0; i < kLoads; ++i) {
+            if (s % kSets == 0) load(step_of(s), s, i, kSet0);
+            else load(step_of(s), s, i, kSet1);
+        }
+        __builtin_amdgcn_sched_barrier(0);      // `meet` counts them in this order
+    }
+    place(step_of(0), 0, kSet0);
     meet(kAhead);
 #pragma unroll
-    for (int i = 0; i < kFirst; ++i) load(step_of(STAGES - 1), STAGES - 1, i);
+    for (int i = 0; i < kFirst; ++i) load(step_of(STAGES - 1), STAGES - 1, i, kSet0);
 #pragma unroll
     for (int q = 0; q < kOperands; ++q) read(0, 0, 0, q);
     int buffer = 0;                             // of step s
-    for (int s = 0; s < last; ++s) {
+    // own: the set of registers that step s had and step s + STAGES - 1 gets; other: that of step s + 1
+    auto multiply = [&](int s, auto own, auto other) {
         const int next = buffer + 1 < STAGES ? buffer + 1 : 0, before = buffer > 0 ? buffer - 1 : STAGES - 1;
-        block(0, true, buffer, 1, true, step_of(s + STAGES - 1), before, kFirst, kLoads - kFirst);
-        block(1, true, buffer, 2, false, 0, 0, 0, 0);
-        block(0, true, buffer, 3, false, 0, 0, 0, 0);
-        place(next);
+        block(0, true, buffer, 1, true, step_of(s + STAGES - 1), before, kFirst, kLoads - kFirst, own);
+        block(1, true, buffer, 2, false, 0, 0, 0, 0, own);
+        block(0, true, buffer, 3, false, 0, 0, 0, 0, own);
+        place(step_of(s + 1), next, other);
         meet(kAhead);
-        block(1, true, next, 0, true, step_of(s + STAGES), buffer, 0, kFirst);
+        block(1, true, next, 0, true, step_of(s + STAGES), buffer, 0, kFirst, own);
         buffer = next;
+    };
+    for (int s = 0; s < last; s += kSets) {
+        multiply(s, kSet0, kSet1);
+        if (kSets > 1 && s + 1 < last) multiply(s + 1, kSet1, kSet0);
     }
-    block(0, true, buffer, 1, false, 0, 0, 0, 0);
-    block(1, true, buffer, 2, false, 0, 0, 0, 0);
-    block(0, true, buffer, 3, false, 0, 0, 0, 0);
-    block(1, false, 0, 0, false, 0, 0, 0, 0);
+    block(0, true, buffer, 1, false, 0, 0, 0, 0, kSet0);
+    block(1, true, buffer, 2, false, 0, 0, 0, 0, kSet0);
+    block(0, true, buffer, 3, false, 0, 0, 0, 0, kSet0);
+    block(1, false, 0, 0, false, 0, 0, 0, 0, kSet0);
 
     if constexpr (kParts)
         if (parts > 1) {
@@ -607,10 +648,8 @@ hipError_t launch_product(const ProductLaunch& L, const TokensLaunch& X)
     switch (p.kind) {
     case Linear8Plan::kRows: return rows<4, false>(L, X, p.split);
     case Linear8Plan::kTiles64Deep:
-        if (direct) return tiles<64, 64, 2, 2, 3, true>(L, parts, X.arrived);
-        [[fallthrough]];
-    case Linear8Plan::kTiles64:
-        return direct ? tiles<64, 64, 2, 2, 2, true>(L, parts, X.arrived) : tiles<64, 64, 2, 2, 2, false>(L, parts, X.arrived);
+        return direct ? tiles<64, 64, 2, 2, 3, true>(L, parts, X.arrived) : tiles<64, 64, 2, 2, 3, false>(L, parts, X.arrived);
+    case Linear8Plan::kTiles64: return direct ? tiles<64, 64, 2, 2, 2, true>(L) : tiles<64, 64, 2, 2, 2, false>(L);
     case Linear8Plan::kTiles256:
         if (direct) return tiles<256, 256, 4, 2, 2, true>(L);
         [[fallthrough]];
