@@ -229,6 +229,8 @@ __device__ __forceinline__ i4 in_place(i4 v, int k, int inputs)
 // rows and add their sums in LDS.  A lane's 16 integers of a matrix instruction are 16 bytes of one row, so the weights come from memory
 // into their places, at any address.  AHEAD chunks of 64 inputs are under way at a time.
 // MADE: the workgroup makes the tokens' integers itself, in LDS, which saves the launch that would, while its first weights are on the way.
+// RAGGED: rows of 16 and more that are no multiple: one token of 1023 to 2048 6.3 us with loads under conditions, now 4.9; other widths are
+// faster with them (2048 to 8192 5.6, without 6.4).
 //
 // One token of 768 to 50257 outputs, 38.6 MB of weights: 10.1 us per call, the kernel 9.6, of which 2.5 pass until the first product; the rest
 // is 5.4 TB/s.  AHEAD 2, 6, 8, 12: 9.6, 10.2, 10.1, 11.4; with a launch for the integers in front 12.  Four wavefronts in a workgroup, where
@@ -241,7 +243,7 @@ __device__ __forceinline__ void lds_barrier()
     asm volatile("" ::: "memory");
 }
 
-template <int AHEAD, bool MADE>
+template <int AHEAD, bool MADE, bool RAGGED>
 __global__ void __launch_bounds__(64 * kRowWaves) k_product_rows(ProductLaunch L, TokensLaunch X, int split)
 {
     extern __shared__ __attribute__((aligned(16))) int8_t lds[];
@@ -270,7 +272,10 @@ __global__ void __launch_bounds__(64 * kRowWaves) k_product_rows(ProductLaunch L
     const int8_t* token = MADE ? lds + (there ? t : 0) * padded : L.codes + (there ? t : 0) * L.codes_stride;
     // chunks under way: chunk c of this wavefront's in place (c - begin) % AHEAD; zeros behind the last one
     i4 w[AHEAD], x[AHEAD];
-    auto load_row = [&](int c, int u) { w[u] = c < end ? load_weights(row, c * 64 + k0, L.inputs) : (i4)0; };
+    auto load_row = [&](int c, int u) {
+        if constexpr (!RAGGED) w[u] = c < end ? load_weights(row, c * 64 + k0, L.inputs) : (i4)0;
+        else w[u] = c < end ? load_window(row, c * 64 + k0, L.inputs) : (i4)0;
+    };
     auto load_token = [&](int c, int u) {
         x[u] = 0;
         if (c < end && there) {
@@ -306,6 +311,7 @@ __global__ void __launch_bounds__(64 * kRowWaves) k_product_rows(ProductLaunch L
         for (int u = 0; u < AHEAD; ++u) {
             if (c + u >= end) break;
             if constexpr (MADE) load_token(c + u, u);
+            if constexpr (RAGGED) w[u] = in_place(w[u], (c + u) * 64 + k0, L.inputs);
             acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u], x[u], acc, 0, 0, 0);
             load_row(c + AHEAD + u, u);
             if constexpr (!MADE) load_token(c + AHEAD + u, u);
@@ -612,10 +618,13 @@ hipError_t tiles(const ProductLaunch& L, int parts = 1, uint32_t* arrived = null
 template <int AHEAD, bool MADE>
 hipError_t rows(const ProductLaunch& L, const TokensLaunch& X, int split)
 {
+    const bool ragged = L.inputs >= 16 && L.inputs % 16 != 0;
     const int of_a_group = 16 * (kRowWaves / split);
     int lds = split > 1 ? kRowWaves * 64 * 16 : 0;
     if (MADE && lds < (int)L.tokens * X.padded) lds = (int)L.tokens * X.padded;
-    k_product_rows<AHEAD, MADE><<<dim3((int)((L.outputs + of_a_group - 1) / of_a_group)), dim3(64 * kRowWaves), lds, L.stream>>>(L, X, split);
+    const dim3 grid((int)((L.outputs + of_a_group - 1) / of_a_group)), threads(64 * kRowWaves);
+    if (ragged) k_product_rows<AHEAD, MADE, true><<<grid, threads, lds, L.stream>>>(L, X, split);
+    else k_product_rows<AHEAD, MADE, false><<<grid, threads, lds, L.stream>>>(L, X, split);
     return hipGetLastError();
 }
 
