@@ -2,7 +2,9 @@
 //
 // Both are bound by memory: a row is read once and stays in registers over its sums, the next one is on the way meanwhile, and results
 // stream past the caches.  16384 rows of 2048 bf16: forward 24 us (134 MB, 5.6 TB/s), backward 36 (201 MB, 5.6 TB/s) and 5 for the sums over
-// rows; 8191 rows of 1001 f16 at odd addresses 14.7 and 3.8; 1024 rows of 768 fp32 4.9 and 4.3, which are two chains of loads.
+// rows; 8191 rows of 1001 f16 at odd addresses 14.4 and 3.9; 1024 rows of 768 fp32 5.0 and 4.3, which are two chains of loads.
+// Where a row ends within a lane's run, its last 8 elements are loaded as a whole run: backward of 8191 rows of 2047 bf16 27.8 us per call (of 2048
+// 23.2), with loads of single elements 58.
 // The variance is taken of differences from the mean, in a second pass over registers: sums of squares would cancel where rows lie far from 0.
 #include <type_traits>
 

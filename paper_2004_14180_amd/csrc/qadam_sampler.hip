@@ -11,10 +11,11 @@
 //     bin's tokens;
 //   * tokens of a bin that are more than kList (2048, that is many equal logits): by digits of the logits, a pass for each.
 //
-// Bound by the instructions of one CU per row.  One row of 50257 fp32, top_k 50: 14.4 us, of which the largest logit takes 2.6, the
-// threads' bins 2.5, the list 5.4 and its sums 2.  top_p alone, fp32: 34.5; of bf16's 92 thousand cycles the masses take 38 (31 operations per
-// token, most of them in fp64) and the two lists 12 to 21 each; 256 such rows 44.  33 rows of 32003 fp16 28.5;
-// by digits throughout they took 300.  kBins of 4096 and 8192: 256 rows of 50257 41.7 and 45.1, 1000 rows of 5000 57.0, 59.7 and 74.0.
+// Bound by the instructions of one CU per row.  One row of 50257 fp32, top_k 50: 12.7 us, of which the list takes about 5, the threads' bins
+// and sums 2 each.  256 rows of 50257 bf16 with filters of their own 50: of top_p's 92 thousand cycles the masses take 38 (31 operations per token,
+// most of them in fp64) and the two lists 12 to 21 each.  33 rows of 32003 fp16 24.7; by digits throughout they took 300.  A run is looked at, and
+// what another thread has of it masked, in its turn: masked as it is loaded, which waits for it, 14.6, 56.8 and 28.6; two runs under way
+// 13.7, 51.7 and 25.3.  kBins of 4096 and 8192, at that time: 256 rows of 50257 41.7 and 45.1, 1000 rows of 5000 57.0, 59.7 and 74.0.
 #include "qadam_layers.h"
 #include "qadam_row.h"
 
