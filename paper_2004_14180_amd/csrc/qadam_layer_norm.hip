@@ -69,6 +69,14 @@ __device__ __forceinline__ f8 fused(f8 a, f8 b, f8 c)
     return y;
 }
 
+// the first n elements, zeros behind them
+__device__ __forceinline__ f8 first_of(f8 x, int n)
+{
+#pragma unroll
+    for (int i = 0; i < kRowRun; ++i) x[i] = i < n ? x[i] : 0.0f;
+    return x;
+}
+
 // What a lane holds of a row: RUNS runs of kRowRun elements, LANES lanes apart.
 template <int LANES, int RUNS>
 struct Lane {
@@ -84,7 +92,7 @@ struct Lane {
     }
 };
 
-template <int LANES, int RUNS, int TYPE>
+template <int LANES, int RUNS, int TYPE, bool REPEAT = false>
 __device__ __forceinline__ void load_row(const Lane<LANES, RUNS>& l, const void* base, int64_t offset,
                                          typename Run<TYPE, kRowRun>::V (&out)[RUNS])
 {
@@ -92,7 +100,7 @@ __device__ __forceinline__ void load_row(const Lane<LANES, RUNS>& l, const void*
 #pragma unroll
     for (int k = 0; k < RUNS; ++k) {
         out[k] = 0;
-        if (l.left(k) > 0) out[k] = load_ahead<TYPE>(p, l.at(k), l.dim);
+        if (REPEAT || l.left(k) > 0) out[k] = load_ahead<TYPE, REPEAT>(p, l.at(k), l.dim);
     }
 }
 
@@ -136,10 +144,7 @@ __global__ void __launch_bounds__(group_threads(LANES)) k_layer_norm(NormForward
 #pragma unroll
         for (int k = 0; k < RUNS; ++k) {
             x[k] -= mean;
-            if (l.left(k) < kRowRun) {
-#pragma unroll
-                for (int i = 0; i < kRowRun; ++i) x[k][i] = i < l.left(k) ? x[k][i] : 0.0f;
-            }
+            if (l.left(k) < kRowRun) x[k] = first_of(x[k], l.left(k));
 #pragma unroll
             for (int i = 0; i < kRowRun; ++i) squares = __builtin_fmaf(x[k][i], x[k][i], squares);
         }
@@ -205,7 +210,7 @@ __global__ void __launch_bounds__(group_threads(LANES)) k_layer_norm_grad(NormBa
     float mean = 0.0f, rstd = 0.0f;
     auto load = [&](int64_t r) {
         load_row<LANES, RUNS, DT>(l, L.dout, r * L.dout_stride, raw_dy);
-        load_row<LANES, RUNS, XT>(l, L.x, r * L.x_stride, raw_x);
+        load_row<LANES, RUNS, XT, true>(l, L.x, r * L.x_stride, raw_x);
         mean = global(L.mean)[r];
         rstd = global(L.rstd)[r];
     };
@@ -222,8 +227,9 @@ __global__ void __launch_bounds__(group_threads(LANES)) k_layer_norm_grad(NormBa
 #pragma unroll
         for (int k = 0; k < RUNS; ++k) {
             const f8 dy = loaded<DT>(raw_dy[k], l.at(k), l.dim);
-            xh[k] = (loaded<XT>(raw_x[k], l.at(k), l.dim) - mean) * r;
-            // no dout behind the row's end: nothing there enters a sum
+            // Behind the row's end dout is 0, so that nothing there enters a sum while xh is finite, which (0 - mean) rstd need not be: x repeats
+            // elements of the row there.
+            xh[k] = (loaded<XT, true>(raw_x[k], l.at(k), l.dim) - mean) * r;
             db[k] += dy;
             dw[k] = fused(dy, xh[k], dw[k]);
             g[k] = dy * w[k];
@@ -296,7 +302,7 @@ __global__ void __launch_bounds__(64 * kLongWaves) k_layer_norm_grad_long(NormBa
             const int n = L.dim - at;
             g = load_part(L.dout, L.dout_type, row * L.dout_stride + at, n);
             if (L.weight) g *= load_part(L.weight, L.weight_type, at, n);
-            xh = (load_part(L.x, L.x_type, row * L.x_stride + at, n) - mean) * rstd;
+            xh = first_of((load_part(L.x, L.x_type, row * L.x_stride + at, n) - mean) * rstd, n);
         };
         float sum = 0.0f, along = 0.0f;
         f8 g, xh;

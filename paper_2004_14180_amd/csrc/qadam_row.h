@@ -22,25 +22,34 @@ __device__ __forceinline__ typename Run<TYPE, kRowRun>::V load_part(const void* 
 }
 
 // The run at `at` < dim of a row of `dim` elements, not yet put in its place: where the row ends within it, its last kRowRun elements, in one
-// load that nothing waits for before the run is used, as a wave does for loads of single elements under conditions.
-template <int TYPE>
+// load that nothing waits for before the run is used, as a wave does for loads of single elements under conditions.  REPEAT: `at` may be
+// behind the row, and what `loaded` gives behind the row's end are elements of the row, where there are zeros else.
+template <int TYPE, bool REPEAT = false>
 __device__ __forceinline__ typename Run<TYPE, kRowRun>::V load_ahead(const typename Element<TYPE>::T* row, int at, int dim)
 {
-    if (dim < kRowRun) return load_part<TYPE, false>(row, dim);
+    if (dim < kRowRun) {
+        typename Run<TYPE, kRowRun>::V v = load_part<TYPE, false>(row, dim);
+        if constexpr (REPEAT) {
+#pragma unroll
+            for (int k = 1; k < kRowRun; ++k) v[k] = k < dim ? v[k] : v[0];
+        }
+        return v;
+    }
     return load_raw<TYPE, kRowRun, false>(row + (at + kRowRun <= dim ? at : dim - kRowRun));
 }
 
-// ... and its elements in their place, zeros behind them
-template <int TYPE>
+// ... and its elements in their place
+template <int TYPE, bool REPEAT = false>
 __device__ __forceinline__ f8 loaded(typename Run<TYPE, kRowRun>::V v, int at, int dim)
 {
+    typedef typename Element<TYPE>::T T;
     if (at < dim && at + kRowRun > dim && dim >= kRowRun) {
         const int by = at + kRowRun - dim;
 #pragma unroll
         for (int b = kRowRun / 2; b > 0; b /= 2)
             if (by & b) {
 #pragma unroll
-                for (int k = 0; k < kRowRun; ++k) v[k] = k + b < kRowRun ? v[k + b < kRowRun ? k + b : 0] : (typename Element<TYPE>::T)0;
+                for (int k = 0; k < kRowRun; ++k) v[k] = k + b < kRowRun ? v[k + b < kRowRun ? k + b : 0] : REPEAT ? v[k] : (T)0;
             }
     }
     return to_float<TYPE, kRowRun>(v);

@@ -150,6 +150,20 @@ def test_values_at_the_ends_of_the_range():
     assert out[1:3].isfinite().all()
 
 
+@pytest.mark.parametrize("dim", [3, 8, 96, 100, 128, 300, 520, 1001, 1030, 2048, 2049, 4100, 8191, 8192, 8193, 8200, 9001])
+@pytest.mark.parametrize("xt", [F32, BF16])
+def test_gradient_of_rows_far_from_zero(dim, xt):
+    """(x - mean) rstd is 0 in every element of such a row, while mean rstd is beyond fp32: nothing behind the row's end enters its sums."""
+    gen = _gen(dim)
+    x = torch.randn(5, dim, generator=gen, device="cuda").to(xt)
+    dout, w = torch.randn(5, dim, generator=gen, device="cuda"), torch.randn(dim, generator=gen, device="cuda")
+    mean, rstd = x.float().mean(1), torch.full((5,), 1.5, device="cuda")
+    for row, value in ((1, 2.0 ** 120), (3, -2.0 ** 127)):
+        x[row], mean[row], rstd[row] = value, value, 1e-5 ** -0.5
+    _check_grad(dout, x, w, mean, rstd, F32, F32)
+    _check_grad(dout, x, None, mean, rstd, F32, F32)
+
+
 def test_no_rows():
     dim = 50
     e, w = torch.zeros(0, dim, device="cuda"), torch.ones(dim, device="cuda")
