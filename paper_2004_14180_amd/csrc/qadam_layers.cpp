@@ -179,7 +179,8 @@ int qadam_linear8_forward(qadam_linear8_t h, int64_t num_tokens, const void* x, 
     QADAM_CHECK(check_count(num_tokens));
     if (num_tokens > h->max_tokens) return fail(QADAM_ERANGE, "num_tokens > max_tokens of the handle");
     if (x_type != QADAM_CODES8 && !float_type(x_type)) return fail(QADAM_EINVAL, "x_type");
-    if ((x_type == QADAM_CODES8) != (x_scales != nullptr)) return fail(QADAM_EINVAL, "x_scales belong to x in QADAM_CODES8");
+    // an empty array of scales may have no address
+    if (x_type == QADAM_CODES8 ? num_tokens > 0 && !x_scales : x_scales != nullptr) return fail(QADAM_EINVAL, "x_scales belong to x in QADAM_CODES8");
     if (!weight_scales && (k_x < 0 || k_x > 6)) return fail(QADAM_EINVAL, "k_x outside 0..6, and no weight_scales");
     if (bias && !float_type(bias_type)) return fail(QADAM_EINVAL, "bias_type");
     if (!float_type(out_type)) return fail(QADAM_EINVAL, "out_type");

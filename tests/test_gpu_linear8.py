@@ -4,7 +4,7 @@ import torch
 
 from layer_util import linear8, token_codes
 from operator_util import BF16, F16, F32
-from paper_2004_14180_amd import Linear8, QAdamError
+from paper_2004_14180_amd import Linear8, QAdamError, binding
 
 pytestmark = pytest.mark.gpu
 
@@ -176,6 +176,29 @@ def test_layouts_and_no_tokens():
     q.forward(x[0, 0, :1].expand(7, 40), w, out.view(30, 24)[:7], k_x=6)
     assert torch.equal(out.view(30, 24)[:7], want[:1].expand(7, 24))
     q.forward(torch.zeros(0, 40, device="cuda"), w, torch.zeros(0, 24, device="cuda"), k_x=6)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_no_tokens_in_integers(native, monkeypatch):
+    """An empty batch in integers is as good as one in floats; scales beside floats are refused there too."""
+    q, w = Linear8(24, 40, 30), _weights(_gen(6), 24, 40)
+    if not native:
+        monkeypatch.setattr(binding, "_native", binding._Unavailable())
+    x, codes, scales = torch.zeros(0, 40, device="cuda"), torch.zeros(0, 40, dtype=torch.int8, device="cuda"), torch.zeros(0, device="cuda")
+    out = torch.zeros(0, 24, device="cuda")
+    q.quantize(x, codes, scales)
+    q.forward(codes, w, out, k_x=6, x_scales=scales)
+    q.forward(codes, w, out, weight_scales=torch.ones(24, device="cuda"), x_scales=scales, bias=torch.ones(24, device="cuda"))
+    for kw in (dict(x=x, x_scales=scales), dict(x=codes), dict(x=x, x_scales=torch.ones(1, device="cuda"))):
+        with pytest.raises(ValueError):
+            q.forward(weight=w, out=out, k_x=6, **kw)
+    # at the boundary: no tokens in integers need no scales, one does, and floats never take any
+    one, y = torch.zeros(1, 40, device="cuda"), torch.zeros(1, 24, device="cuda")
+    call = lambda n, kind, at: q._lib.qadam_linear8_forward(q._h, n, one.data_ptr(), kind, 40, at, w.data_ptr(), 40, None, 6, None, 0,  # noqa: E731
+                                                            y.data_ptr(), binding.QADAM_F32, 24, None)
+    assert call(0, binding.QADAM_CODES8, None) == 0 and call(0, binding.QADAM_CODES8, one.data_ptr()) == 0
+    assert call(1, binding.QADAM_CODES8, None) == -1
+    assert call(0, binding.QADAM_F32, one.data_ptr()) == -1 and call(1, binding.QADAM_F32, one.data_ptr()) == -1
 
 
 @pytest.mark.parametrize("tokens,inputs,outputs", [(1, 768, 3000), (20, 768, 3000), (40, 768, 3000), (300, 768, 3000), (40, 8192, 192), (20, 2047, 500), (2500, 128, 3000), (5000, 128, 5120)])
