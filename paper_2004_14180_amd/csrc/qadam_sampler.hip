@@ -638,8 +638,9 @@ __global__ void __launch_bounds__(kThreads) k_sample(SampleLaunch L, int64_t fir
     } else if (!none) {
         const double log2e = 0x1.71547652b82fep+0;
         r.mass = {all_high, log2e / f.temperature};
-        // bins down to where masses vanish, 29 temperatures below the largest, or to the smallest logit; any scale is right
-        const float range = fminf(fminf(29.0f * (float)f.temperature, all_high - all_low), kMost);
+        // bins down to where masses vanish, 29 temperatures below the largest, or to the smallest logit; any scale is right.  At most 2^126, so that
+        // kBins times the width of one, rounded, is finite.
+        const float range = fminf(fminf(29.0f * (float)f.temperature, all_high - all_low), 0x1p126f);
         const float scale = (float)(kBins - 1) / range;
         r.bin = {all_high, scale < 1e30f ? scale : 1e30f};
         const bool by_k = f.top_k > 0 && f.top_k <= kMostTopK, by_min_p = !by_k && f.top_k == 0 && !(f.top_p < 1.0) && f.min_p > 0.0;

@@ -91,6 +91,25 @@ def test_random_numbers_at_the_ends():
         _check(x, u, **kw)
 
 
+@pytest.mark.parametrize("temperature", [1e37, 1.17e37, 1.2e37, 1e38, 3.4028234e38])
+@pytest.mark.parametrize("vocab", [5, 300, 2047, 3000])
+def test_temperatures_at_the_end_of_the_range(temperature, vocab):
+    """Logits as far apart as fp32 has them, all of which have masses at such temperatures."""
+    x, _ = _logits(8, vocab, F32)
+    x[0, 3] = math.inf
+    x[1, 2] = 3.4e38
+    x[2, ::2], x[2, 1::2] = 3e38, -3e38
+    x[3] = torch.linspace(-3.4e38, 3.4e38, vocab, dtype=torch.float64).float()
+    x[4, 0], x[4, 1] = math.inf, -math.inf
+    x[5, 1:] = torch.finfo(F32).min
+    x[6, 4] = -3.4e38
+    for u in (0.0, 0.4, 0.8, 0.97, 1.0 - 2.0 ** -24):
+        us = torch.full((8,), u, device="cuda")
+        for kw in (dict(), dict(top_k=2), dict(top_k=vocab - 1), dict(top_p=0.9), dict(min_p=0.02), dict(min_p=0.9), dict(top_k=900, top_p=0.99, min_p=0.001)):
+            _check(x, us, temperature=temperature, **kw)
+            _check(x, us, temperature=torch.full((8,), temperature, device="cuda"), **kw)
+
+
 def test_masks_and_rows_without_a_token():
     x, u = _logits(12, 2000, F32)
     x[0] = -math.inf                                        # nothing left
