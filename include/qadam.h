@@ -491,7 +491,8 @@ int qadam_linear8_destroy(qadam_linear8_t h);
 int qadam_linear8_quantize(qadam_linear8_t h, int64_t num_tokens, const void* x, int32_t x_type, int64_t x_stride, int8_t* codes,
                            int64_t codes_stride, float* scales, void* stream);
 
-/*   x               tokens in a float type, with x_scales NULL; or QADAM_CODES8 with their scales, any integers in int8
+/*   x               tokens in a float type, with x_scales NULL; or QADAM_CODES8 with their scales (NULL too where there are no tokens), any
+ *                   integers in int8
  *   weight          int8, weight_stride >= inputs, at any address: any integers in int8
  *   weight_scales   fp32 of each output, or NULL with the codes' k_x (0..6)
  *   bias            outputs elements of bias_type, or NULL
@@ -502,7 +503,8 @@ int qadam_linear8_forward(qadam_linear8_t h, int64_t num_tokens, const void* x, 
 
 /* Sampling of one token per row of `vocab` (1 to 2^22) logits from given random numbers.  Tokens are taken in descending order of their logits,
  * the lower index first among equals, and every filter keeps the first ones of that order:
- *     mass_i = round(2^40 exp((logit_i - largest) / temperature)) in fp64, an integer, so that sums are exact;
+ *     mass_i = round(2^40 exp((logit_i - largest) / temperature)) in fp64, an integer, so that sums of masses are exact (the exponential is
+ *              within 1/64 of a unit: a mass that lies so near to a half may be rounded the other way);
  *     top_k > 0      the first top_k;
  *     top_p < 1      of those the fewest, but one at least, whose masses' sum reaches top_p of all of theirs;
  *     min_p > 0      of those the ones whose mass reaches min_p 2^40;

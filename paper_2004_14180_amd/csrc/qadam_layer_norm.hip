@@ -2,7 +2,8 @@
 //
 // Both are bound by memory: a row is read once and stays in registers over its sums, the next one is on the way meanwhile, and results
 // stream past the caches.  16384 rows of 2048 bf16: forward 24 us (134 MB, 5.6 TB/s), backward 36 (201 MB, 5.6 TB/s) and 5 for the sums over
-// rows; 8191 rows of 1001 f16 at odd addresses 14.4 and 3.9; 1024 rows of 768 fp32 5.0 and 4.3, which are two chains of loads.
+// rows; of 8192 fp32, per call, 246 us (4.4 TB/s) and 346 (4.7), bf16 109 and 157; 8191 rows of 1001 f16 at odd addresses 14.4 and 3.9; 1024 rows
+// of 768 fp32 5.0 and 4.3, which are two chains of loads.
 // Where a row ends within a lane's run, its last 8 elements are loaded as a whole run: backward of 8191 rows of 2047 bf16 27.8 us per call (of 2048
 // 23.2), with loads of single elements 58.
 // The variance is taken of differences from the mean, in a second pass over registers: sums of squares would cancel where rows lie far from 0.
@@ -159,7 +160,9 @@ __global__ void __launch_bounds__(group_threads(LANES)) k_layer_norm(NormForward
     }
 }
 
-// Rows that are too long for registers: a workgroup reads each three times, from the caches after the first.
+// Rows that are too long for registers: a workgroup reads each three times, from the caches after the first; the gradient's kernels do so
+// together.  us per call, forward and gradient: 16384 rows of 9001 fp32 455 and 897 (2.6 and 2.0 TB/s of what has to
+// move), bf16 432 and 942; 2048 rows of 65536 fp32 320 and 687, bf16 170 and 577; 64 rows of 2^20 fp32 449 and 1162.
 constexpr int kLongWaves = 16;
 
 __global__ void __launch_bounds__(64 * kLongWaves) k_layer_norm_long(NormForward L)
@@ -365,7 +368,9 @@ int groups_of(int64_t rows, int each, int most)
 }
 
 // Lanes and runs per row, by its width.  us per call with rows in the registers of a wavefront / of as many as here: 16384 rows of 2048
-// bf16 forward 25.7 / 25.8, backward 66 / 42.9; with a wavefront / 16 lanes: 40000 rows of 64 bf16 12.2 / 4.9 and 18.9 / 8.6.
+// bf16 forward 25.7 / 25.8, backward 66 / 42.9; with a wavefront / 16 lanes: 40000 rows of 64 bf16 12.2 / 4.9 and 18.9 / 8.6.  Beyond 4096 columns
+// a workgroup of 16 wavefronts has a CU to itself (the gradient's 102 and more registers), and nothing runs while it waits for a row's sums:
+// 16384 rows of 8192 fp32 reach 4.4 and 4.7 TB/s where rows of 4096 reach 5.0; more runs on fewer lanes were not measured.
 template <typename F>
 void by_width(int dim, F&& body)
 {

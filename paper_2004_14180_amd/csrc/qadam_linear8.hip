@@ -229,8 +229,8 @@ __device__ __forceinline__ i4 in_place(i4 v, int k, int inputs)
 // rows and add their sums in LDS.  A lane's 16 integers of a matrix instruction are 16 bytes of one row, so the weights come from memory
 // into their places, at any address.  AHEAD chunks of 64 inputs are under way at a time.
 // MADE: the workgroup makes the tokens' integers itself, in LDS, which saves the launch that would, while its first weights are on the way.
-// RAGGED: rows of 16 and more that are no multiple: one token of 1023 to 2048 6.3 us with loads under conditions, now 4.9; other widths are
-// faster with them (2048 to 8192 5.6, without 6.4).
+// RAGGED: rows of 16 and more that are no multiple: one token of 1023 to 2048 6.3 us per call with loads under conditions, 5.4 without, of 2047
+// 8.1 and 6.8; other widths take the same either way (2048 to 8192 5.5).
 //
 // One token of 768 to 50257 outputs, 38.6 MB of weights: 10.1 us per call, the kernel 9.6, of which 2.5 pass until the first product; the rest
 // is 5.4 TB/s.  AHEAD 2, 6, 8, 12: 9.6, 10.2, 10.1, 11.4; with a launch for the integers in front 12.  Four wavefronts in a workgroup, where
@@ -352,11 +352,11 @@ __global__ void __launch_bounds__(64 * kRowWaves) k_product_rows(ProductLaunch L
 // and products alternate with waits (the bare product of the sizes below, plain stores: 312 us, so 300).  The step changes in front of its
 // last block, whose operands are in registers by then.
 //
-// 16384 tokens of 2048 to 8192 outputs: about 256 of the call's 280 us, 2.1 POPS, which the card's power sets: the matrix units are busy 56 %
-// of the time at 1.74 GHz, and the bare product without results takes 268 us of usual integers and 217 of zeros; its matrix instructions
-// alone, without loads and LDS, take 177.  Results (268 MB) are stored past the caches, since they would push the operands out: 333 us per
+// 16384 tokens of 2048 to 8192 outputs: 260 us of a call's 280 to 285, 2.1 POPS; the tokens' integers take 18 (the calls of each alone, in a loop).
+// The card's power sets it: the matrix units are busy 56 % of the time at 1.74 GHz, and the same product takes 199 us where all integers are
+// zero; its matrix instructions alone, without loads and LDS, take 177.  Results (268 MB) are stored past the caches, since they would push the operands out: 333 us per
 // call with ordinary stores, 291 so.  Taken back: steps of 64 inputs with three to five of them in LDS (306-313, 287), four wavefronts of
-// 128 x 128 (bare 268, 256), columns of 8 and 16 tiles (291, 286), a higher priority of the products (the same).
+// 128 x 128 (without results 268, 256), columns of 8 and 16 tiles (291, 286), a higher priority of the products (the same).
 // DIRECT: rows of the weights lie at addresses of 16 bytes and are loaded into LDS directly; else they pass through registers, STAGES - 1 steps
 // of them on the way, all by loads of 16 bytes without a condition: 64 tokens of 2047 to 2048 10.9 us, 13.2 with conditions and a step less.
 // parts: workgroups that share a tile of 64 by 64, each with a part of the steps.

@@ -9,13 +9,20 @@
 //     more than top_k) are listed, and no mass of another token is taken.  The same where min_p is the only filter: it names the bin;
 //   * else the masses of all tokens are added by bins, and each of the sums that are asked for takes one more pass, which lists a
 //     bin's tokens;
-//   * tokens of a bin that are more than kList (2048, that is many equal logits): by digits of the logits, a pass for each.
+//   * where the bin of a sum holds more than kList (2048) tokens: by digits of the logits, four passes with atomics for each sum.
+// The last of these is slow, and not for many equal logits alone.  One row of 50257 fp32 of deviation 2, top_k 50 and top_p 0.95, takes 12.6 us
+// at a temperature of 0.3, but 417 at 0.1, 468 at 0.3 with one token 14 above the others, and 840 where all but 40 tokens have the lowest
+// finite fp32 (minus infinity: 13): fewer than top_k threads hold a logit within 29 temperatures of the largest, so that the last bin, whose tokens
+// have no mass, is listed, found too long and searched by digits.  (Elementary torch operations take 290.)  One row of 128256 of deviation 0.3, top_p
+// 0.9, takes 362 us with one temperature up to 1 for all rows, which leaves the bins 29 temperatures wide in all, and 65 with a temperature of its
+// own, for which the smallest logit is looked for too.
 //
 // Bound by the instructions of one CU per row.  One row of 50257 fp32, top_k 50: 12.7 us, of which the list takes about 5, the threads' bins
-// and sums 2 each.  256 rows of 50257 bf16 with filters of their own 50: of top_p's 92 thousand cycles the masses take 38 (31 operations per token,
+// and sums 2 each.  256 rows of 50257 bf16 with filters of their own 49: of top_p's 92 thousand cycles the masses take 38 (31 operations per token,
 // most of them in fp64) and the two lists 12 to 21 each.  33 rows of 32003 fp16 24.7; by digits throughout they took 300.  A run is looked at, and
 // what another thread has of it masked, in its turn: masked as it is loaded, which waits for it, 14.6, 56.8 and 28.6; two runs under way
-// 13.7, 51.7 and 25.3.  kBins of 4096 and 8192, at that time: 256 rows of 50257 41.7 and 45.1, 1000 rows of 5000 57.0, 59.7 and 74.0.
+// 13.7, 51.7 and 25.3.  kBins of 2048, 4096 and 8192, bf16, top_p 0.9: 256 rows of 50257 37.8, 36.1 and 39.7 (behind top_k 2000 43.0, 44.4 and 49.0),
+// 1000 rows of 5000 52.4, 56.5 and 70.8; 256 flat rows of 128256 501, 126 and 136.
 #include "qadam_layers.h"
 #include "qadam_row.h"
 
@@ -46,7 +53,7 @@ constexpr float kInf = __builtin_inff();
 constexpr float kMost = 0x1.fffffep+127f;       // infinite logits count as this
 
 // round(2^40 exp((x - largest) / temperature)): 2^y = 2^n 2^r with n = round(y) and r from -1/2 to 1/2, where the polynomial of degree 9 that
-// meets 2^r at the ten Chebyshev nodes is within 2^-45 of it: a fortieth of a unit.  Beside 1.5 2^52 the last place of a number is 1, so
+// meets 2^r at the ten Chebyshev nodes is within 2^-46 of it: 1/67 of a unit.  Beside 1.5 2^52 the last place of a number is 1, so
 // that adding it rounds, and leaves n in the lower bits.
 struct Mass {
     float largest;
